@@ -16,6 +16,8 @@
  *   omc_aggregate_mean           server: mean of R clients' mixed-precision copies        (Sec. 1, 2.5)
  *   omc_reselect                 a new round's quantized subset without a full-precision copy (Sec. 2.5)
  *   omc_transport_pack / _open   the packed set as one self-describing message / checkpoint  (Sec. 1)
+ *   omc_mx4_*                    a linear layer on 4-bit microscaled operands, forward and backward
+ *   omc_layer_norm, _backward    the norm in front of it
  *
  * Conventions that hold for every entry point
  *   - "device" pointers are HIP device memory owned by the caller; "host" pointers are ordinary
@@ -29,7 +31,7 @@
  *     OMC_ERR_DEVICE is the HIP runtime refusing a launch; a call that needs several launches may
  *     then already have enqueued the earlier ones, so the buffers it writes are undefined.
  *   - Device buffers of packed codes, fp32 values, gradients and optimizer state must be
- *     16-byte aligned (OMC_ERR_ALIGN otherwise).
+ *     16-byte aligned (OMC_ERR_ALIGN otherwise); omc_mx4_* and omc_layer_norm* say what theirs need.
  *
  * Format (Sec. 2.2; notation SxEyMz of Sec. 3.1, x = 1).  A code has B = 1 + E + M bits,
  * most significant first [sign | e : E bits | m : M bits].
@@ -440,6 +442,93 @@ omc_status omc_dw_update_recompress(const uint16_t *X, const uint16_t *dY, void 
                                     float *sb, int use_pvt, float *state0, float *state1,
                                     const omc_opt *opt, float *dW_out, uint32_t M, uint32_t N, uint32_t K,
                                     void *ws, size_t ws_bytes, void *stream);
+
+/* ---- a linear layer in 4-bit microscaled floats -------------------------------------------------
+ * MX4: 32 neighbouring values share a power of two and hold an E2M1 value each (0, 0.5, 1, 1.5, 2, 3, 4, 6 and their
+ * negatives).  With a the largest magnitude of the 32,
+ *     e = max(floor(log2 a) - 2, -127),   value_i = 2^e * E2M1(x_i * 2^-e),
+ * nearest, ties to the even code, saturating at 6 (a lies in [4, 8) units).  A value that is not finite makes all 32 NaN.
+ *
+ * A matrix of `rows` rows along which `cols` values are blocked is held in two buffers.
+ *     codes    omc_mx4_code_bytes: row r begins at byte r * 64 * ceil(cols / 128); value k of it in byte k / 2, the even one in the
+ *              low four bits: sign, then the index of the magnitude above
+ *     scales   omc_mx4_scale_bytes: row r begins at byte r * 4 * ceil(cols / 128), a byte e + 127 for every block; 255: its values are NaN
+ * Rows are padded to whole multiples of 128 values with codes 0 and scales 0.  codes must be 16-byte aligned, scales 4-byte aligned; other
+ * tensors here need only the alignment of their elements, and rows of theirs may lie apart (ld = elements from one row to the next, at least
+ * a row's length).  A dimension must lie in 1 .. 2^24 (OMC_ERR_SIZE). */
+typedef enum { OMC_F32 = 0, OMC_BF16 = 1 } omc_type; /* fp32, bfloat16 bit patterns; others are OMC_ERR_FORMAT */
+
+/* Bytes of the two buffers; 0 if a dimension is out of range. */
+size_t omc_mx4_code_bytes(uint32_t rows, uint32_t cols);
+size_t omc_mx4_scale_bytes(uint32_t rows, uint32_t cols);
+
+/* A matrix to MX4, blocked along its rows, along its columns, or both from one read.
+ *   x                  device, rows x cols values of `type`, row stride ldx
+ *   codes, scales      device, the matrix blocked along its rows (rows x cols); both or neither
+ *   codes_t, scales_t  device, its transpose blocked along the matrix's columns (cols x rows); both or neither
+ *   values             device or NULL, rows x cols of `type`, row stride ldv: the values that codes and scales stand for (exact)
+ * At least one output (OMC_ERR_NULL).  Outputs are written whole, paddings too, and must not overlap x. */
+omc_status omc_mx4_quantize(const void *x, omc_type type, uint32_t rows, uint32_t cols, uint64_t ldx, void *codes, void *scales, void *codes_t,
+                            void *scales_t, void *values, uint64_t ldv, void *stream);
+
+/* C[M x N] = A[M x K] * B[N x K]^T + bias on operands in MX4, both blocked along K; fp32 sums, rounded once to c_type.
+ *   bias     device, N floats, or NULL
+ *   C        device, row stride ldc
+ *   ws       device workspace of omc_mx4_gemm_workspace_bytes(M, N, K) bytes, 16-byte aligned (may be 0: then ws may be NULL)
+ * The order of the sums is fixed by the sizes alone.  Sums below 2^-126 may be flushed to zero by the matrix cores. */
+size_t omc_mx4_gemm_workspace_bytes(uint32_t M, uint32_t N, uint32_t K);
+omc_status omc_mx4_gemm(const void *a_codes, const void *a_scales, const void *b_codes, const void *b_scales, const float *bias, void *C,
+                        omc_type c_type, uint64_t ldc, uint32_t M, uint32_t N, uint32_t K, void *ws, size_t ws_bytes, void *stream);
+
+/* A layer's forward pass: Y[M x N] = Q(X) * W^T + bias, X[M x K] rounded to MX4 along its rows on the way.  The same bits as omc_mx4_quantize and
+ * omc_mx4_gemm one after the other would give but for the order of the sums; from one row (a frame of a stream) to whole batches.
+ *   X                   device, of x_type, row stride ldx
+ *   w_codes, w_scales   device, the weights in MX4, N rows blocked along K
+ *   bias                device, N floats, or NULL
+ *   Y                   device, of y_type, row stride ldy
+ *   ws                  device workspace of omc_mx4_linear_workspace_bytes(M, N, K) bytes, 16-byte aligned */
+size_t omc_mx4_linear_workspace_bytes(uint32_t M, uint32_t N, uint32_t K);
+omc_status omc_mx4_linear(const void *X, omc_type x_type, uint64_t ldx, const void *w_codes, const void *w_scales, const float *bias, void *Y,
+                          omc_type y_type, uint64_t ldy, uint32_t M, uint32_t N, uint32_t K, void *ws, size_t ws_bytes, void *stream);
+
+/* A layer's backward pass, the gradients taken straight through the rounding:
+ *     dX[M x K] = Q(dY) * W'^T      dY rounded along its rows, W' the weights blocked along N
+ *     dW[K x N] = Q(X^T) * Q(dY^T)^T   both rounded along the batch
+ *     dbias[N]  = sum over the rows of dY, not rounded
+ *   dY, X               device, of `type` both, row strides lddy and ldx
+ *   w_codes, w_scales   device, the weights in MX4, K rows blocked along N; not needed without dX
+ *   dX                  device, of dx_type, row stride lddx, or NULL
+ *   dW                  device, K*N floats, or NULL: the gradient as omc_step_update_recompress takes it for a K x N variable.  X is not needed without it
+ *   dbias               device, N floats, or NULL
+ *   ws                  device workspace of omc_mx4_linear_backward_workspace_bytes(M, N, K) bytes, 16-byte aligned
+ * At least one output (OMC_ERR_NULL).  Every sum's order is fixed by the sizes. */
+size_t omc_mx4_linear_backward_workspace_bytes(uint32_t M, uint32_t N, uint32_t K);
+omc_status omc_mx4_linear_backward(const void *dY, uint64_t lddy, const void *X, uint64_t ldx, omc_type type, const void *w_codes,
+                                   const void *w_scales, void *dX, omc_type dx_type, uint64_t lddx, float *dW, float *dbias, uint32_t M,
+                                   uint32_t N, uint32_t K, void *ws, size_t ws_bytes, void *stream);
+
+/* ---- layer norm ---------------------------------------------------------------------------------
+ * Its weights are the vectors that stay fp32 in a variable set (Sec. 2.4).  For every row x of `cols` values
+ *     mean = sum x / cols,   rstd = 1 / sqrt(sum (x - mean)^2 / cols + eps),   y = (x - mean) * rstd * gamma + beta
+ * in fp32, rounded once to y's type.  Rows and cols in 1 .. 2^24 (OMC_ERR_SIZE), eps finite and not negative (OMC_ERR_OPT).
+ *   x, y          device, of x_type and y_type, row strides ldx and ldy
+ *   gamma, beta   device, cols floats each; NULL: 1 and 0
+ *   mean, rstd    device, a float for every row, for the backward pass; NULL: not kept */
+omc_status omc_layer_norm(const void *x, omc_type x_type, uint64_t ldx, const float *gamma, const float *beta, float eps, void *y,
+                          omc_type y_type, uint64_t ldy, float *mean, float *rstd, uint32_t rows, uint32_t cols, void *stream);
+
+/* Its backward pass.  With xhat = (x - mean) * rstd and u = dy * gamma,
+ *     dx = rstd * (u - sum u / cols - xhat * sum (u * xhat) / cols),   dgamma = sum over rows of dy * xhat,   dbeta = sum over rows of dy.
+ *   dy              device, of dy_type (y's), row stride lddy
+ *   x, dx           device, of x_type, row strides ldx and lddx; dx NULL: not wanted
+ *   mean, rstd      device, as the forward pass left them
+ *   dgamma, dbeta   device, cols floats each, or NULL; at least one output (OMC_ERR_NULL)
+ *   ws              device workspace of omc_layer_norm_backward_workspace_bytes(rows, cols) bytes, 16-byte aligned
+ * The order of the sums is fixed by the sizes. */
+size_t omc_layer_norm_backward_workspace_bytes(uint32_t rows, uint32_t cols);
+omc_status omc_layer_norm_backward(const void *dy, omc_type dy_type, uint64_t lddy, const void *x, omc_type x_type, uint64_t ldx,
+                                   const float *gamma, const float *mean, const float *rstd, void *dx, uint64_t lddx, float *dgamma,
+                                   float *dbeta, uint32_t rows, uint32_t cols, void *ws, size_t ws_bytes, void *stream);
 
 #ifdef __cplusplus
 }

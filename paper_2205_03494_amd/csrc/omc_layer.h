@@ -1,0 +1,81 @@
+// Launchers of the layer's operators: 4-bit microscaled products and the layer norm.  Arguments already validated; return hipError_t as int.
+#pragma once
+#include <cstddef>
+#include <cstdint>
+
+#include "omc.h"
+
+namespace omc {
+
+// A matrix in MX4: rows of `blocks` blocks of 32 values (whole multiples of 4 blocks), 16 bytes of codes and a scale byte each.
+struct Mx4 {
+    const uint8_t *codes, *scales;
+};
+constexpr uint32_t mx4_padded(uint32_t cols) { return (cols + 127) / 128 * 128; }   // (cols <= 2^32 - 128)
+constexpr uint64_t mx4_code_bytes(uint64_t rows, uint32_t cols) { return rows * (mx4_padded(cols) / 2); }
+constexpr uint64_t mx4_scale_bytes(uint64_t rows, uint32_t cols) { return rows * (mx4_padded(cols) / 32); }
+
+struct QuantArgs {
+    const void *x;
+    uint64_t ldx;
+    uint32_t rows, cols;
+    uint8_t *codes, *scales;       // blocks along a row; may be null
+    uint8_t *codes_t, *scales_t;   // blocks along a column; may be null
+    void *values;                  // may be null
+    uint64_t ldv;
+    float *colsum;                 // partial sums of the columns, one row of them for every 128 rows of x; may be null
+};
+int launch_mx4_quantize(const QuantArgs &qa, bool bf16, void *stream);
+
+struct Mx4GemmArgs {
+    Mx4 a, b;
+    const float *bias;
+    void *c;
+    uint64_t ldc;
+    uint32_t M, N, K;
+    float *parts;                  // partial results of a split contraction
+};
+// c = a b^T + bias, c in bf16 or fp32.
+size_t mx4_gemm_workspace(uint32_t M, uint32_t N, uint32_t K);   // bytes of parts
+int launch_mx4_gemm(const Mx4GemmArgs &ga, bool bf16, void *stream);
+// The same for few rows of a.  Where mx4_few_rounds, these may come as they are (`rows`), and are rounded on the way.
+constexpr uint32_t kMx4FewRows = 64;
+struct Mx4Rows {
+    const void *x;
+    uint64_t ldx;
+    bool bf16;
+};
+bool mx4_few_rounds(uint32_t M, uint32_t N, uint32_t K);
+int launch_mx4_few(const Mx4GemmArgs &ga, const Mx4Rows *rows, bool bf16, void *stream);
+
+// Of `count` rows of partial sums, `width` floats each: the columns' sums, the first `cols` of them to out0, the others to out1 (either may be null).
+int launch_column_sums(const float *parts, uint32_t count, uint32_t cols, uint32_t width, float *out0, float *out1, void *stream);
+
+struct NormArgs {
+    const void *x;
+    uint64_t ldx;
+    const float *gamma, *beta;
+    float eps;
+    void *y;
+    uint64_t ldy;
+    float *mean, *rstd;
+    uint32_t rows, cols;
+};
+int launch_layer_norm(const NormArgs &na, bool x_bf16, bool y_bf16, void *stream);
+
+struct NormGradArgs {
+    const void *dy;
+    uint64_t lddy;
+    const void *x;
+    uint64_t ldx;
+    const float *gamma, *mean, *rstd;
+    void *dx;
+    uint64_t lddx;
+    float *dgamma, *dbeta;
+    uint32_t rows, cols;
+    float *parts;
+};
+size_t layer_norm_backward_workspace(uint32_t rows, uint32_t cols);
+int launch_layer_norm_backward(const NormGradArgs &na, bool x_bf16, bool dy_bf16, void *stream);
+
+}  // namespace omc

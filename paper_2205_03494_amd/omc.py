@@ -103,6 +103,21 @@ _dw = _sig("omc_dw_update_recompress", C.c_int, _vp, _vp, _vp, omc_format, _vp, 
            C.c_uint32, C.c_uint32, C.c_uint32, _vp, C.c_size_t, _vp)
 _gemm_dx = _sig("omc_dequant_gemm_dx", C.c_int, _vp, _vp, omc_format, _vp, _vp, C.c_uint32, C.c_uint32,
                 C.c_uint32, _vp, C.c_size_t, _vp)
+_i, _u32, _u64, _sz = C.c_int, C.c_uint32, C.c_uint64, C.c_size_t
+_mx4_codes = _sig("omc_mx4_code_bytes", _sz, _u32, _u32)
+_mx4_scales = _sig("omc_mx4_scale_bytes", _sz, _u32, _u32)
+_mx4_quantize = _sig("omc_mx4_quantize", _i, _vp, _i, _u32, _u32, _u64, _vp, _vp, _vp, _vp, _vp, _u64, _vp)
+_mx4_gemm_ws = _sig("omc_mx4_gemm_workspace_bytes", _sz, _u32, _u32, _u32)
+_mx4_gemm = _sig("omc_mx4_gemm", _i, _vp, _vp, _vp, _vp, _vp, _vp, _i, _u64, _u32, _u32, _u32, _vp, _sz, _vp)
+_mx4_linear_ws = _sig("omc_mx4_linear_workspace_bytes", _sz, _u32, _u32, _u32)
+_mx4_linear = _sig("omc_mx4_linear", _i, _vp, _i, _u64, _vp, _vp, _vp, _vp, _i, _u64, _u32, _u32, _u32, _vp, _sz, _vp)
+_mx4_backward_ws = _sig("omc_mx4_linear_backward_workspace_bytes", _sz, _u32, _u32, _u32)
+_mx4_backward = _sig("omc_mx4_linear_backward", _i, _vp, _u64, _vp, _u64, _i, _vp, _vp, _vp, _i, _u64, _vp, _vp, _u32, _u32, _u32, _vp,
+                     _sz, _vp)
+_norm = _sig("omc_layer_norm", _i, _vp, _i, _u64, _vp, _vp, C.c_float, _vp, _i, _u64, _vp, _vp, _u32, _u32, _vp)
+_norm_backward_ws = _sig("omc_layer_norm_backward_workspace_bytes", _sz, _u32, _u32)
+_norm_backward = _sig("omc_layer_norm_backward", _i, _vp, _i, _u64, _vp, _i, _u64, _vp, _vp, _vp, _vp, _u64, _vp, _vp, _u32, _u32, _vp,
+                      _sz, _vp)
 
 EXPORTED = ["omc_status_string", "omc_format_validate", "omc_format_bits", "omc_format_max",
             "omc_packed_bytes", "omc_compress_workspace_bytes", "omc_compress", "omc_decompress",
@@ -116,7 +131,11 @@ EXPORTED = ["omc_status_string", "omc_format_validate", "omc_format_bits", "omc_
             "omc_aggregate_plan_bytes", "omc_aggregate_plan_build",
             "omc_aggregate_mean", "omc_dequant_gemm_workspace_bytes",
             "omc_dequant_gemm", "omc_dequant_gemm_dx", "omc_dw_update_workspace_bytes",
-            "omc_dw_update_recompress"]
+            "omc_dw_update_recompress",
+            "omc_mx4_code_bytes", "omc_mx4_scale_bytes", "omc_mx4_quantize", "omc_mx4_gemm_workspace_bytes", "omc_mx4_gemm",
+            "omc_mx4_linear_workspace_bytes", "omc_mx4_linear", "omc_mx4_linear_backward_workspace_bytes",
+            "omc_mx4_linear_backward", "omc_layer_norm", "omc_layer_norm_backward_workspace_bytes",
+            "omc_layer_norm_backward"]
 
 
 class OmcError(RuntimeError):
@@ -438,3 +457,145 @@ def omc_aggregate_mean(agg: AggregatePlan, arenas: Sequence[torch.Tensor], sb_ta
     sp = (C.c_void_p * R)(*[_ptr(s) for s in sb_tables])
     _check(_agg_mean(agg.host.ctypes.data, _ptr(agg.dev), ap, ab, sp, _ptr(out), out.numel(), _stream(stream)),
            "omc_aggregate_mean")
+
+
+# --------------------------------------------------------------------------- a linear layer in 4-bit microscaled floats, and layer norm
+OMC_F32, OMC_BF16 = 0, 1
+_TYPES = {torch.float32: OMC_F32, torch.bfloat16: OMC_BF16}
+
+
+def _matrix(t: torch.Tensor):
+    """(pointer, type, row stride) of a device matrix whose rows are contiguous."""
+    if not t.is_cuda or t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1):
+        raise ValueError("a device matrix with contiguous rows is expected")
+    kind = _TYPES.get(t.dtype)
+    if kind is None:
+        raise ValueError(f"fp32 or bfloat16 is expected, not {t.dtype}")
+    rows, cols = t.shape
+    return t.data_ptr(), kind, t.stride(0) if rows > 1 else cols
+
+
+def _rows_like(t: torch.Tensor, rows: int, cols: int):
+    if t.shape[0] != rows or t.shape[1] != cols:
+        raise ValueError(f"{rows} x {cols} is expected, not {tuple(t.shape)}")
+    return _matrix(t)
+
+
+def _floats(t: Optional[torch.Tensor], n: int):
+    if t is None:
+        return None
+    if t.dtype != torch.float32 or t.numel() != n:
+        raise ValueError(f"{n} fp32 values are expected")
+    return _ptr(t)
+
+
+def _bytes(t: Optional[torch.Tensor], n: int):
+    if t is None:
+        return None
+    if t.dtype != torch.uint8 or t.numel() != n:
+        raise ValueError(f"{n} bytes are expected")
+    return _ptr(t)
+
+
+def _space(ws: Optional[torch.Tensor]):
+    return (None, 0) if ws is None else (_ptr(ws), ws.numel() * ws.element_size())
+
+
+def omc_mx4_code_bytes(rows: int, cols: int) -> int:
+    return _mx4_codes(rows, cols)
+
+
+def omc_mx4_scale_bytes(rows: int, cols: int) -> int:
+    return _mx4_scales(rows, cols)
+
+
+def omc_mx4_gemm_workspace_bytes(M: int, N: int, K: int) -> int:
+    return _mx4_gemm_ws(M, N, K)
+
+
+def omc_mx4_linear_workspace_bytes(M: int, N: int, K: int) -> int:
+    return _mx4_linear_ws(M, N, K)
+
+
+def omc_mx4_linear_backward_workspace_bytes(M: int, N: int, K: int) -> int:
+    return _mx4_backward_ws(M, N, K)
+
+
+def omc_layer_norm_backward_workspace_bytes(rows: int, cols: int) -> int:
+    return _norm_backward_ws(rows, cols)
+
+
+def omc_mx4_quantize(x: torch.Tensor, codes: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None,
+                     codes_t: Optional[torch.Tensor] = None, scales_t: Optional[torch.Tensor] = None,
+                     values: Optional[torch.Tensor] = None, stream=None) -> None:
+    """x [rows, cols] in fp32 or bf16; codes and scales: uint8 buffers of omc_mx4_*_bytes(rows, cols); codes_t and scales_t of
+    omc_mx4_*_bytes(cols, rows): the transpose, blocked along x's columns; values: like x, what the codes stand for."""
+    rows, cols = x.shape
+    px, kind, ldx = _matrix(x)
+    pv, vkind, ldv = (None, kind, 0) if values is None else _rows_like(values, rows, cols)
+    if vkind != kind:
+        raise ValueError("values have x's type")
+    _check(_mx4_quantize(px, kind, rows, cols, ldx, _bytes(codes, _mx4_codes(rows, cols)), _bytes(scales, _mx4_scales(rows, cols)),
+                         _bytes(codes_t, _mx4_codes(cols, rows)), _bytes(scales_t, _mx4_scales(cols, rows)), pv, ldv,
+                         _stream(stream)), "omc_mx4_quantize")
+
+
+def omc_mx4_gemm(a_codes: torch.Tensor, a_scales: torch.Tensor, b_codes: torch.Tensor, b_scales: torch.Tensor,
+                 bias: Optional[torch.Tensor], Cout: torch.Tensor, K: int, ws: Optional[torch.Tensor], stream=None) -> None:
+    """Cout [M, N] in fp32 or bf16 = A [M x K] B [N x K]^T + bias."""
+    M, N = Cout.shape
+    pc, kind, ldc = _matrix(Cout)
+    _check(_mx4_gemm(_bytes(a_codes, _mx4_codes(M, K)), _bytes(a_scales, _mx4_scales(M, K)), _bytes(b_codes, _mx4_codes(N, K)),
+                     _bytes(b_scales, _mx4_scales(N, K)), _floats(bias, N), pc, kind, ldc, M, N, K, *_space(ws),
+                     _stream(stream)), "omc_mx4_gemm")
+
+
+def omc_mx4_linear(X: torch.Tensor, w_codes: torch.Tensor, w_scales: torch.Tensor, bias: Optional[torch.Tensor], Y: torch.Tensor,
+                   ws: Optional[torch.Tensor], stream=None) -> None:
+    """Y [M, N] = Q(X [M, K]) W^T + bias; w_codes, w_scales: the weights, N rows blocked along K."""
+    M, K = X.shape
+    N = Y.shape[1]
+    px, xkind, ldx = _matrix(X)
+    py, ykind, ldy = _rows_like(Y, M, N)
+    _check(_mx4_linear(px, xkind, ldx, _bytes(w_codes, _mx4_codes(N, K)), _bytes(w_scales, _mx4_scales(N, K)), _floats(bias, N), py,
+                       ykind, ldy, M, N, K, *_space(ws), _stream(stream)), "omc_mx4_linear")
+
+
+def omc_mx4_linear_backward(dY: torch.Tensor, X: Optional[torch.Tensor], w_codes: Optional[torch.Tensor],
+                            w_scales: Optional[torch.Tensor], dX: Optional[torch.Tensor], dW: Optional[torch.Tensor],
+                            dbias: Optional[torch.Tensor], ws: torch.Tensor, stream=None) -> None:
+    """dY [M, N], X [M, K]; w_codes, w_scales: the weights, K rows blocked along N; dX [M, K], dW [K, N] fp32, dbias [N] fp32, each
+    or None.  Without dX the weights, without dW X may be None (K is taken from whichever is there)."""
+    M, N = dY.shape
+    K = next((t.shape[d] for t, d in ((X, 1), (dX, 1), (dW, 0)) if t is not None), 1)
+    pdy, kind, lddy = _matrix(dY)
+    px, xkind, ldx = (None, kind, 0) if X is None else _rows_like(X, M, K)
+    if xkind != kind:
+        raise ValueError("dY and X are of one type")
+    pdx, dxkind, lddx = (None, kind, 0) if dX is None else _rows_like(dX, M, K)
+    _check(_mx4_backward(pdy, lddy, px, ldx, kind, _bytes(w_codes, _mx4_codes(K, N)), _bytes(w_scales, _mx4_scales(K, N)), pdx, dxkind,
+                         lddx, _floats(dW, K * N), _floats(dbias, N), M, N, K, *_space(ws), _stream(stream)),
+           "omc_mx4_linear_backward")
+
+
+def omc_layer_norm(x: torch.Tensor, gamma: Optional[torch.Tensor], beta: Optional[torch.Tensor], eps: float, y: torch.Tensor,
+                   mean: Optional[torch.Tensor] = None, rstd: Optional[torch.Tensor] = None, stream=None) -> None:
+    rows, cols = x.shape
+    px, xkind, ldx = _matrix(x)
+    py, ykind, ldy = _rows_like(y, rows, cols)
+    _check(_norm(px, xkind, ldx, _floats(gamma, cols), _floats(beta, cols), eps, py, ykind, ldy, _floats(mean, rows),
+                 _floats(rstd, rows), rows, cols, _stream(stream)), "omc_layer_norm")
+
+
+def omc_layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, gamma: Optional[torch.Tensor], mean: torch.Tensor, rstd: torch.Tensor,
+                            dx: Optional[torch.Tensor], dgamma: Optional[torch.Tensor], dbeta: Optional[torch.Tensor],
+                            ws: torch.Tensor, stream=None) -> None:
+    rows, cols = x.shape
+    px, xkind, ldx = _matrix(x)
+    pdy, ykind, lddy = _rows_like(dy, rows, cols)
+    pdx, dxkind, lddx = (None, xkind, 0) if dx is None else _rows_like(dx, rows, cols)
+    if dxkind != xkind:
+        raise ValueError("dx has x's type")
+    _check(_norm_backward(pdy, ykind, lddy, px, xkind, ldx, _floats(gamma, cols), _floats(mean, rows), _floats(rstd, rows), pdx, lddx,
+                          _floats(dgamma, cols), _floats(dbeta, cols), rows, cols, *_space(ws), _stream(stream)),
+           "omc_layer_norm_backward")

@@ -1,0 +1,72 @@
+"""Plain 64-bit references of the layer's operators, on the CPU, written from the definitions (numpy)."""
+import numpy as np
+import torch
+
+GRID = np.array([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0])
+
+
+def padded(n):
+    return -(-n // 128) * 128
+
+
+def quantize(x):
+    """(codes [rows, padded / 2], scales [rows, padded / 32], values [rows, cols] in fp64) of a float array, blocked along its rows."""
+    rows, cols = x.shape
+    x = np.asarray(x, dtype=np.float64)
+    wide = np.zeros((rows, padded(cols)))
+    wide[:, :cols] = x
+    b = wide.reshape(rows, -1, 32)
+    bad = ~np.isfinite(b).all(-1)
+    b = np.where(bad[..., None], 0.0, b)
+    top = np.abs(b).max(-1)
+    e = np.where(top > 0, np.frexp(top)[1] - 1 - 2, -127)
+    e = np.maximum(e, -127)
+    u = np.ldexp(np.abs(b), -e[..., None])
+    assert (u < 8).all()
+    code = np.zeros(u.shape, np.int64)
+    best = np.full(u.shape, np.inf)
+    for k in (0, 2, 4, 6, 1, 3, 5, 7):       # of two equally near the even one, which is looked at first
+        d = np.abs(u - GRID[k])
+        code = np.where(d < best, k, code)
+        best = np.minimum(d, best)
+    value = np.ldexp(GRID[code], e[..., None]) * np.where(np.signbit(b), -1.0, 1.0)
+    value[bad] = np.nan
+    code = np.where(np.signbit(b), code + 8, code)
+    code[bad] = 0
+    scale = np.where(bad, 255, e + 127).astype(np.uint8)
+    flat = code.reshape(rows, -1).astype(np.uint8)
+    return flat[:, 0::2] | (flat[:, 1::2] << 4), scale, value.reshape(rows, -1)[:, :cols]
+
+
+def values(codes, scales, cols):
+    """fp64 values of codes and scales."""
+    c = np.stack((codes & 15, codes >> 4), -1).reshape(codes.shape[0], -1).astype(np.int64)
+    v = GRID[c & 7] * np.where(c & 8, -1.0, 1.0)
+    unit = np.where(scales == 255, np.nan, np.ldexp(1.0, scales.astype(np.int64) - 127))
+    return (v * np.repeat(unit, 32, 1))[:, :cols]
+
+
+def layer_norm(x, gamma, beta, eps):
+    mean = x.mean(1, keepdims=True)
+    rstd = 1.0 / np.sqrt(((x - mean) ** 2).mean(1, keepdims=True) + eps)
+    return (x - mean) * rstd * gamma + beta, mean[:, 0], rstd[:, 0]
+
+
+def layer_norm_backward(dy, x, gamma, mean, rstd):
+    hat = (x - mean[:, None]) * rstd[:, None]
+    u = dy * gamma
+    dx = rstd[:, None] * (u - u.mean(1, keepdims=True) - hat * (u * hat).mean(1, keepdims=True))
+    return dx, (dy * hat).sum(0), dy.sum(0)
+
+
+def product_bound(a, b, K):
+    """How far fp32 sums may be from a b^T: K / 128 instructions one after the other, parts joined, two bits of an instruction's own sum."""
+    return (K / 128 + 16) * 2.0 ** -23 * (np.abs(a) @ np.abs(b).T)
+
+
+def rounding(ref, dtype):
+    return np.abs(ref) * (2.0 ** -8 if dtype is torch.bfloat16 else 2.0 ** -23)
+
+
+def as64(t):
+    return t.detach().cpu().to(torch.float64).numpy()

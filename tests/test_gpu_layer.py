@@ -1,0 +1,461 @@
+"""The layer's operators against 64-bit references: MX4 rounding bit for bit, products, both gradients, layer norm."""
+import numpy as np
+import pytest
+import torch
+
+import mx4_ref as ref
+from paper_2205_03494_amd import omc
+
+pytestmark = pytest.mark.gpu
+
+BF16, F32 = torch.bfloat16, torch.float32
+GUARD = 0xA5
+
+
+def tensor(a, dtype, pad=0):
+    """A device matrix, in a wider buffer if pad > 0 (then its rows are as unaligned as pad makes them)."""
+    wide = torch.zeros(a.shape[0], a.shape[1] + pad, dtype=dtype, device="cuda")
+    wide[:, :a.shape[1]] = torch.from_numpy(np.asarray(a, dtype=np.float32)).to(dtype).cuda()
+    return wide[:, :a.shape[1]]
+
+
+def empty(rows, cols, dtype, pad=0):
+    wide = torch.full((rows, cols + pad), 7.0, dtype=dtype, device="cuda")
+    return wide, wide[:, :cols]
+
+
+def untouched(wide, cols):
+    assert (wide[:, cols:] == 7.0).all(), "written past the end of a row"
+
+
+def buffers(rows, cols):
+    nc, ns = omc.omc_mx4_code_bytes(rows, cols), omc.omc_mx4_scale_bytes(rows, cols)
+    c = torch.full((nc + 64,), GUARD, dtype=torch.uint8, device="cuda")
+    s = torch.full((ns + 64,), GUARD, dtype=torch.uint8, device="cuda")
+    return c, s, c[:nc], s[:ns]
+
+
+def guarded(whole, part):
+    assert (whole[part.numel():] == GUARD).all(), "written past the end of a buffer"
+
+
+def inputs(rows, cols, seed, spread=1.0):
+    rng = np.random.default_rng(seed)
+    x = rng.standard_normal((rows, cols)) * spread * np.exp(rng.standard_normal(cols))
+    if rows > 2:
+        x[rng.integers(0, rows)] = 0.0
+    return x
+
+
+def special(rows, cols, seed):
+    """Values at which rounding can go wrong: ties of every binade, zeros of both signs, the smallest and largest, infinities and NaN."""
+    rng = np.random.default_rng(seed)
+    x = rng.integers(-128, 129, (rows, cols)) / 16.0
+    x *= np.exp2(rng.integers(-30, 30, (rows, -(-cols // 32))).repeat(32, 1)[:, :cols].astype(np.float64))
+    flat = x.reshape(-1)
+    some = np.array([0.0, -0.0, 2.0 ** -126, -(2.0 ** -126), 2.0 ** -130, 2.0 ** -133, 3e38, -3e38, 2.0 ** 127, np.inf, -np.inf, np.nan, 1e-38, 7.0, 5.0, 2.5])
+    at = rng.integers(0, flat.size, max(1, flat.size // 97))
+    flat[at] = some[rng.integers(0, some.size, at.size)]
+    if rows > 3:
+        x[1] = 0.0
+        x[2] = -0.0
+        x[3] = 2.0 ** -128 * rng.integers(-3, 4, cols)
+    return x
+
+
+def same_values(got, want):
+    got = ref.as64(got)
+    assert np.array_equal(np.isnan(got), np.isnan(want))
+    assert np.array_equal(np.nan_to_num(got), np.nan_to_num(want))
+
+
+SHAPES = [(1, 1, 0), (1, 31, 0), (2, 32, 1), (5, 33, 0), (33, 64, 3), (127, 128, 0), (128, 130, 1), (131, 257, 7), (300, 100, 0), (64, 2056, 5), (513, 640, 0)]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows,cols,pad", SHAPES)
+@pytest.mark.parametrize("make", [inputs, special])
+def test_quantize(rows, cols, pad, dtype, make):
+    x = tensor(make(rows, cols, rows * 1000 + cols), dtype, pad)
+    x64 = ref.as64(x)
+    codes, scales, values = ref.quantize(x64)
+    codes_t, scales_t, _ = ref.quantize(x64.T)
+    for which in ("rows", "columns", "values", "all"):
+        cw, sw, c, s = buffers(rows, cols)
+        ctw, stw, ct, st = buffers(cols, rows)
+        vw, v = empty(rows, cols, dtype, pad)
+        by_row, by_col = which in ("rows", "all"), which in ("columns", "all")
+        with_values = which in ("values", "all")
+        omc.omc_mx4_quantize(x, *((c, s) if by_row else (None, None)), *((ct, st) if by_col else (None, None)), values=v if with_values else None)
+        if by_row:
+            assert np.array_equal(s.cpu().numpy().reshape(rows, -1), scales)
+            assert np.array_equal(c.cpu().numpy().reshape(rows, -1), codes)
+        if by_col:
+            assert np.array_equal(st.cpu().numpy().reshape(cols, -1), scales_t)
+            assert np.array_equal(ct.cpu().numpy().reshape(cols, -1), codes_t)
+        if with_values:
+            same_values(v, values)
+        untouched(vw, cols)
+        for whole, part in ((cw, c), (sw, s), (ctw, ct), (stw, st)):
+            guarded(whole, part)
+
+
+def random_mx4(rows, cols, seed, nan=False, low=110, high=140):
+    """Any codes and scales, paddings as they have to be; their values."""
+    rng = np.random.default_rng(seed)
+    wide, blocks = ref.padded(cols), -(-cols // 32)
+    codes = rng.integers(0, 256, (rows, wide // 2), dtype=np.uint8)
+    scales = rng.integers(low, high, (rows, wide // 32), dtype=np.uint8)
+    k = np.arange(wide)
+    codes &= ((k[0::2] < cols) * 15 + (k[1::2] < cols) * 240).astype(np.uint8)
+    scales[:, blocks:] = 0
+    if nan:
+        scales[rows // 2, 0] = 255
+    return codes, scales, ref.values(codes, scales, cols)
+
+
+def to_dev(a):
+    return torch.from_numpy(np.ascontiguousarray(a).reshape(-1)).cuda()
+
+
+def workspace(n):
+    """Exactly n bytes, with a guard behind them."""
+    w = torch.full((n + 256,), GUARD, dtype=torch.uint8, device="cuda")
+    return w, w[:n]
+
+
+def check(got, want, bound, dtype):
+    got = ref.as64(got)
+    assert np.array_equal(np.isnan(got), np.isnan(want))
+    ok = ~np.isnan(want)
+    err = np.abs(got - want)[ok]
+    limit = (bound + ref.rounding(np.abs(want) + bound, dtype))[ok]
+    assert (err <= limit).all(), (float(err.max()), float((err / np.maximum(limit, 1e-300)).max()))
+
+
+GEMM = [(1, 1, 1), (1, 16, 32), (3, 17, 33), (16, 64, 128), (17, 100, 129), (29, 200, 1000), (33, 31, 256), (64, 96, 384), (65, 64, 64), (100, 65, 257),
+        (128, 128, 512), (129, 130, 640), (256, 256, 1024), (300, 257, 128), (511, 770, 896), (1000, 300, 4096), (70, 4100, 300), (4099, 70, 200), (2500, 1700, 160)]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("M,N,K", GEMM)
+def test_gemm(M, N, K, dtype):
+    ac, asc, a = random_mx4(M, K, M + K, nan=M > 2)
+    bc, bsc, b = random_mx4(N, K, N + 2 * K + 1, nan=N > 40)
+    bias = np.random.default_rng(7).standard_normal(N).astype(np.float32)
+    whole, ws = workspace(omc.omc_mx4_gemm_workspace_bytes(M, N, K))
+    with np.errstate(invalid="ignore"):
+        want, bound = a @ b.T, ref.product_bound(a, b, K)
+    for with_bias in (False, True):
+        cw, c = empty(M, N, dtype, 5 if with_bias else 0)
+        omc.omc_mx4_gemm(to_dev(ac), to_dev(asc), to_dev(bc), to_dev(bsc), torch.from_numpy(bias).cuda() if with_bias else None, c, K, ws)
+        check(c, want + bias if with_bias else want, bound + 2.0 ** -23 * np.abs(bias) if with_bias else bound, dtype)
+        untouched(cw, N)
+        guarded(whole, ws)
+
+
+def test_gemm_over_all_scales():
+    """Products of the smallest and largest scales; what leaves fp32's range becomes an infinity, what lies below it may become zero."""
+    M, N, K = 80, 96, 160
+    ac, asc, a = random_mx4(M, K, 1, low=0, high=255)
+    bc, bsc, b = random_mx4(N, K, 2, low=0, high=255)
+    asc[:, 1:5] = asc[:, :1]
+    bsc[:, 1:5] = bsc[:, :1]
+    a, b = ref.values(ac, asc, K), ref.values(bc, bsc, K)
+    _, c = empty(M, N, F32)
+    omc.omc_mx4_gemm(to_dev(ac), to_dev(asc), to_dev(bc), to_dev(bsc), None, c, K, workspace(omc.omc_mx4_gemm_workspace_bytes(M, N, K))[1])
+    want, got = a @ b.T, ref.as64(c)
+    in_range = (np.abs(a) @ np.abs(b).T) < 2.0 ** 127
+    err = np.abs(got - want)[in_range]
+    assert (err <= (ref.product_bound(a, b, K) + ref.rounding(want, F32) + K * 2.0 ** -126)[in_range]).all()
+    assert in_range.mean() > 0.3
+
+
+LINEAR = [(1, 1, 1, 0), (1, 4096, 1024, 0), (1, 100, 33, 3), (2, 513, 8192, 1), (7, 48, 2000, 0), (16, 272, 512, 2), (17, 300, 96, 1), (29, 520, 1031, 0), (48, 64, 160, 0),
+          (64, 130, 4096, 0), (65, 200, 200, 1), (257, 384, 300, 0), (1003, 129, 1000, 3)]
+
+
+@pytest.mark.parametrize("x_type,y_type", [(BF16, BF16), (BF16, F32), (F32, BF16), (F32, F32)])
+@pytest.mark.parametrize("M,N,K,pad", LINEAR)
+def test_linear(M, N, K, pad, x_type, y_type):
+    x = tensor(inputs(M, K, M * 7 + K), x_type, pad)
+    wc, wsc, w = random_mx4(N, K, N + K)
+    bias = np.random.default_rng(3).standard_normal(N).astype(np.float32)
+    whole, ws = workspace(omc.omc_mx4_linear_workspace_bytes(M, N, K))
+    a = ref.quantize(ref.as64(x))[2]
+    yw, y = empty(M, N, y_type, pad)
+    omc.omc_mx4_linear(x, to_dev(wc), to_dev(wsc), torch.from_numpy(bias).cuda(), y, ws)
+    check(y, a @ w.T + bias, ref.product_bound(a, w, K) + 2.0 ** -23 * np.abs(bias), y_type)
+    untouched(yw, N)
+    guarded(whole, ws)
+
+
+@pytest.mark.parametrize("M", [1, 16, 40, 300])
+def test_rows_that_are_not_finite_stay_alone(M):
+    N, K = 70, 512
+    x = inputs(M, K, 5)
+    x[M // 2, 100] = np.inf
+    if M > 20:
+        x[20, 3] = np.nan
+    wc, wsc, w = random_mx4(N, K, 9)
+    a = ref.quantize(ref.as64(tensor(x, BF16)))[2]
+    _, y = empty(M, N, F32)
+    omc.omc_mx4_linear(tensor(x, BF16), to_dev(wc), to_dev(wsc), None, y, workspace(omc.omc_mx4_linear_workspace_bytes(M, N, K))[1])
+    with np.errstate(invalid="ignore"):
+        check(y, a @ w.T, ref.product_bound(a, w, K), F32)
+
+
+BACKWARD = [(1, 1, 1, 0), (1, 64, 96, 0), (3, 33, 65, 1), (40, 96, 300, 0), (128, 64, 64, 0), (129, 257, 130, 3), (300, 520, 70, 0), (1003, 243, 97, 1), (2100, 128, 384, 0)]
+
+
+@pytest.mark.parametrize("dtype,dx_type", [(BF16, BF16), (F32, F32), (BF16, F32)])
+@pytest.mark.parametrize("M,N,K,pad", BACKWARD)
+def test_linear_backward(M, N, K, pad, dtype, dx_type):
+    x, dy = tensor(inputs(M, K, M + 3), dtype, pad), tensor(inputs(M, N, M + 4, 1e-3), dtype, pad)
+    wc, wsc, w = random_mx4(K, N, N + K)
+    x64, dy64 = ref.as64(x), ref.as64(dy)
+    dyq, dyt, xt = ref.quantize(dy64)[2], ref.quantize(dy64.T)[2], ref.quantize(x64.T)[2]
+    whole, ws = workspace(omc.omc_mx4_linear_backward_workspace_bytes(M, N, K))
+    for which in ("all", "dx", "dw", "dbias"):
+        dxw, dx = empty(M, K, dx_type, pad)
+        dw, dbias = torch.full((K, N), 7.0, device="cuda"), torch.full((N,), 7.0, device="cuda")
+        omc.omc_mx4_linear_backward(dy, None if which in ("dx", "dbias") else x, *((None, None) if which in ("dw", "dbias") else (to_dev(wc), to_dev(wsc))),
+                                    dx if which in ("all", "dx") else None, dw if which in ("all", "dw") else None,
+                                    dbias if which in ("all", "dbias") else None, ws)
+        if which in ("all", "dx"):
+            check(dx, dyq @ w.T, ref.product_bound(dyq, w, N), dx_type)
+        if which in ("all", "dw"):
+            check(dw, xt @ dyt.T, ref.product_bound(xt, dyt, M), F32)
+        if which in ("all", "dbias"):   # chains of 32, then of the 128s' sums
+            check(dbias, dy64.sum(0), (64 + M / 128) * 2.0 ** -24 * np.abs(dy64).sum(0), F32)
+        untouched(dxw, K)
+        guarded(whole, ws)
+
+
+def test_linear_backward_against_differences():
+    """On values that MX4 holds exactly in both directions the layer is linear and its gradients are exact: differences give the same numbers."""
+    rng = np.random.default_rng(11)
+    M, N, K = 96, 64, 160
+    pick = lambda *shape: rng.choice(np.concatenate((ref.GRID, -ref.GRID)), shape)
+    x, w, dy = pick(M, K), pick(N, K), pick(M, N)
+    wt = w.T.copy()                      # K x N, blocked along N
+    cw, sw = [torch.from_numpy(a.reshape(-1)).cuda() for a in ref.quantize(w)[:2]]
+    cwt, swt = [torch.from_numpy(a.reshape(-1)).cuda() for a in ref.quantize(wt)[:2]]
+    ws = workspace(max(omc.omc_mx4_linear_backward_workspace_bytes(M, N, K), omc.omc_mx4_linear_workspace_bytes(M, N, K)))[1]
+    dx, dw, dbias = torch.empty(M, K, device="cuda"), torch.empty(K, N, device="cuda"), torch.empty(N, device="cuda")
+    omc.omc_mx4_linear_backward(tensor(dy, F32), tensor(x, F32), cwt, swt, dx, dw, dbias, ws)
+    loss = lambda x, cw, sw, b: _loss(x, cw, sw, b, dy, ws)
+    base = loss(x, cw, sw, np.zeros(N))
+    for _ in range(6):
+        m, k, n = rng.integers(M), rng.integers(K), rng.integers(N)
+        moved = x.copy()
+        moved[m, k] = 0.5 if x[m, k] != 0.5 else 1.0
+        assert loss(moved, cw, sw, np.zeros(N)) - base == dx[m, k].item() * (moved[m, k] - x[m, k])
+        other = w.copy()
+        other[n, k] = 0.5 if w[n, k] != 0.5 else 1.0
+        co, so = [torch.from_numpy(a.reshape(-1)).cuda() for a in ref.quantize(other)[:2]]
+        assert loss(x, co, so, np.zeros(N)) - base == dw[k, n].item() * (other[n, k] - w[n, k])
+        b = np.zeros(N)
+        b[n] = 0.25
+        assert loss(x, cw, sw, b) - base == dbias[n].item() * 0.25
+
+
+def _loss(x, cw, sw, b, dy, ws):
+    y = torch.empty(x.shape[0], dy.shape[1], device="cuda")
+    omc.omc_mx4_linear(tensor(x, F32), cw, sw, torch.from_numpy(b.astype(np.float32)).cuda(), y, ws)
+    return float((ref.as64(y) * dy).sum())
+
+
+NORM = [(1, 1, 0), (1, 512, 0), (2, 7, 1), (3, 64, 0), (5, 511, 1), (9, 513, 0), (33, 1000, 3), (4, 1024, 0), (7, 2047, 1), (6, 2056, 0), (5, 4096, 0), (3, 5001, 2),
+        (4, 8192, 0), (3, 8195, 1), (2, 16384, 0), (3, 16385, 0), (2, 40000, 1), (2500, 96, 0), (9000, 40, 0)]
+TYPES = [(F32, F32), (F32, BF16), (BF16, BF16), (BF16, F32)]
+
+
+def norm_inputs(rows, cols, seed):
+    rng = np.random.default_rng(seed)
+    x = rng.standard_normal((rows, cols)) * np.exp(0.5 * rng.standard_normal(cols)) + 0.5 * rng.standard_normal(cols)
+    if rows > 2:
+        x[1] = 0.0
+        x[2] += 100.0
+    return x, rng.standard_normal(cols).astype(np.float32), rng.standard_normal(cols).astype(np.float32)
+
+
+@pytest.mark.parametrize("x_type,y_type", TYPES)
+@pytest.mark.parametrize("rows,cols,pad", NORM)
+def test_layer_norm(rows, cols, pad, x_type, y_type):
+    x, gamma, beta = norm_inputs(rows, cols, rows + cols)
+    xd = tensor(x, x_type, pad)
+    x64 = ref.as64(xd)
+    for affine, eps in ((True, 1e-5), (False, 1e-3)):
+        yw, y = empty(rows, cols, y_type, pad)
+        mean, rstd = torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+        g, b = (gamma, beta) if affine else (np.ones(cols), np.zeros(cols))
+        omc.omc_layer_norm(xd, torch.from_numpy(gamma).cuda() if affine else None, torch.from_numpy(beta).cuda() if affine else None, eps, y,
+                           mean if affine else None, rstd if affine else None)
+        want, mean64, rstd64 = ref.layer_norm(x64, g.astype(np.float64), b.astype(np.float64), eps)
+        # chains of fp32 sums of up to 64 additions (a long row: cols / 1024 more): the mean's error by the row's largest value, the others follow from it
+        chain = (64 + cols / 1024) * 2.0 ** -24
+        off = chain * np.abs(x64).max(1, keepdims=True)
+        rel = 4 * chain + 2 * off * rstd64[:, None]           # of rstd
+        bound = np.abs(g) * (off * rstd64[:, None] + np.abs((x64 - mean64[:, None]) * rstd64[:, None]) * rel) + 2.0 ** -22 * np.abs(b)
+        check(y, want, bound, y_type)
+        untouched(yw, cols)
+        if affine:
+            assert (np.abs(ref.as64(mean) - mean64) <= off[:, 0] + 1e-300).all()
+            assert (np.abs(ref.as64(rstd) - rstd64) <= rel[:, 0] * rstd64).all()
+
+
+@pytest.mark.parametrize("x_type,dy_type", TYPES)
+@pytest.mark.parametrize("rows,cols,pad", NORM)
+def test_layer_norm_backward(rows, cols, pad, x_type, dy_type):
+    x, gamma, _ = norm_inputs(rows, cols, rows + cols + 1)
+    xd, dyd = tensor(x, x_type, pad), tensor(inputs(rows, cols, 77, 1e-2), dy_type, pad)
+    x64, dy64 = ref.as64(xd), ref.as64(dyd)
+    _, mean, rstd = ref.layer_norm(x64, 1.0, 0.0, 1e-5)
+    mean, rstd = mean.astype(np.float32), rstd.astype(np.float32)
+    whole, ws = workspace(omc.omc_layer_norm_backward_workspace_bytes(rows, cols))
+    hat = (x64 - mean[:, None].astype(np.float64)) * rstd[:, None]
+    hat_off = 2.0 ** -22 * (np.abs(hat) + np.abs(x64) * rstd[:, None])
+    for which in ("all", "dx", "dgamma", "dbeta"):
+        g = gamma.astype(np.float64) if which != "dx" else np.ones(cols)
+        dx64, dg64, db64 = ref.layer_norm_backward(dy64, x64, g, mean.astype(np.float64), rstd.astype(np.float64))
+        dxw, dx = empty(rows, cols, x_type, pad)
+        dg, db = torch.full((cols,), 7.0, device="cuda"), torch.full((cols,), 7.0, device="cuda")
+        omc.omc_layer_norm_backward(dyd, xd, torch.from_numpy(gamma).cuda() if which != "dx" else None, torch.from_numpy(mean).cuda(), torch.from_numpy(rstd).cuda(),
+                                    dx if which in ("all", "dx") else None, dg if which in ("all", "dgamma") else None,
+                                    db if which in ("all", "dbeta") else None, ws)
+        chain = (64 + cols / 1024) * 2.0 ** -24
+        if which in ("all", "dx"):
+            u = np.abs(dy64 * g)
+            uh = u * np.abs(hat)
+            part = chain * (u.mean(1, keepdims=True) + np.abs(hat) * uh.mean(1, keepdims=True)) + hat_off * np.abs((dy64 * g * hat).mean(1, keepdims=True))
+            part += np.abs(hat) * (u * hat_off).mean(1, keepdims=True)
+            check(dx, dx64, rstd[:, None] * (part + 2.0 ** -22 * (u + u.mean(1, keepdims=True) + np.abs(hat) * uh.mean(1, keepdims=True))), x_type)
+        chain = (64 + rows / 32) * 2.0 ** -24
+        if which in ("all", "dgamma"):
+            check(dg, dg64, chain * np.abs(dy64 * hat).sum(0) + (np.abs(dy64) * hat_off).sum(0), F32)
+        if which in ("all", "dbeta"):
+            check(db, db64, chain * np.abs(dy64).sum(0), F32)
+        untouched(dxw, cols)
+        guarded(whole, ws)
+
+
+def test_layer_norm_backward_against_differences():
+    rng = np.random.default_rng(5)
+    rows, cols, eps = 6, 200, 1e-5
+    x, dy, gamma, beta = (rng.standard_normal(s) for s in ((rows, cols), (rows, cols), cols, cols))
+    xd, gd = tensor(x, F32), torch.from_numpy(gamma.astype(np.float32)).cuda()
+    x, gamma, dy = ref.as64(xd), ref.as64(gd), ref.as64(tensor(dy, F32))
+    mean, rstd, y = torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda"), torch.empty(rows, cols, device="cuda")
+    omc.omc_layer_norm(xd, gd, None, eps, y, mean, rstd)
+    dx, dg, db = torch.empty(rows, cols, device="cuda"), torch.empty(cols, device="cuda"), torch.empty(cols, device="cuda")
+    omc.omc_layer_norm_backward(tensor(dy, F32), xd, gd, mean, rstd, dx, dg, db, workspace(omc.omc_layer_norm_backward_workspace_bytes(rows, cols))[1])
+    loss = lambda x, g, b: float((ref.layer_norm(x, g, b, eps)[0] * dy).sum())
+    h = 1e-5                             # central differences in 64 bits: off by h^2 and by 1e-16 / h of a loss of about 30
+    for _ in range(4):
+        d, e, f = (rng.standard_normal(s) for s in ((rows, cols), cols, cols))
+        for moved, grad, direction in (((d, 0 * e, 0 * f), dx, d), ((0 * d, e, 0 * f), dg, e), ((0 * d, 0 * e, f), db, f)):
+            num = (loss(x + h * moved[0], gamma + h * moved[1], beta + h * moved[2]) - loss(x - h * moved[0], gamma - h * moved[1], beta - h * moved[2])) / (2 * h)
+            got = float((ref.as64(grad) * direction).sum())
+            assert abs(got - num) <= 1e-6 * np.sqrt(direction.size) * (1 + abs(num))
+
+
+def test_rows_of_a_norm_that_are_not_finite_stay_alone():
+    x, gamma, beta = norm_inputs(12, 300, 3)
+    x[4, 7], x[9, 0] = np.inf, np.nan
+    xd = tensor(x, F32)
+    y = torch.empty(12, 300, device="cuda", dtype=BF16)
+    omc.omc_layer_norm(xd, torch.from_numpy(gamma).cuda(), torch.from_numpy(beta).cuda(), 1e-5, y)
+    bad = torch.isnan(y.float()).all(1).cpu().numpy()
+    assert bad.tolist() == [i in (4, 9) for i in range(12)]
+    assert torch.isfinite(y[~torch.from_numpy(bad).cuda()]).all()
+
+
+def test_other_streams_and_repeats():
+    """On a stream of the caller's; the same bits every time."""
+    M, N, K = 700, 300, 520
+    x, dy = tensor(inputs(M, K, 1), BF16), tensor(inputs(M, N, 2), BF16)
+    wc, wsc, _ = random_mx4(N, K, 3)
+    vc, vsc, _ = random_mx4(K, N, 4)
+    gamma = torch.ones(K, device="cuda")
+    dev = [to_dev(a) for a in (wc, wsc, vc, vsc)]
+    ws = workspace(max(omc.omc_mx4_linear_workspace_bytes(M, N, K), omc.omc_mx4_linear_backward_workspace_bytes(M, N, K), omc.omc_layer_norm_backward_workspace_bytes(M, K)))[1]
+
+    def once(stream):
+        y, dx, dw, db = torch.empty(M, N, device="cuda"), torch.empty(M, K, device="cuda"), torch.empty(K, N, device="cuda"), torch.empty(N, device="cuda")
+        h, mean, rstd, dg, dbeta, dh = torch.empty_like(x), torch.empty(M, device="cuda"), torch.empty(M, device="cuda"), torch.empty(K, device="cuda"), torch.empty(K, device="cuda"), torch.empty_like(x)
+        torch.cuda.synchronize()
+        omc.omc_layer_norm(x, gamma, None, 1e-5, h, mean, rstd, stream=stream)
+        omc.omc_mx4_linear(h, dev[0], dev[1], None, y, ws, stream=stream)
+        omc.omc_mx4_linear_backward(dy, h, dev[2], dev[3], dx, dw, db, ws, stream=stream)
+        omc.omc_layer_norm_backward(dx, x, gamma, mean, rstd, dh, dg, dbeta, ws, stream=stream)
+        torch.cuda.synchronize()
+        return [t.clone() for t in (y, dx, dw, db, h, mean, rstd, dg, dbeta, dh)]
+    first = once(None)
+    for stream in (torch.cuda.Stream(), None):
+        for a, b in zip(first, once(stream)):
+            assert torch.equal(a, b)
+
+
+def test_replayed_graph():
+    M, N, K = 200, 256, 384
+    x, out = torch.empty(M, K, device="cuda", dtype=BF16), torch.empty(M, N, device="cuda")
+    h, mean, rstd = torch.empty_like(x), torch.empty(M, device="cuda"), torch.empty(M, device="cuda")
+    dx, dw, db = torch.empty(M, K, device="cuda", dtype=BF16), torch.empty(K, N, device="cuda"), torch.empty(N, device="cuda")
+    dh, dg, dbeta = torch.empty_like(x), torch.empty(K, device="cuda"), torch.empty(K, device="cuda")
+    dy = tensor(inputs(M, N, 9), BF16)
+    wc, wsc = [to_dev(a) for a in random_mx4(N, K, 3)[:2]]
+    vc, vsc = [to_dev(a) for a in random_mx4(K, N, 4)[:2]]
+    ws = workspace(max(omc.omc_mx4_linear_workspace_bytes(M, N, K), omc.omc_mx4_linear_backward_workspace_bytes(M, N, K), omc.omc_layer_norm_backward_workspace_bytes(M, K)))[1]
+    results = (out, h, mean, rstd, dx, dw, db, dh, dg, dbeta)
+
+    def step():
+        omc.omc_layer_norm(x, None, None, 1e-5, h, mean, rstd)
+        omc.omc_mx4_linear(h, wc, wsc, None, out, ws)
+        omc.omc_mx4_linear_backward(dy, h, vc, vsc, dx, dw, db, ws)
+        omc.omc_layer_norm_backward(dx, x, None, mean, rstd, dh, dg, dbeta, ws)
+    x.copy_(tensor(inputs(M, K, 0), BF16))
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for seed in range(1, 4):
+        x.copy_(tensor(inputs(M, K, seed), BF16))
+        step()
+        want = [t.clone() for t in results]
+        for t in results:
+            t.fill_(7.0)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(want, results):
+            assert torch.equal(a, b)
+
+
+def test_offsets_past_32_bits():
+    """A weight matrix whose codes pass 4 GiB, of an input that passes 2^32 elements; a norm of as many."""
+    rows, cols = (1 << 19) + 33, 16400
+    x = torch.empty(rows, cols, device="cuda", dtype=BF16)
+    x.zero_()
+    tail = tensor(inputs(70, cols, 1), BF16)
+    x[-70:] = tail
+    codes = torch.empty(omc.omc_mx4_code_bytes(rows, cols), dtype=torch.uint8, device="cuda")
+    scales = torch.empty(omc.omc_mx4_scale_bytes(rows, cols), dtype=torch.uint8, device="cuda")
+    assert codes.numel() > 1 << 32 and x.numel() > 1 << 32
+    omc.omc_mx4_quantize(x, codes, scales)
+    want_c, want_s, w = ref.quantize(ref.as64(tail))
+    assert np.array_equal(codes.view(rows, -1)[-70:].cpu().numpy(), want_c)
+    assert np.array_equal(scales.view(rows, -1)[-70:].cpu().numpy(), want_s)
+    mean, rstd = torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+    y = torch.empty_like(x)
+    omc.omc_layer_norm(x, None, None, 1e-5, y, mean, rstd)
+    assert np.allclose(ref.as64(y[-70:]), ref.layer_norm(ref.as64(tail), 1.0, 0.0, 1e-5)[0], rtol=2.0 ** -8, atol=1e-4)
+    del y
+    for M in (3, 70):
+        f = tensor(inputs(M, cols, M), BF16)
+        y = torch.full((M, rows), 7.0, device="cuda")
+        omc.omc_mx4_linear(f, codes, scales, None, y, workspace(omc.omc_mx4_linear_workspace_bytes(M, rows, cols))[1])
+        a = ref.quantize(ref.as64(f))[2]
+        check(y[:, -70:], a @ w.T, ref.product_bound(a, w, cols), F32)
+        assert (y[:, :-70] == 0).all()
