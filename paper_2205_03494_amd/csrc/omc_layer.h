@@ -15,6 +15,19 @@ constexpr uint32_t mx4_padded(uint32_t cols) { return (cols + 127) / 128 * 128; 
 constexpr uint64_t mx4_code_bytes(uint64_t rows, uint32_t cols) { return rows * (mx4_padded(cols) / 2); }
 constexpr uint64_t mx4_scale_bytes(uint64_t rows, uint32_t cols) { return rows * (mx4_padded(cols) / 32); }
 
+// The scales as the tiles of launch_mx4_gemm read them: for every 256 values of a row, one after the other, 8 bytes of every row (rows padded to 256, which need not be
+// written), those of its blocks 0, 1, 4, 5, 2, 3, 6, 7, and 0 for the second 128 values if the row has none.
+constexpr uint32_t mx4_image_byte(uint32_t block) { return 4 * (block / 2 % 2) + 2 * (block / 4) + block % 2; }
+constexpr uint64_t mx4_image_pitch(uint32_t rows) { return (static_cast<uint64_t>(rows) + 255) / 256 * 2048; }
+constexpr uint64_t mx4_image_bytes(uint32_t rows, uint32_t cols) { return (static_cast<uint64_t>(cols) + 255) / 256 * mx4_image_pitch(rows); }
+
+// Scales in the order of omc.h, to be brought into that of the tiles.
+struct Mx4Reorder {
+    const uint8_t *scales;
+    uint8_t *image;                // null: nothing to do
+    uint32_t rows, cols;
+};
+
 struct QuantArgs {
     const void *x;
     uint64_t ldx;
@@ -24,7 +37,10 @@ struct QuantArgs {
     void *values;                  // may be null
     uint64_t ldv;
     float *colsum;                 // partial sums of the columns, one row of them for every 128 rows of x; may be null
+    bool images;                   // scales and scales_t in the tiles' order
+    Mx4Reorder also;               // another matrix' scales, by the same launch
 };
+int launch_mx4_reorder(const Mx4Reorder &a, const Mx4Reorder &b, void *stream);
 int launch_mx4_quantize(const QuantArgs &qa, bool bf16, void *stream);
 
 struct Mx4GemmArgs {
@@ -35,10 +51,10 @@ struct Mx4GemmArgs {
     uint32_t M, N, K;
     float *parts;                  // partial results of a split contraction
 };
-// c = a b^T + bias, c in bf16 or fp32.
+// c = a b^T + bias, c in bf16 or fp32; the operands' scales in the tiles' order.
 size_t mx4_gemm_workspace(uint32_t M, uint32_t N, uint32_t K);   // bytes of parts
 int launch_mx4_gemm(const Mx4GemmArgs &ga, bool bf16, void *stream);
-// The same for few rows of a.  Where mx4_few_rounds, these may come as they are (`rows`), and are rounded on the way.
+// The same for few rows of a, with scales in the order of omc.h.  Where mx4_few_rounds, these may come as they are (`rows`), and are rounded on the way.
 constexpr uint32_t kMx4FewRows = 64;
 struct Mx4Rows {
     const void *x;

@@ -24,45 +24,68 @@ struct Parts {
         used += (bytes + 255) / 256 * 256;
         return p;
     }
-    Mx4 take_mx4(uint32_t rows, uint32_t cols) {
-        uint8_t *codes = take(mx4_code_bytes(rows, cols));
-        return Mx4{codes, take(mx4_scale_bytes(rows, cols))};
-    }
 };
-static uint8_t *writable(const uint8_t *p) { return const_cast<uint8_t *>(p); }
+static const uint8_t *bytes(const void *p) { return static_cast<const uint8_t *>(p); }
 
-static uint64_t product_workspace(uint32_t M, uint32_t N, uint32_t K) { return M <= kMx4FewRows ? 0 : mx4_gemm_workspace(M, N, K); }
+// A product's way: few rows of the first operand, or tiles, whose scales are reordered first.
+static bool few(uint32_t M) { return M <= kMx4FewRows; }
+static uint64_t scale_bytes(uint32_t M, uint32_t rows, uint32_t K) { return few(M) ? mx4_scale_bytes(rows, K) : mx4_image_bytes(rows, K); }
+static uint64_t parts_bytes(uint32_t M, uint32_t N, uint32_t K) { return few(M) ? 0 : mx4_gemm_workspace(M, N, K); }
 static int launch_product(const Mx4GemmArgs &ga, bool bf16, void *stream) {
-    return ga.M <= kMx4FewRows ? launch_mx4_few(ga, nullptr, bf16, stream) : launch_mx4_gemm(ga, bf16, stream);
+    return few(ga.M) ? launch_mx4_few(ga, nullptr, bf16, stream) : launch_mx4_gemm(ga, bf16, stream);
+}
+
+struct GemmLayout {
+    uint8_t *a_image, *b_image;
+    float *parts;
+    uint64_t bytes;
+};
+static GemmLayout gemm_layout(uint8_t *ws, uint32_t M, uint32_t N, uint32_t K) {
+    GemmLayout l{};
+    if (few(M)) return l;
+    Parts p{ws};
+    l.a_image = p.take(mx4_image_bytes(M, K));
+    l.b_image = p.take(mx4_image_bytes(N, K));
+    l.parts = reinterpret_cast<float *>(p.take(parts_bytes(M, N, K)));
+    l.bytes = p.used;
+    return l;
 }
 
 struct LinearLayout {
-    Mx4 x;
+    uint8_t *codes, *scales, *w_image;
     float *parts;
     uint64_t bytes;
 };
 static LinearLayout linear_layout(uint8_t *ws, uint32_t M, uint32_t N, uint32_t K) {
     LinearLayout l{};
+    if (few(M) && mx4_few_rounds(M, N, K)) return l;
     Parts p{ws};
-    if (!mx4_few_rounds(M, N, K)) l.x = p.take_mx4(M, K);
-    l.parts = reinterpret_cast<float *>(p.take(product_workspace(M, N, K)));
+    l.codes = p.take(mx4_code_bytes(M, K));
+    l.scales = p.take(scale_bytes(M, M, K));
+    if (!few(M)) l.w_image = p.take(mx4_image_bytes(N, K));
+    l.parts = reinterpret_cast<float *>(p.take(parts_bytes(M, N, K)));
     l.bytes = p.used;
     return l;
 }
 
+// The two products go different ways if M or K is small: dX's first operand has M rows, dW's K.
 struct BackwardLayout {
-    Mx4 dy, dy_t, x_t;
+    uint8_t *dy, *dy_scales, *dy_t, *dy_t_scales, *x_t, *x_t_scales, *w_image;
     float *sums, *parts;
     uint64_t bytes;
 };
 static BackwardLayout backward_layout(uint8_t *ws, uint32_t M, uint32_t N, uint32_t K) {
     BackwardLayout l{};
     Parts p{ws};
-    l.dy = p.take_mx4(M, N);
-    l.dy_t = p.take_mx4(N, M);
-    l.x_t = p.take_mx4(K, M);
+    l.dy = p.take(mx4_code_bytes(M, N));
+    l.dy_scales = p.take(scale_bytes(M, M, N));
+    l.dy_t = p.take(mx4_code_bytes(N, M));
+    l.dy_t_scales = p.take(scale_bytes(K, N, M));
+    l.x_t = p.take(mx4_code_bytes(K, M));
+    l.x_t_scales = p.take(scale_bytes(K, K, M));
+    if (!few(M)) l.w_image = p.take(mx4_image_bytes(K, N));
     l.sums = reinterpret_cast<float *>(p.take(4ull * ((M + 127) / 128) * N));
-    const uint64_t dx = product_workspace(M, K, N), dw = product_workspace(K, N, M);
+    const uint64_t dx = parts_bytes(M, K, N), dw = parts_bytes(K, N, M);
     l.parts = reinterpret_cast<float *>(p.take(dx > dw ? dx : dw));
     l.bytes = p.used;
     return l;
@@ -84,12 +107,12 @@ omc_status omc_mx4_quantize(const void *x, omc_type type, uint32_t rows, uint32_
     if (!dims_ok(rows, cols) || ldx < cols || (values && ldv < cols)) return OMC_ERR_SIZE;
     if (!element_aligned(x, type) || !element_aligned(values, type) || !mx4_aligned(codes, scales) || !mx4_aligned(codes_t, scales_t)) return OMC_ERR_ALIGN;
     const QuantArgs qa{x, ldx, rows, cols, static_cast<uint8_t *>(codes), static_cast<uint8_t *>(scales), static_cast<uint8_t *>(codes_t),
-                       static_cast<uint8_t *>(scales_t), values, ldv, nullptr};
+                       static_cast<uint8_t *>(scales_t), values, ldv, nullptr, false, {}};
     return from_hip(launch_mx4_quantize(qa, type == OMC_BF16, stream));
 }
 
 size_t omc_mx4_gemm_workspace_bytes(uint32_t M, uint32_t N, uint32_t K) {
-    return dims_ok(M, N) && dims_ok(M, K) && dims_ok(N, K) ? product_workspace(M, N, K) : 0;
+    return dims_ok(M, N) && dims_ok(M, K) && dims_ok(N, K) ? gemm_layout(nullptr, M, N, K).bytes : 0;
 }
 
 omc_status omc_mx4_gemm(const void *a_codes, const void *a_scales, const void *b_codes, const void *b_scales, const float *bias, void *C,
@@ -98,13 +121,17 @@ omc_status omc_mx4_gemm(const void *a_codes, const void *a_scales, const void *b
     if (!type_ok(c_type)) return OMC_ERR_FORMAT;
     if (!dims_ok(M, N) || !dims_ok(M, K) || !dims_ok(N, K) || ldc < N) return OMC_ERR_SIZE;
     if (!mx4_aligned(a_codes, a_scales) || !mx4_aligned(b_codes, b_scales) || !aligned(bias, 4) || !element_aligned(C, c_type)) return OMC_ERR_ALIGN;
-    const uint64_t need = product_workspace(M, N, K);
-    if (need > 0 && (!ws || ws_bytes < need)) return OMC_ERR_WORKSPACE;
-    if (need > 0 && !aligned(ws, 16)) return OMC_ERR_ALIGN;
-    const Mx4GemmArgs ga{{static_cast<const uint8_t *>(a_codes), static_cast<const uint8_t *>(a_scales)},
-                         {static_cast<const uint8_t *>(b_codes), static_cast<const uint8_t *>(b_scales)},
-                         bias, C, ldc, M, N, K, static_cast<float *>(ws)};
-    return from_hip(launch_product(ga, c_type == OMC_BF16, stream));
+    const GemmLayout l = gemm_layout(static_cast<uint8_t *>(ws), M, N, K);
+    if (l.bytes > 0 && (!ws || ws_bytes < l.bytes)) return OMC_ERR_WORKSPACE;
+    if (l.bytes > 0 && !aligned(ws, 16)) return OMC_ERR_ALIGN;
+    Mx4GemmArgs ga{{bytes(a_codes), bytes(a_scales)}, {bytes(b_codes), bytes(b_scales)}, bias, C, ldc, M, N, K, l.parts};
+    int rc = 0;
+    if (!few(M)) {
+        rc = launch_mx4_reorder({ga.a.scales, l.a_image, M, K}, {ga.b.scales, l.b_image, N, K}, stream);
+        ga.a.scales = l.a_image;
+        ga.b.scales = l.b_image;
+    }
+    return from_hip(rc != 0 ? rc : launch_product(ga, c_type == OMC_BF16, stream));
 }
 
 size_t omc_mx4_linear_workspace_bytes(uint32_t M, uint32_t N, uint32_t K) {
@@ -121,12 +148,13 @@ omc_status omc_mx4_linear(const void *X, omc_type x_type, uint64_t ldx, const vo
     if (l.bytes > 0 && (!ws || ws_bytes < l.bytes)) return OMC_ERR_WORKSPACE;
     if (l.bytes > 0 && !aligned(ws, 16)) return OMC_ERR_ALIGN;
     const bool x_bf16 = x_type == OMC_BF16, y_bf16 = y_type == OMC_BF16;
-    const Mx4GemmArgs ga{l.x, {static_cast<const uint8_t *>(w_codes), static_cast<const uint8_t *>(w_scales)}, bias, Y, ldy, M, N, K, l.parts};
-    if (mx4_few_rounds(M, N, K)) {
+    const Mx4 w{bytes(w_codes), few(M) ? bytes(w_scales) : l.w_image};
+    const Mx4GemmArgs ga{{l.codes, l.scales}, w, bias, Y, ldy, M, N, K, l.parts};
+    if (!l.codes) {
         const Mx4Rows rows{X, ldx, x_bf16};
         return from_hip(launch_mx4_few(ga, &rows, y_bf16, stream));
     }
-    const QuantArgs qa{X, ldx, M, K, writable(l.x.codes), writable(l.x.scales), nullptr, nullptr, nullptr, 0, nullptr};
+    const QuantArgs qa{X, ldx, M, K, l.codes, l.scales, nullptr, nullptr, nullptr, 0, nullptr, !few(M), {bytes(w_scales), l.w_image, N, K}};
     const int rc = launch_mx4_quantize(qa, x_bf16, stream);
     return from_hip(rc != 0 ? rc : launch_product(ga, y_bf16, stream));
 }
@@ -149,25 +177,33 @@ omc_status omc_mx4_linear_backward(const void *dY, uint64_t lddy, const void *X,
     if (!aligned(ws, 16)) return OMC_ERR_ALIGN;
     const bool bf16 = type == OMC_BF16;
 
-    QuantArgs qa{dY, lddy, M, N, nullptr, nullptr, nullptr, nullptr, nullptr, 0, dbias ? l.sums : nullptr};
+    // dY's rounding in one pass, unless its two products want their scales in different orders
+    const bool dx_tiles = !few(M), dw_tiles = !few(K);
+    QuantArgs qa{dY, lddy, M, N, nullptr, nullptr, nullptr, nullptr, nullptr, 0, dbias ? l.sums : nullptr, dx_tiles, {}};
     if (dX) {
-        qa.codes = writable(l.dy.codes);
-        qa.scales = writable(l.dy.scales);
+        qa.codes = l.dy;
+        qa.scales = l.dy_scales;
+        if (dx_tiles) qa.also = Mx4Reorder{bytes(w_scales), l.w_image, K, N};
     }
-    if (dW) {
-        qa.codes_t = writable(l.dy_t.codes);
-        qa.scales_t = writable(l.dy_t.scales);
+    int rc = 0;
+    if (dW && (!dX || dx_tiles == dw_tiles)) {
+        qa.codes_t = l.dy_t;
+        qa.scales_t = l.dy_t_scales;
+        qa.images = dw_tiles;
+    } else if (dW) {
+        const QuantArgs ta{dY, lddy, M, N, nullptr, nullptr, l.dy_t, l.dy_t_scales, nullptr, 0, nullptr, dw_tiles, {}};
+        rc = launch_mx4_quantize(ta, bf16, stream);
     }
-    int rc = launch_mx4_quantize(qa, bf16, stream);
+    if (rc == 0) rc = launch_mx4_quantize(qa, bf16, stream);
     if (rc == 0 && dbias) rc = launch_column_sums(l.sums, (M + 127) / 128, N, N, dbias, nullptr, stream);
     if (rc == 0 && dX) {
-        const Mx4GemmArgs ga{l.dy, {static_cast<const uint8_t *>(w_codes), static_cast<const uint8_t *>(w_scales)}, nullptr, dX, lddx, M, K, N, l.parts};
+        const Mx4GemmArgs ga{{l.dy, l.dy_scales}, {bytes(w_codes), dx_tiles ? l.w_image : bytes(w_scales)}, nullptr, dX, lddx, M, K, N, l.parts};
         rc = launch_product(ga, dx_type == OMC_BF16, stream);
     }
     if (rc == 0 && dW) {
-        const QuantArgs xa{X, ldx, M, K, nullptr, nullptr, writable(l.x_t.codes), writable(l.x_t.scales), nullptr, 0, nullptr};
+        const QuantArgs xa{X, ldx, M, K, nullptr, nullptr, l.x_t, l.x_t_scales, nullptr, 0, nullptr, dw_tiles, {}};
         rc = launch_mx4_quantize(xa, bf16, stream);
-        const Mx4GemmArgs ga{l.x_t, l.dy_t, nullptr, dW, N, K, N, M, l.parts};
+        const Mx4GemmArgs ga{{l.x_t, l.x_t_scales}, {l.dy_t, l.dy_t_scales}, nullptr, dW, N, K, N, M, l.parts};
         if (rc == 0) rc = launch_product(ga, false, stream);
     }
     return from_hip(rc);

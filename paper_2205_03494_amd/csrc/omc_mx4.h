@@ -14,6 +14,7 @@ namespace omc {
 
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x8 __attribute__((ext_vector_type(8)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
@@ -109,11 +110,17 @@ __device__ __forceinline__ i32x8 mx4_operand(i32x4 x) { return __builtin_shuffle
 
 // acc += a b^T over 128 values: lane l holds of either operand row l % 16, block l / 16, its scale in byte BYTE_A or BYTE_B of a register.  The result's value v of
 // lane l is row 4 (l / 16) + v of a, row l % 16 of b.
+constexpr int kE2M1 = 4;                       // the operands' type, as the instructions name it
 template <int BYTE_A, int BYTE_B>
 __device__ __forceinline__ f32x4 mx4_multiply(i32x4 a, uint32_t scale_a, i32x4 b, uint32_t scale_b, f32x4 acc) {
-    constexpr int kE2M1 = 4;
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(mx4_operand(a), mx4_operand(b), acc, kE2M1, kE2M1, BYTE_A, static_cast<int>(scale_a), BYTE_B,
                                                             static_cast<int>(scale_b));
+}
+// The same over 64 values and 32 x 32 results: row l % 32, block l / 32; value v is row 8 (v / 4) + 4 (l / 32) + v % 4 of a, row l % 32 of b.
+template <int BYTE>
+__device__ __forceinline__ f32x16 mx4_multiply_32(i32x4 a, uint32_t scale_a, i32x4 b, uint32_t scale_b, f32x16 acc) {
+    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(mx4_operand(a), mx4_operand(b), acc, kE2M1, kE2M1, BYTE, static_cast<int>(scale_a), BYTE,
+                                                           static_cast<int>(scale_b));
 }
 
 // COUNT neighbours of a result's row, in fp32 or bf16: `left` of them lie inside.

@@ -1,175 +1,324 @@
-// omc_mx4_gemm: C[M x N] = A[M x K] B[N x K]^T + bias, both operands in MX4, on the scaled matrix instructions (16 x 16 results over 128 values).
+// omc_mx4_gemm: C[M x N] = A[M x K] B[N x K]^T + bias, both operands in MX4, on the scaled matrix instructions (32 x 32 results over 64 values).
 //
-// Codes and scales go from global memory straight into a ring of S LDS stages of 256 values of K: a row's stage is 128 bytes of codes, eight pieces of 16 bytes that are
-// a block each, and 8 scale bytes.  In step s of a stage's two, lane l multiplies block 2 (l / 16) + s of its row: the order of K is free as long as both operands agree, and this
-// one puts the scales of a lane's two steps next to each other.  The last stage may be half one (an odd number of 128s): its lanes bring the
-// first half twice instead of reading past the row, and one step multiplies the blocks l / 16.
+// Codes and scales go from global memory straight into a ring of S LDS stages of 256 values of K: a row's stage is 128 bytes of codes, eight pieces of 16 bytes that are a block each, and 8 scale
+// bytes.  (Rows of 64 bytes, stages of 128 values, would make a deeper ring, but the load path moves a cache line in two clocks, whole or half: 54 bytes a clock and compute unit with rows of
+// 128 bytes, 27 with rows of 64.)  In step s of a stage's four, lane l multiplies block 2 (l / 32) + s % 2 + 4 (s / 2) of its row.  Which blocks meet in a step is
+// free as long as both operands agree, and the scales are reordered before (mx4_image_pitch), so that a lane's four are a dword and a load of them is as dense as one of the codes:
+// read from rows of K / 32 bytes, 8 bytes a row, they take as many cache lines as the codes (16384 x 8192 x 8192: 600 us with such loads, 490 without any scales).  Of an odd number of 128s the last
+// stage's second half is its first one again, with scales of 2^-127 on both sides: what it adds is below 2^-240.
 //
-// Pieces are XOR-swizzled on their way in, so that the 16 that one read takes at a time lie on different banks.  The B operand comes first in the instruction, and row i of B's tile t in a
-// group of four is column 16 (i / 4) + 4 t + i % 4 of the group's 64: a lane then holds 16 neighbours of a row of C, and four lanes 64.
+// Pieces are XOR-swizzled on their way in, so that the 16 that one read takes at a time lie on different ones of the 64 banks.  The B operand comes first in the instruction, and its
+// tiles' row i is column 16 (i / 4 % 2) + 4 (i / 8) + i % 4: a lane then holds 16 neighbours of a row of C.
+//
+// The fragments of a step are read while the step before is multiplied; a stage's last step is multiplied behind the barrier of the next one, under that one's first reads and loads.  A
+// workgroup goes on to its next tile without a break: the loads run ahead of the products by S - 1 stages, whosever they are, and a tile's stores pass under the next one's products.
+#include <type_traits>
+
 #include "omc_mma.h"
 #include "omc_mx4.h"
 
 namespace omc {
 
-// One wave copies 64 dwords from global memory into 256 bytes of LDS at `dst`, lane l's to dst + 4 l.  (See load_to_lds.)
-__device__ __forceinline__ void load_dwords_to_lds(const uint8_t *base, uint32_t off, uint32_t dst) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(dst), "v"(off), "s"(base) : "memory", "m0");
+// Direct loads into LDS (see load_to_lds): lane l's 16 bytes to `to` + TO + 16 l, in the lanes that `lanes` has; all lanes are on before and after.
+template <uint32_t TO>
+__device__ __forceinline__ void load_pieces(const uint8_t *base, uint32_t off, uint32_t to, uint64_t lanes) {
+    asm volatile("s_add_u32 m0, %0, %3\n\ts_mov_b64 exec, %4\n\tglobal_load_lds_dwordx4 %1, %2\n\ts_mov_b64 exec, -1" ::"s"(to), "v"(off), "s"(base), "n"(TO), "s"(lanes)
+                 : "memory", "m0", "scc");
 }
+template <uint32_t TO>
+__device__ __forceinline__ void load_pieces(const uint8_t *lanes_own, uint32_t to, uint64_t lanes) {
+    asm volatile("s_add_u32 m0, %0, %2\n\ts_mov_b64 exec, %3\n\tglobal_load_lds_dwordx4 %1, off\n\ts_mov_b64 exec, -1" ::"s"(to), "v"(lanes_own), "n"(TO), "s"(lanes)
+                 : "memory", "m0", "scc");
+}
+
+// Between a wave's writes to LDS and reads by its other lanes, and back.  The hardware takes a wave's LDS accesses in order; the compiler must not carry a value over.
+__device__ __forceinline__ void lanes_exchange() { asm volatile("" ::: "memory"); }
+
+// The same address in all lanes, in scalar registers whatever the compiler thinks of its origin.
+__device__ __forceinline__ const uint8_t *in_scalars(const uint8_t *p) {
+    const uint64_t v = reinterpret_cast<uintptr_t>(p);
+    const uint32_t lo = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(v)), hi = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(v >> 32));
+    return reinterpret_cast<const uint8_t *>(static_cast<uint64_t>(hi) << 32 | lo);
+}
+
+// Keeps a product between the reads and loads that it is written between: without it the compiler gathers the products behind all of them.  (With one wave a SIMD the sums
+// are in the accumulation registers.)
+template <bool ACCUMULATION>
+__device__ __forceinline__ void stays_here(f32x16 &x) {
+    if constexpr (ACCUMULATION) asm volatile("" : "+a"(x));
+    else asm volatile("" : "+v"(x));
+}
+
+// Tile x of a grid of tiles: as tile_of_block deals them to the workgroups, x for the workgroup's number.
+__device__ __forceinline__ void tile_of(uint32_t x, uint32_t group_rows, uint32_t tiles_m, uint32_t tiles_n, uint32_t &tm, uint32_t &tn) {
+    const uint32_t total = tiles_m * tiles_n, q = total / 8, r = total % 8, die = x % 8, id = die * q + min(die, r) + x / 8;
+    const uint32_t rows = min(tiles_m, group_rows), group = id / (rows * tiles_n), first = group * rows, height = min(tiles_m - first, rows), in = id - group * rows * tiles_n;
+    tm = first + in % height;
+    tn = in / height;
+}
+
+constexpr uint32_t kCorner = 2560;             // LDS of a wave for its results on their way out
 
 struct Mx4TileArgs {
     Mx4GemmArgs g;
-    uint32_t tiles_m, tiles_n;
-    uint32_t stages_per_split;
+    uint32_t tiles_m, tiles_n, splits, stages_per_split;
 };
 
-// WM x WN waves of TM x (4 TG) matrix tiles.  SPLIT: the contraction is cut into gridDim.y parts, whose results go to g.parts in fp32.
-template <int WM, int WN, int TM, int TG, int S, int OCC, typename T, bool SPLIT>
+// WM x WN waves of TM x TN matrix tiles, OCC waves per SIMD.  SPLIT: the contraction is cut into parts, whose results go to g.parts in fp32.
+template <int WM, int WN, int TM, int TN, int S, int OCC, typename T, bool SPLIT>
 __global__ __attribute__((amdgpu_flat_work_group_size(64 * WM * WN, 64 * WM * WN))) __attribute__((amdgpu_waves_per_eu(OCC, OCC)))
 void mx4_gemm_kernel(Mx4TileArgs ta) {
-    constexpr int NW = WM * WN, BM = 16 * TM * WM, BN = 64 * TG * WN, TN = 4 * TG;
-    constexpr int kALoads = BM / 8 / NW, kBLoads = BN / 8 / NW, kScaleUnits = (BM + BN) / 32, kSLoads = (kScaleUnits + NW - 1) / NW;
-    constexpr int kLoads = kALoads + kBLoads + kSLoads;
-    constexpr uint32_t kA = 0, kB = BM * 128, kSA = kB + BN * 128, kStage = kSA + (BM + BN) * 8;
-    static_assert(BM % (8 * NW) == 0 && BN % (8 * NW) == 0, "whole loads");
-    __shared__ __attribute__((aligned(1024))) uint8_t lds[S * kStage];
+    constexpr int NW = WM * WN, BM = 32 * TM * WM, BN = 32 * TN * WN;
+    constexpr int kALoads = BM / 8 / NW, kBLoads = BN / 8 / NW, kLoads = kALoads + kBLoads + 1;
+    constexpr uint32_t kB = BM * 128, kS = kB + BN * 128, kStage = kS + (BM + BN) * 8, kScaleLoads = (BM + BN) / 128, kCorners = S * kStage;
+    constexpr int kStores = TM * TN * (T::kBytes == 2 && !SPLIT ? 2 : 4);
+    static_assert(BM % (8 * NW) == 0 && BN % (8 * NW) == 0 && NW % 4 == 0 && kScaleLoads >= 1 && 256 % BM == 0 && 256 % BN == 0, "whole loads, one swizzle per wave");
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[kCorners + NW * kCorner];
     const Mx4GemmArgs &g = ta.g;
     const uint32_t lds0 = lds_offset(lds);
     const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave / WN, wn = wave % WN;
-    uint32_t m0, n0;
-    tile_of_block(BM == 256 ? 4 : 8, ta.tiles_m, ta.tiles_n, m0, n0);
-    m0 *= BM;
-    n0 *= BN;
-    const uint32_t k128 = (g.K + 127) / 128, all_stages = (k128 + 1) / 2;
-    const uint32_t first = SPLIT ? blockIdx.y * ta.stages_per_split : 0u;
-    const uint32_t stages = SPLIT ? min(ta.stages_per_split, all_stages - first) : all_stages;
-    const bool half_end = (k128 & 1u) != 0 && first + stages == all_stages;
-    const uint32_t row_bytes = k128 * 64, row_scales = k128 * 4;
+    const uint32_t k128 = (g.K + 127) / 128, all_stages = (k128 + 1) / 2, half_at = (k128 & 1u) != 0 ? k128 / 2 : ~0u;
+    const uint32_t row_bytes = k128 * 64, tiles = ta.tiles_m * ta.tiles_n, items = SPLIT ? tiles * ta.splits : tiles;
 
-    // ---- global -> LDS
-    const uint8_t *a_from = g.a.codes + static_cast<uint64_t>(m0) * row_bytes + first * 128;
-    const uint8_t *b_from = g.b.codes + static_cast<uint64_t>(n0) * row_bytes + first * 128;
-    const uint8_t *sa_from = g.a.scales + static_cast<uint64_t>(m0) * row_scales + first * 8;
-    const uint8_t *sb_from = g.b.scales + static_cast<uint64_t>(n0) * row_scales + first * 8;
-    const uint32_t last_m = g.M - 1 - m0, last_n = g.N - 1 - n0;   // rows past the end: the last one again
-    uint32_t a_off[kALoads], b_off[kBLoads], s_off[kSLoads];
-    uint32_t upper = 0;                        // bit i: this lane's piece of load i lies in the second half of a stage
+    // Tile and part of a work item.  Workgroups go to the 8 dies in turn (the grid is a multiple of 8, or there is no second item).
+    struct Place {
+        uint32_t m0, n0, part, first, stages;
+    };
+    auto locate = [&](uint32_t item) {
+        Place p;                               // (divisions go through vector registers)
+        p.part = SPLIT ? __builtin_amdgcn_readfirstlane(item / tiles) : 0u;
+        tile_of(item - p.part * tiles, BM == 256 ? 4 : 8, ta.tiles_m, ta.tiles_n, p.m0, p.n0);
+        p.m0 = __builtin_amdgcn_readfirstlane(p.m0) * BM;
+        p.n0 = __builtin_amdgcn_readfirstlane(p.n0) * BN;
+        p.first = SPLIT ? p.part * ta.stages_per_split : 0u;
+        p.stages = SPLIT ? min(ta.stages_per_split, all_stages - p.first) : all_stages;
+        return p;
+    };
+
+    // ---- global -> LDS: load i of a wave is the rows 8 (wave + NW i) .. + 8 of an operand, lane l's piece l % 8 of row l / 8 (before the swizzle).  Rows past the end: the last one again.
+    const uint8_t *a_from, *b_from, *s_from;
+    uint32_t off[kALoads + kBLoads];
+    const uint32_t a_piece = 16 * ((lane & 7u) ^ ((lane >> 4) + 4 * (wave & 1u)));                  // row / 2 % 8
+    const uint32_t b_piece = 16 * ((lane & 7u) ^ ((lane >> 4) + 4 * ((wave >> 1) & 1u)));           // row / 2 % 4 + 4 (row / 16 % 2)
+    const uint32_t s_unit = wave % kScaleLoads, s_row = 2 * (64 * s_unit + lane);                   // two rows' scales a lane (some waves bring the same)
+    const uint64_t s_pitch = mx4_image_pitch(s_row < BM ? g.M : g.N);
+    uint32_t ask_item = blockIdx.x, ask_stage, ask_end;
+    uint64_t lanes = ~0ull;                    // that load: none once everything has been asked for
+    auto upper_is_lower = [&]() {              // before half a stage
 #pragma unroll
-    for (uint32_t i = 0; i < kALoads; ++i) {
-        const uint32_t row = 8 * (wave + NW * i) + (lane >> 3), piece = (lane & 7u) ^ ((row >> 1) & 7u);
-        a_off[i] = min(row, last_m) * row_bytes + piece * 16;
-        upper |= (piece >> 2) << i;
-    }
+        for (uint32_t i = 0; i < kALoads + kBLoads; ++i) off[i] -= i < kALoads ? a_piece & 64u : b_piece & 64u;
+    };
+    auto ask_for = [&](uint32_t item) {
+        const Place p = locate(item);
+        a_from = g.a.codes + static_cast<uint64_t>(p.m0) * row_bytes + p.first * 128;
+        b_from = g.b.codes + static_cast<uint64_t>(p.n0) * row_bytes + p.first * 128;
+        s_from = (s_row < BM ? g.a.scales + 8ull * (p.m0 + s_row) : g.b.scales + 8ull * (p.n0 + s_row - BM)) + p.first * s_pitch;
+        const uint32_t last_m = g.M - 1 - p.m0, last_n = g.N - 1 - p.n0;
 #pragma unroll
-    for (uint32_t i = 0; i < kBLoads; ++i) {
-        const uint32_t row = 8 * (wave + NW * i) + (lane >> 3), piece = (lane & 7u) ^ (((row >> 1) & 1u) + 2 * ((row >> 4) & 3u));
-        b_off[i] = min(row, last_n) * row_bytes + piece * 16;
-        upper |= (piece >> 2) << (kALoads + i);
-    }
+        for (uint32_t i = 0; i < kALoads; ++i) off[i] = min(8 * (wave + NW * i) + (lane >> 3), last_m) * row_bytes + a_piece;
 #pragma unroll
-    for (uint32_t i = 0; i < kSLoads; ++i) {
-        const uint32_t unit = min(wave + NW * i, static_cast<uint32_t>(kScaleUnits - 1)), row = 32 * unit + (lane >> 1);
-        s_off[i] = (row < BM ? min(row, last_m) : min(row - BM, last_n)) * row_scales + 4 * (lane & 1u);
-    }
-    auto load_stage = [&](uint32_t at, bool half) {
-#pragma unroll
-        for (uint32_t i = 0; i < kALoads; ++i)
-            load_to_lds(a_from, half ? a_off[i] - 64 * ((upper >> i) & 1u) : a_off[i], lds0 + at + kA + 1024 * (wave + NW * i));
-#pragma unroll
-        for (uint32_t i = 0; i < kBLoads; ++i)
-            load_to_lds(b_from, half ? b_off[i] - 64 * ((upper >> (kALoads + i)) & 1u) : b_off[i], lds0 + at + kB + 1024 * (wave + NW * i));
-#pragma unroll
-        for (uint32_t i = 0; i < kSLoads; ++i) {
-            const uint32_t unit = min(wave + NW * i, static_cast<uint32_t>(kScaleUnits - 1));
-            load_dwords_to_lds(unit < BM / 32 ? sa_from : sb_from, half ? s_off[i] - 4 * (lane & 1u) : s_off[i], lds0 + at + kSA + 256 * unit);
+        for (uint32_t i = 0; i < kBLoads; ++i) off[kALoads + i] = min(8 * (wave + NW * i) + (lane >> 3), last_n) * row_bytes + b_piece;
+        ask_stage = p.first;
+        ask_end = p.first + p.stages;
+        if (ask_stage == half_at) upper_is_lower();
+    };
+    const uint32_t codes_to = lds0 + 1024 * wave, scales_to = lds0 + kS + 1024 * s_unit;
+    struct From {
+        const uint8_t *a, *b;
+    };
+    auto from_now = [&]() { return From{in_scalars(a_from), in_scalars(b_from)}; };
+    auto load_one = [&](const From &from, uint32_t at, auto index) {
+        constexpr uint32_t I = decltype(index)::value;
+        if constexpr (I < kALoads) load_pieces<1024 * NW * I>(from.a, off[I], codes_to + at, lanes);
+        else if constexpr (I < kALoads + kBLoads) load_pieces<kB + 1024 * NW * (I - kALoads)>(from.b, off[I], codes_to + at, lanes);
+        else load_pieces<0>(s_from, scales_to + at, lanes);
+    };
+    auto load_stage = [&](uint32_t at) {
+        const From from = from_now();
+        for_constants<kLoads>([&](auto i) { load_one(from, at, i); });
+    };
+    auto next_stage = [&]() {
+        if (lanes == 0) return;
+        if (++ask_stage == ask_end) {
+            ask_item += gridDim.x;
+            if (ask_item < items) ask_for(ask_item);
+            else lanes = 0;
+        } else {
+            a_from += 128;
+            b_from += 128;
+            s_from += s_pitch;
+            if (ask_stage == half_at) upper_is_lower();
         }
-        a_from += 128;
-        b_from += 128;
-        sa_from += 8;
-        sb_from += 8;
     };
 
     // ---- LDS -> fragments
-    const uint32_t r = lane & 15u, q = lane >> 4;
-    const uint32_t a_row = 16 * TM * wm + r, b_row = 64 * TG * wn + 16 * (r >> 2) + (r & 3u);
-    const uint32_t a_swz = (r >> 1) & 7u, b_swz = ((r >> 1) & 1u) + 2 * (r >> 2);
-    f32x4 acc[TM][TN];
+    const uint32_t r = lane & 31u, h = lane >> 5;
+    const uint32_t a_row = 32 * TM * wm + r, b_col = 32 * TN * wn + 16 * ((r >> 2) & 1u) + 4 * (r >> 3) + (r & 3u);
+    const uint32_t a_swz = (r >> 1) & 7u, b_swz = ((b_col >> 1) & 3u) + 4 * ((b_col >> 4) & 1u);
+    f32x16 acc[TM][TN];
+    i32x4 a[2][TM], b[2][TN];
+    uint32_t sa[2][TM], sb[2][TN];             // of this stage, of the next
+    uint32_t a_at[4], b_at[4];
 #pragma unroll
-    for (int i = 0; i < TM; ++i)
-#pragma unroll
-        for (int j = 0; j < TN; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    auto code = [&](uint32_t at) { return *reinterpret_cast<const i32x4 *>(lds + at); };
-    auto multiply_stage = [&](uint32_t at) {
-        uint32_t sa[TM], sb[TN];
-#pragma unroll
-        for (uint32_t i = 0; i < TM; ++i) sa[i] = *reinterpret_cast<const uint16_t *>(lds + at + kSA + (a_row + 16 * i) * 8 + 2 * q);
-#pragma unroll
-        for (uint32_t j = 0; j < TN; ++j) sb[j] = *reinterpret_cast<const uint16_t *>(lds + at + kSA + (BM + b_row + 64 * (j / 4) + 4 * (j % 4)) * 8 + 2 * q);
-        for_constants<2>([&](auto step) {
-            constexpr int s = decltype(step)::value;
-            const uint32_t a_at = at + kA + a_row * 128 + (((2 * q + s) ^ a_swz) << 4), b_at = at + kB + b_row * 128 + (((2 * q + s) ^ b_swz) << 4);
-            i32x4 b[TN];
-#pragma unroll
-            for (uint32_t j = 0; j < TN; ++j) b[j] = code(b_at + 8192 * (j / 4) + 512 * (j % 4));
-#pragma unroll
-            for (uint32_t i = 0; i < TM; ++i) {
-                const i32x4 a = code(a_at + 2048 * i);
-#pragma unroll
-                for (uint32_t j = 0; j < TN; ++j) acc[i][j] = mx4_multiply<s, s>(b[j], sb[j], a, sa[i], acc[i][j]);
-            }
+    for (uint32_t s = 0; s < 4; ++s) {
+        const uint32_t piece = 2 * h + s % 2 + 4 * (s / 2);
+        a_at[s] = a_row * 128 + ((piece ^ a_swz) << 4);
+        b_at[s] = kB + b_col * 128 + ((piece ^ b_swz) << 4);
+    }
+    const uint32_t sa_at = kS + a_row * 8 + 4 * h, sb_at = kS + (BM + b_col) * 8 + 4 * h;
+    // read `index` of a step's: B's fragments first
+    auto read_one = [&](uint32_t at, auto step, auto index) {
+        constexpr uint32_t s = decltype(step)::value, I = decltype(index)::value;
+        if constexpr (I < TN) b[s & 1][I] = *reinterpret_cast<const i32x4 *>(lds + at + b_at[s] + 4096 * I);
+        else a[s & 1][I - TN] = *reinterpret_cast<const i32x4 *>(lds + at + a_at[s] + 4096 * (I - TN));
+    };
+    auto read_scale = [&](uint32_t at, auto index, auto set) {
+        constexpr uint32_t I = decltype(index)::value, s = decltype(set)::value;
+        if constexpr (I < TN) sb[s][I] = *reinterpret_cast<const uint32_t *>(lds + at + sb_at + 256 * I);
+        else sa[s][I - TN] = *reinterpret_cast<const uint32_t *>(lds + at + sa_at + 256 * (I - TN));
+    };
+    constexpr int kReads = TM + TN, kProducts = TM * TN;
+    uint32_t cur = 0, far = (S - 1) * kStage;  // the stage that is read, the one that is asked for
+    // The products of step s, and beside them the reads of the next step; after a stage's last one of the next stage, with its scales, and the loads of the stage that is asked for.
+    auto multiply = [&](auto step) {
+        constexpr uint32_t s = decltype(step)::value, N = (s + 1) % 4;
+        constexpr int kR = s == 3 ? 2 * kReads : kReads, kL = s == 3 ? kLoads : 0;
+        const From from = kL > 0 ? from_now() : From{};
+        for_constants<kProducts>([&](auto product) {
+            constexpr int P = decltype(product)::value, i = P / TN, j = P % TN;
+            constexpr int R0 = P * kR / kProducts, R1 = (P + 1) * kR / kProducts, L0 = P * kL / kProducts, L1 = (P + 1) * kL / kProducts;
+            for_constants<R1 - R0>([&](auto x) {
+                constexpr int I = R0 + decltype(x)::value;
+                if constexpr (I < kReads) read_one(cur, UintTag<N>{}, UintTag<I>{});
+                else read_scale(cur, UintTag<I - kReads>{}, UintTag<1>{});
+            });
+            for_constants<L1 - L0>([&](auto x) { load_one(from, far, UintTag<L0 + decltype(x)::value>{}); });
+            acc[i][j] = mx4_multiply_32<s>(b[s & 1][j], sb[0][j], a[s & 1][i], sa[0][i], acc[i][j]);
+            stays_here<OCC == 1>(acc[i][j]);
+            __builtin_amdgcn_sched_barrier(0);
         });
     };
-    auto multiply_half = [&](uint32_t at) {
-        const uint32_t a_at = at + kA + a_row * 128 + ((q ^ a_swz) << 4), b_at = at + kB + b_row * 128 + ((q ^ b_swz) << 4);
-        i32x4 b[TN];
-        uint32_t sb[TN];
-#pragma unroll
-        for (uint32_t j = 0; j < TN; ++j) {
-            b[j] = code(b_at + 8192 * (j / 4) + 512 * (j % 4));
-            sb[j] = lds[at + kSA + (BM + b_row + 64 * (j / 4) + 4 * (j % 4)) * 8 + q];
-        }
-#pragma unroll
-        for (uint32_t i = 0; i < TM; ++i) {
-            const i32x4 a = code(a_at + 2048 * i);
-            const uint32_t sa = lds[at + kSA + (a_row + 16 * i) * 8 + q];
-#pragma unroll
-            for (uint32_t j = 0; j < TN; ++j) acc[i][j] = mx4_multiply<0, 0>(b[j], sb[j], a, sa, acc[i][j]);
-        }
-    };
-
-    uint32_t cur = 0, far = (S - 1) * kStage;
-#pragma unroll
-    for (uint32_t i = 0; i < S - 1; ++i)
-        if (i < stages) load_stage(i * kStage, half_end && i + 1 == stages);
-    for (uint32_t j = 0; j < stages; ++j) {
-        wait_stage<S, kLoads>(j, stages);
-        if (j + S - 1 < stages) load_stage(far, half_end && j + S == stages);
-        if (half_end && j + 1 == stages) multiply_half(cur);
-        else multiply_stage(cur);
+    // Waits for the next stage: it is there when at most the loads of the S - 2 after it, and the stores behind loads of its own age, are on their way.  (At the end it is nothing that is
+    // waited for, read and asked for.  Loads without lanes are not relied on to count.)
+    uint32_t behind = 0;                       // so many stages yet that were asked for before the last stores
+    auto wait_for_next = [&]() {
+        constexpr int kLater = (S - 2) * kLoads;
+        if (lanes == 0) wait_loads_and_sync<0>();
+        else if (behind > 0) wait_loads_and_sync<(kLater + kStores < 63 ? kLater + kStores : 63)>();
+        else wait_loads_and_sync<kLater>();
+        behind -= behind > 0 ? 1 : 0;
         cur = cur == (S - 1) * kStage ? 0 : cur + kStage;
         far = far == (S - 1) * kStage ? 0 : far + kStage;
-    }
+    };
 
-    // ---- a lane's runs of 16 neighbours
-    float *parts = SPLIT ? g.parts + static_cast<uint64_t>(blockIdx.y) * g.M * g.N : nullptr;
+    ask_for(ask_item);
 #pragma unroll
-    for (uint32_t gr = 0; gr < TG; ++gr) {
-        const uint32_t n = n0 + 64 * (TG * wn + gr) + 16 * q;
-        if (n >= g.N) continue;
-        const uint32_t left = g.N - n;
-        float bias[16];
+    for (uint32_t i = 0; i < S - 1; ++i) {
+        load_stage(i * kStage);
+        next_stage();
+    }
+    if (lanes != 0) wait_loads_and_sync<(S - 2) * kLoads>();
+    else wait_loads_and_sync<0>();
+    load_stage(far);
+    next_stage();
+    for_constants<kReads>([&](auto i) {
+        read_one(0, UintTag<0>{}, i);
+        read_scale(0, i, UintTag<0>{});
+    });
+    for (uint32_t item = blockIdx.x; item < items; item += gridDim.x) {
+        const Place p = locate(item);
 #pragma unroll
-        for (uint32_t e = 0; e < 16; ++e) bias[e] = !SPLIT && g.bias ? g.bias[min(n + e, g.N - 1)] : 0.0f;
+        for (int i = 0; i < TM; ++i)
 #pragma unroll
-        for (uint32_t i = 0; i < TM; ++i) {
-            const uint32_t m = m0 + a_row + 16 * i;
-            if (m >= g.M) continue;
-            float v[16];
+            for (int j = 0; j < TN; ++j)
 #pragma unroll
-            for (uint32_t e = 0; e < 16; ++e) v[e] = acc[i][4 * gr + e / 4][e % 4] + bias[e];
-            if (SPLIT) store_run<F32, 16>(parts + static_cast<uint64_t>(m) * g.N + n, v, left);
-            else store_run<T, 16>(static_cast<typename T::type *>(g.c) + m * g.ldc + n, v, left);
+                for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.0f;
+        for (uint32_t left = p.stages; left > 0; --left) {
+            multiply(UintTag<0>{});
+            multiply(UintTag<1>{});
+            multiply(UintTag<2>{});
+            wait_for_next();
+            multiply(UintTag<3>{});
+            next_stage();
+#pragma unroll
+            for (int i = 0; i < TM; ++i) sa[0][i] = sa[1][i];
+#pragma unroll
+            for (int i = 0; i < TN; ++i) sb[0][i] = sb[1][i];
         }
+
+        // ---- through the wave's own corner of LDS, so that a row's 64 (bf16) or 128 bytes (fp32) of a tile are stored together
+        typedef typename std::conditional<SPLIT, F32, T>::type Out;
+        constexpr uint32_t kRun = 16 / Out::kBytes, kLanes = 32 / kRun, kRows = 64 / kLanes, kPitch = 32 * Out::kBytes + 16, kPass = Out::kBytes == 2 ? 32 : 16;
+        static_assert(kPass * kPitch <= kCorner, "fits");
+        uint8_t *corner = lds + kCorners + wave * kCorner;
+        typename Out::type *c;
+        uint64_t ldc;
+        if constexpr (SPLIT) {
+            c = g.parts + static_cast<uint64_t>(p.part) * g.M * g.N;
+            ldc = g.N;
+        } else {
+            c = static_cast<typename T::type *>(g.c);
+            ldc = g.ldc;
+        }
+        const uint32_t s_row = lane / kLanes, s_col = kRun * (lane % kLanes);
+        const bool stored = p.m0 + BM <= g.M && p.n0 + BN <= g.N;   // a whole tile
+#pragma unroll
+        for (uint32_t j = 0; j < TN; ++j) {
+            const uint32_t n_tile = p.n0 + 32 * (TN * wn + j), n = n_tile + s_col;
+            float bias[16];               // of the lane's 16 columns, by scalar loads, which wait for none of the loads on their way
+            const bool whole_bias = !SPLIT && g.bias && stored;
+            if (whole_bias) {
+                const __attribute__((address_space(4))) float *from = reinterpret_cast<const __attribute__((address_space(4))) float *>(reinterpret_cast<uintptr_t>(g.bias + n_tile));
+#pragma unroll
+                for (uint32_t e = 0; e < 16; ++e) bias[e] = h == 0 ? from[e] : from[16 + e];
+            } else {
+#pragma unroll
+                for (uint32_t e = 0; e < 16; ++e) bias[e] = 0.0f;
+                if (!SPLIT && g.bias) {
+#pragma unroll
+                    for (uint32_t e = 0; e < 16; ++e) bias[e] = g.bias[min(n_tile + 16 * h + e, g.N - 1)];
+                }
+            }
+#pragma unroll
+            for (uint32_t i = 0; i < TM; ++i)
+#pragma unroll
+                for (uint32_t pass = 0; pass < 32 / kPass; ++pass) {
+                    if (kPass == 32 || r / kPass == pass) {
+                        float v[16];
+#pragma unroll
+                        for (uint32_t e = 0; e < 16; ++e) v[e] = acc[i][j][e] + bias[e];
+                        uint8_t *to = corner + (r % kPass) * kPitch + 16 * h * Out::kBytes;
+                        if constexpr (Out::kBytes == 4) {
+#pragma unroll
+                            for (uint32_t e = 0; e < 4; ++e) *reinterpret_cast<f32x4 *>(to + 16 * e) = f32x4{v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]};
+                        } else {
+#pragma unroll
+                            for (uint32_t e = 0; e < 2; ++e)
+                                *reinterpret_cast<u32x4 *>(to + 16 * e) = u32x4{to_bf16_pair(v[8 * e], v[8 * e + 1]), to_bf16_pair(v[8 * e + 2], v[8 * e + 3]),
+                                                                                to_bf16_pair(v[8 * e + 4], v[8 * e + 5]), to_bf16_pair(v[8 * e + 6], v[8 * e + 7])};
+                        }
+                    }
+                    lanes_exchange();
+#pragma unroll
+                    for (uint32_t k = 0; k < kPass / kRows; ++k) {
+                        const u32x4 w = *reinterpret_cast<const u32x4 *>(corner + (kRows * k + s_row) * kPitch + 4 * (lane % kLanes) * 4);
+                        const uint32_t m = p.m0 + 32 * (TM * wm + i) + kPass * pass + kRows * k + s_row;
+                        typename Out::type *to = c + m * ldc + n;
+                        if (stored) {
+                            __builtin_memcpy(to, &w, 16);
+                        } else if (m < g.M) {
+#pragma unroll
+                            for (uint32_t e = 0; e < kRun; ++e)
+                                if (n + e < g.N) {
+                                    if constexpr (Out::kBytes == 4) to[e] = __uint_as_float(w[e]);
+                                    else to[e] = static_cast<uint16_t>(w[e / 2] >> (16 * (e & 1)));
+                                }
+                        }
+                    }
+                    lanes_exchange();
+                }
+        }
+        behind = stored ? S - 1 : 0;
     }
 }
 
@@ -206,9 +355,9 @@ struct Mx4Choice {
 };
 static Mx4Choice choose(uint32_t M, uint32_t N, uint32_t K) {
     const uint32_t stages = (K + 255) / 256;
-    const uint32_t sizes[3][2] = {{256, 256}, {128, 128}, {64, 64}};
-    Mx4Choice c{2, 64, 64, 1};
-    for (int i = 0; i < 3; ++i) {
+    const uint32_t sizes[5][2] = {{256, 256}, {256, 128}, {128, 128}, {128, 64}, {64, 64}};
+    Mx4Choice c{4, 64, 64, 1};
+    for (int i = 0; i < 5; ++i) {
         c = Mx4Choice{i, sizes[i][0], sizes[i][1], 1};
         if (static_cast<uint64_t>((M + c.bm - 1) / c.bm) * ((N + c.bn - 1) / c.bn) >= 256) return c;
     }
@@ -225,22 +374,29 @@ size_t mx4_gemm_workspace(uint32_t M, uint32_t N, uint32_t K) {
     return c.splits > 1 ? 4ull * c.splits * M * N : 0;
 }
 
-template <int WM, int WN, int TM, int TG, int S, int OCC, typename T>
-static void launch_tile(const Mx4TileArgs &ta, uint32_t splits, hipStream_t st) {
-    const dim3 grid(ta.tiles_m * ta.tiles_n, splits), block(64 * WM * WN);
-    if (splits > 1) mx4_gemm_kernel<WM, WN, TM, TG, S, OCC, T, true><<<grid, block, 0, st>>>(ta);
-    else mx4_gemm_kernel<WM, WN, TM, TG, S, OCC, T, false><<<grid, block, 0, st>>>(ta);
+template <int WM, int WN, int TM, int TN, int S, int OCC, typename T>
+static void launch_tile(const Mx4TileArgs &ta, hipStream_t st) {
+    constexpr uint32_t kLds = 32 * (TM * WM + TN * WN) * S * 136 + WM * WN * kCorner, kByLds = 163840 / kLds, kByWaves = 4 * OCC / (WM * WN);
+    const uint32_t items = ta.tiles_m * ta.tiles_n * ta.splits, most = 256 * (kByLds < kByWaves ? kByLds : kByWaves);
+    const dim3 grid(items < most ? items : most), block(64 * WM * WN);
+    if (ta.splits > 1) mx4_gemm_kernel<WM, WN, TM, TN, S, OCC, T, true><<<grid, block, 0, st>>>(ta);
+    else mx4_gemm_kernel<WM, WN, TM, TN, S, OCC, T, false><<<grid, block, 0, st>>>(ta);
 }
 
 template <typename T>
 static int launch(const Mx4GemmArgs &ga, hipStream_t st) {
-    const Mx4Choice c = choose(ga.M, ga.N, ga.K);
+    Mx4Choice c = choose(ga.M, ga.N, ga.K);
+#ifdef OMC_FORCE
+    c = OMC_FORCE;
+#endif
     const uint32_t stages = (ga.K + 255) / 256, each = (stages + c.splits - 1) / c.splits, splits = (stages + each - 1) / each;
-    const Mx4TileArgs ta{ga, (ga.M + c.bm - 1) / c.bm, (ga.N + c.bn - 1) / c.bn, each};
+    const Mx4TileArgs ta{ga, (ga.M + c.bm - 1) / c.bm, (ga.N + c.bn - 1) / c.bn, splits, each};
     switch (c.tile) {
-        case 0: launch_tile<2, 4, 8, 1, 2, 2, T>(ta, splits, st); break;
-        case 1: launch_tile<2, 2, 4, 1, 2, 2, T>(ta, splits, st); break;
-        default: launch_tile<4, 1, 1, 1, 2, 4, T>(ta, splits, st); break;
+        case 0: launch_tile<2, 2, 4, 4, 2, 1, T>(ta, st); break;
+        case 1: launch_tile<4, 2, 2, 2, 2, 2, T>(ta, st); break;
+        case 2: launch_tile<2, 2, 2, 2, 2, 2, T>(ta, st); break;
+        case 3: launch_tile<2, 2, 2, 1, 2, 2, T>(ta, st); break;
+        default: launch_tile<2, 2, 1, 1, 4, 2, T>(ta, st); break;
     }
     if (splits > 1) {
         const hipError_t e = hipGetLastError();

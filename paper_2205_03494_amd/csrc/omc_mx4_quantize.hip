@@ -50,14 +50,53 @@ __device__ __forceinline__ void quantize_eight(const QuantArgs &qa, const Eight<
     if (!mine) return;
     if (qa.codes) {
         *reinterpret_cast<uint32_t *>(qa.codes + static_cast<uint64_t>(row) * (padded / 2) + col / 2) = codes;
-        if (col % 32 == 0) qa.scales[static_cast<uint64_t>(row) * (padded / 32) + col / 32] = static_cast<uint8_t>(byte);
+        if (col % 32 == 0) {
+            const uint32_t block = col / 32;
+            if (!qa.images) {
+                qa.scales[static_cast<uint64_t>(row) * (padded / 32) + block] = static_cast<uint8_t>(byte);
+            } else {
+                uint8_t *to = qa.scales + (block / 8) * mx4_image_pitch(qa.rows) + 8ull * row;
+                to[mx4_image_byte(block % 8)] = static_cast<uint8_t>(byte);
+                if (block % 8 == 0 && col + 128 == padded) {
+                    *reinterpret_cast<uint16_t *>(to + mx4_image_byte(4)) = 0;
+                    *reinterpret_cast<uint16_t *>(to + mx4_image_byte(6)) = 0;
+                }
+            }
+        }
     }
     if (qa.values && col < qa.cols) store_values<T>(qa, row, col, codes, byte);
 }
 
-// `first`: row of the launch's first item (a launch has less than 2^32 items).
+// 8 bytes of scales of a row, a thread.
+__device__ __forceinline__ void reorder_scales(const Mx4Reorder &re, uint32_t block) {
+    const uint32_t k128 = mx4_padded(re.cols) / 128, stages = (k128 + 1) / 2, groups = (re.rows + 255) / 256;
+    const uint32_t stage = block / groups, row = block % groups * 256 + threadIdx.x;
+    if (stage >= stages || row >= re.rows) return;
+    const uint32_t *from = reinterpret_cast<const uint32_t *>(re.scales) + static_cast<uint64_t>(row) * k128 + 2 * stage;
+    const uint32_t lower = from[0], upper = 2 * stage + 1 < k128 ? from[1] : 0u;
+    uint32_t *to = reinterpret_cast<uint32_t *>(re.image + stage * mx4_image_pitch(re.rows)) + 2 * row;
+    to[0] = (lower & 0xffffu) | upper << 16;
+    to[1] = lower >> 16 | (upper & 0xffff0000u);
+}
+static uint32_t reorder_blocks(const Mx4Reorder &re) { return re.image ? (re.rows + 255) / 256 * ((mx4_padded(re.cols) + 255) / 256) : 0u; }
+
+__global__ __launch_bounds__(256) void mx4_reorder_kernel(Mx4Reorder a, Mx4Reorder b, uint32_t blocks_a) {
+    if (blockIdx.x < blocks_a) reorder_scales(a, blockIdx.x);
+    else reorder_scales(b, blockIdx.x - blocks_a);
+}
+int launch_mx4_reorder(const Mx4Reorder &a, const Mx4Reorder &b, void *stream) {
+    const uint32_t blocks_a = reorder_blocks(a), blocks = blocks_a + reorder_blocks(b);
+    mx4_reorder_kernel<<<dim3(blocks), dim3(256), 0, static_cast<hipStream_t>(stream)>>>(a, b, blocks_a);
+    return static_cast<int>(hipGetLastError());
+}
+
+// `first`: row of the launch's first item (a launch has less than 2^32 items).  The workgroups behind the items reorder the other matrix' scales.
 template <typename T>
 __global__ __launch_bounds__(256) void mx4_rows_kernel(QuantArgs qa, uint32_t first, uint32_t items) {
+    if (qa.also.image && blockIdx.x >= (items + 255) / 256) {
+        reorder_scales(qa.also, blockIdx.x - (items + 255) / 256);
+        return;
+    }
     const uint32_t padded = mx4_padded(qa.cols), eights = padded / 8, item = blockIdx.x * 256 + threadIdx.x;
     const bool mine = item < items;            // (whole blocks: padded / 8 is a multiple of 16)
     const uint32_t row = first + item / eights, col = 8 * (item % eights);
@@ -116,6 +155,10 @@ __global__ __launch_bounds__(256) void mx4_tiles_kernel(QuantArgs qa, uint32_t t
     __shared__ float sums_lds[4][kTile];
     const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     // neighbours down a column, whose codes share a cache line, one after the other on the same die
+    if (qa.also.image && blockIdx.x >= tiles_r * tiles_c) {
+        reorder_scales(qa.also, blockIdx.x - tiles_r * tiles_c);
+        return;
+    }
     const uint32_t total = tiles_r * tiles_c, q = total / 8, rest = total % 8, die = blockIdx.x % 8;
     const uint32_t id = die * q + min(die, rest) + blockIdx.x / 8;
     const uint32_t tr = id % tiles_r, tc = id / tiles_r;
@@ -182,8 +225,17 @@ __global__ __launch_bounds__(256) void mx4_tiles_kernel(QuantArgs qa, uint32_t t
                     *reinterpret_cast<const u32x4 *>(codes_lds + c * kPitch + 16 * (p % 4));
         }
         const uint32_t c = threadIdx.x;
-        if (c < kTile && c0 + c < qa.cols)
-            *reinterpret_cast<uint32_t *>(qa.scales_t + static_cast<uint64_t>(c0 + c) * (padded_t / 32) + 4 * tr) = *reinterpret_cast<const uint32_t *>(scales_lds + 4 * c);
+        if (c < kTile && c0 + c < qa.cols) {
+            const uint32_t bytes = *reinterpret_cast<const uint32_t *>(scales_lds + 4 * c);
+            if (!qa.images) {
+                *reinterpret_cast<uint32_t *>(qa.scales_t + static_cast<uint64_t>(c0 + c) * (padded_t / 32) + 4 * tr) = bytes;
+            } else {
+                uint16_t *to = reinterpret_cast<uint16_t *>(qa.scales_t + (tr / 2) * mx4_image_pitch(qa.cols) + 8ull * (c0 + c));
+                to[tr % 2] = static_cast<uint16_t>(bytes);
+                to[2 + tr % 2] = static_cast<uint16_t>(bytes >> 16);
+                if (tr % 2 == 0 && tr + 1 == tiles_r) to[1] = to[3] = 0;
+            }
+        }
     }
     if (qa.colsum) {
         const uint32_t c = threadIdx.x;
@@ -204,16 +256,17 @@ __global__ __launch_bounds__(256) void mx4_tiles_kernel(QuantArgs qa, uint32_t t
 }
 
 template <typename T>
-static int launch(const QuantArgs &qa, hipStream_t st) {
+static int launch(QuantArgs qa, hipStream_t st) {
     if (qa.codes_t || qa.colsum) {
         const uint32_t tiles_r = (qa.rows + kTile - 1) / kTile, tiles_c = (qa.cols + kTile - 1) / kTile;
-        mx4_tiles_kernel<T><<<dim3(tiles_r * tiles_c), dim3(256), 0, st>>>(qa, tiles_r, tiles_c);
+        mx4_tiles_kernel<T><<<dim3(tiles_r * tiles_c + reorder_blocks(qa.also)), dim3(256), 0, st>>>(qa, tiles_r, tiles_c);
         return static_cast<int>(hipGetLastError());
     }
     const uint32_t eights = mx4_padded(qa.cols) / 8, most = (1u << 30) / eights;   // rows of one launch
     for (uint32_t first = 0; first < qa.rows; first += most) {
         const uint32_t items = (qa.rows - first < most ? qa.rows - first : most) * eights;
-        mx4_rows_kernel<T><<<dim3((items + 255) / 256), dim3(256), 0, st>>>(qa, first, items);
+        mx4_rows_kernel<T><<<dim3((items + 255) / 256 + reorder_blocks(qa.also)), dim3(256), 0, st>>>(qa, first, items);
+        qa.also.image = nullptr;
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess || qa.rows - first <= most) return static_cast<int>(e);
     }
