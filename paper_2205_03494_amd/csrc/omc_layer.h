@@ -55,7 +55,7 @@ struct Mx4GemmArgs {
 size_t mx4_gemm_workspace(uint32_t M, uint32_t N, uint32_t K);   // bytes of parts
 int launch_mx4_gemm(const Mx4GemmArgs &ga, bool bf16, void *stream);
 // The same for few rows of a, with scales in the order of omc.h.  Where mx4_few_rounds, these may come as they are (`rows`), and are rounded on the way.
-constexpr uint32_t kMx4FewRows = 64;
+constexpr uint32_t kMx4FewRows = 32;
 struct Mx4Rows {
     const void *x;
     uint64_t ldx;
