@@ -36,7 +36,7 @@ struct QuantArgs {
     uint8_t *codes_t, *scales_t;   // blocks along a column; may be null
     void *values;                  // may be null
     uint64_t ldv;
-    float *colsum;                 // partial sums of the columns, one row of them for every 128 rows of x; may be null
+    float *colsum;                 // partial sums of the columns, one row of them for every 256 rows of x; may be null
     bool images;                   // scales and scales_t in the tiles' order
     Mx4Reorder also;               // another matrix' scales, by the same launch
 };

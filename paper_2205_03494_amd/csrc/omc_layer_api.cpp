@@ -84,7 +84,7 @@ static BackwardLayout backward_layout(uint8_t *ws, uint32_t M, uint32_t N, uint3
     l.x_t = p.take(mx4_code_bytes(K, M));
     l.x_t_scales = p.take(scale_bytes(K, K, M));
     if (!few(M)) l.w_image = p.take(mx4_image_bytes(K, N));
-    l.sums = reinterpret_cast<float *>(p.take(4ull * ((M + 127) / 128) * N));
+    l.sums = reinterpret_cast<float *>(p.take(4ull * ((M + 255) / 256) * N));
     const uint64_t dx = parts_bytes(M, K, N), dw = parts_bytes(K, N, M);
     l.parts = reinterpret_cast<float *>(p.take(dx > dw ? dx : dw));
     l.bytes = p.used;
@@ -195,7 +195,7 @@ omc_status omc_mx4_linear_backward(const void *dY, uint64_t lddy, const void *X,
         rc = launch_mx4_quantize(ta, bf16, stream);
     }
     if (rc == 0) rc = launch_mx4_quantize(qa, bf16, stream);
-    if (rc == 0 && dbias) rc = launch_column_sums(l.sums, (M + 127) / 128, N, N, dbias, nullptr, stream);
+    if (rc == 0 && dbias) rc = launch_column_sums(l.sums, (M + 255) / 256, N, N, dbias, nullptr, stream);
     if (rc == 0 && dX) {
         const Mx4GemmArgs ga{{l.dy, l.dy_scales}, {bytes(w_codes), dx_tiles ? l.w_image : bytes(w_scales)}, nullptr, dX, lddx, M, K, N, l.parts};
         rc = launch_product(ga, dx_type == OMC_BF16, stream);

@@ -34,7 +34,7 @@ __global__ __launch_bounds__(512) void mx4_few_kernel(Mx4GemmArgs g, Mx4Rows row
     // ---- global -> LDS: a load is 8 rows of an operand, lane l's piece l % 8 of row l / 8, XOR-swizzled by half the row
     uint8_t *ring = few_lds + wave * (S * kStage);
     const uint32_t ring0 = lds_offset(few_lds) + wave * (S * kStage), last_n = g.N - 1 - n0;
-    uint32_t off[2 * kOperands], piece[2], s_off[kScaleLoads];
+    uint32_t off[2 * kOperands], piece[2];
 #pragma unroll
     for (uint32_t i = 0; i < 2; ++i) piece[i] = (lane & 7u) ^ ((4 * i + (lane >> 4)) & 7u);
 #pragma unroll
@@ -43,22 +43,19 @@ __global__ __launch_bounds__(512) void mx4_few_kernel(Mx4GemmArgs g, Mx4Rows row
         off[i] = (i < 2 ? min(row, last_n) : min(16 * (i / 2 - 1) + row, g.M - 1)) * row_bytes + 16 * piece[i % 2];
     }
     const uint8_t *b_from = g.b.codes + static_cast<uint64_t>(n0) * row_bytes + 128 * begin, *a_from = g.a.codes + 128 * begin;
-    // scales: B's rows and A's first tile, then A's second; 2 dwords a row
+    // scales, two dwords a row: B's rows and in the upper lanes A's first tile, then A's second tile
+    const uint32_t s_row = lane >> 1, s_dword = 4 * (lane & 1u);
     const uint8_t *b_scales = g.b.scales + static_cast<uint64_t>(n0) * blocks + 8 * begin, *a_scales = FUSED ? b_scales : g.a.scales + 8 * begin;
-    s_off[0] = lane < 32 ? min(lane >> 1, last_n) * blocks + 4 * (lane & 1u) : 0u;
-    if (kScaleLoads > 1) s_off[kScaleLoads - 1] = min(16 + (lane >> 1), g.M - 1) * blocks + 4 * (lane & 1u);
-    const uint8_t *first_scales = lane < 32 || FUSED ? b_scales : a_scales;   // a lane's own
-    const uint32_t first_off = FUSED ? min((lane >> 1) & 15u, last_n) * blocks + 4 * (lane & 1u)
-                                     : lane < 32 ? s_off[0] : min((lane >> 1) - 16, g.M - 1) * blocks + 4 * (lane & 1u);
-    first_scales += first_off;
+    const uint8_t *first_scales = (FUSED || lane < 32 ? b_scales + min(s_row % 16, last_n) * blocks : a_scales + min(s_row - 16, g.M - 1) * blocks) + s_dword;   // (the lane's own)
+    const uint32_t second_scales = min(16 + s_row, g.M - 1) * blocks + s_dword;
     auto load_unit = [&](uint32_t unit, uint32_t at) {
         const bool half = 2 * unit + 1 == k128;               // its second half is not there: the first one twice
 #pragma unroll
         for (uint32_t i = 0; i < 2 * kOperands; ++i)
             load_to_lds(i < 2 ? b_from : a_from, off[i] - (half ? 16 * (piece[i % 2] & 4u) : 0u), ring0 + at + 1024 * i);
-        const uint8_t *own = first_scales - (half ? 4 * (lane & 1u) : 0u);
+        const uint8_t *own = first_scales - (half ? s_dword : 0u);
         asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(ring0 + at + kScales), "v"(own) : "memory", "m0");
-        if constexpr (kScaleLoads > 1) load_dwords_to_lds(a_scales, s_off[kScaleLoads - 1] - (half ? 4 * (lane & 1u) : 0u), ring0 + at + kScales + 256);
+        if constexpr (kScaleLoads > 1) load_dwords_to_lds(a_scales, second_scales - (half ? s_dword : 0u), ring0 + at + kScales + 256);
         b_from += 128;
         a_from += 128;
         first_scales += 8;
@@ -72,19 +69,27 @@ __global__ __launch_bounds__(512) void mx4_few_kernel(Mx4GemmArgs g, Mx4Rows row
     if constexpr (FUSED) {
         uint8_t *codes_lds = few_lds + waves * (S * kStage), *scales_lds = codes_lds + g.M * blocks * 16;
         const uint32_t eights = blocks * 4, items = g.M * eights;
-        for (uint32_t base = 0; base < items; base += blockDim.x) {   // (blocks stay together: both counts are multiples of 4)
-            const uint32_t item = base + threadIdx.x, row = item / eights, col = 8 * (item % eights);
-            Eight<X> v;
-            v.clear();
-            if (item < items && col < g.K) v.load(static_cast<const typename X::type *>(rows.x) + row * rows.ldx + col, g.K - col);
-            uint32_t top = v.top();
-            top = max(top, static_cast<uint32_t>(__builtin_amdgcn_mov_dpp(static_cast<int>(top), 0xb1, 0xf, 0xf, true)));
-            top = max(top, static_cast<uint32_t>(__builtin_amdgcn_mov_dpp(static_cast<int>(top), 0x4e, 0xf, 0xf, true)));
-            const uint32_t byte = mx4_scale<X>(top);
-            const uint32_t codes = byte == kMx4NaN ? 0u : v.codes(mx4_unit(byte));
-            if (item < items) {
-                reinterpret_cast<uint32_t *>(codes_lds)[item] = codes;
-                if (item % 4 == 0) scales_lds[item / 4] = static_cast<uint8_t>(byte);
+        constexpr uint32_t kTogether = 4;                     // loads on their way at a time
+        for (uint32_t base = 0; base < items; base += kTogether * blockDim.x) {   // (blocks stay together: both counts are multiples of 4)
+            Eight<X> v[kTogether];
+#pragma unroll
+            for (uint32_t k = 0; k < kTogether; ++k) {
+                const uint32_t item = base + k * blockDim.x + threadIdx.x, row = item / eights, col = 8 * (item % eights);
+                v[k].clear();
+                if (item < items && col < g.K) v[k].load(static_cast<const typename X::type *>(rows.x) + row * rows.ldx + col, g.K - col);
+            }
+#pragma unroll
+            for (uint32_t k = 0; k < kTogether; ++k) {
+                const uint32_t item = base + k * blockDim.x + threadIdx.x;
+                uint32_t top = v[k].top();
+                top = max(top, static_cast<uint32_t>(__builtin_amdgcn_mov_dpp(static_cast<int>(top), 0xb1, 0xf, 0xf, true)));
+                top = max(top, static_cast<uint32_t>(__builtin_amdgcn_mov_dpp(static_cast<int>(top), 0x4e, 0xf, 0xf, true)));
+                const uint32_t byte = mx4_scale<X>(top);
+                const uint32_t codes = byte == kMx4NaN ? 0u : v[k].codes(mx4_unit(byte));
+                if (item < items) {
+                    reinterpret_cast<uint32_t *>(codes_lds)[item] = codes;
+                    if (item % 4 == 0) scales_lds[item / 4] = static_cast<uint8_t>(byte);
+                }
             }
         }
         sync_lds();

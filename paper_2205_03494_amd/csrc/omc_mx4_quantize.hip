@@ -2,10 +2,10 @@
 //
 // Bound by memory: 2 or 4 bytes read and 17/32 written a value and direction, some ten instructions a value between them.
 //
-// Along rows a lane takes eight neighbours, 16 or 32 bytes and one dword of codes, and the four lanes of a block compare their largest magnitudes.
+// Along rows alone a lane takes eight neighbours, 16 or 32 bytes and one dword of codes, and the four lanes of a block compare their largest magnitudes.
 // Along columns a wave takes 32 rows x 128 columns, a lane two columns of them, so that a lane holds two whole blocks and no lane needs another's
-// values; the codes of a workgroup's 128 rows go through LDS, so that 64 bytes of a column are written together.  Where both
-// directions are asked for, the tile is read a second time, row-wise, from the cache.
+// values; the codes of a workgroup's 256 rows go through LDS, so that 128 bytes of a column are written together.  Where both directions are asked for, 16 lanes compare
+// their largest magnitudes of a row, from the same registers.
 #include "omc_mx4.h"
 
 namespace omc {
@@ -71,7 +71,7 @@ __device__ __forceinline__ void quantize_eight(const QuantArgs &qa, const Eight<
 __device__ __forceinline__ void reorder_scales(const Mx4Reorder &re, uint32_t block) {
     const uint32_t k128 = mx4_padded(re.cols) / 128, stages = (k128 + 1) / 2, groups = (re.rows + 255) / 256;
     const uint32_t stage = block / groups, row = block % groups * 256 + threadIdx.x;
-    if (stage >= stages || row >= re.rows) return;
+    if (stage >= stages || row >= re.rows || threadIdx.x >= 256) return;
     const uint32_t *from = reinterpret_cast<const uint32_t *>(re.scales) + static_cast<uint64_t>(row) * k128 + 2 * stage;
     const uint32_t lower = from[0], upper = 2 * stage + 1 < k128 ? from[1] : 0u;
     uint32_t *to = reinterpret_cast<uint32_t *>(re.image + stage * mx4_image_pitch(re.rows)) + 2 * row;
@@ -106,11 +106,11 @@ __global__ __launch_bounds__(256) void mx4_rows_kernel(QuantArgs qa, uint32_t fi
     quantize_eight<T>(qa, v, row, col, padded, mine);
 }
 
-constexpr uint32_t kTile = 128;
+constexpr uint32_t kHigh = 256, kWide = 128;   // a tile; a wave takes 32 rows of it
 
-// Two columns of 32 rows in a lane: their blocks' codes and scale bytes.
+// Two columns of 32 rows in a lane (bf16: both in lo): their blocks' codes and scale bytes.
 template <typename T>
-__device__ __forceinline__ void quantize_pair(const uint32_t (&lo)[32], const uint32_t (&hi)[32], u32x4 (&codes)[2], uint32_t (&byte)[2]) {
+__device__ __forceinline__ void quantize_columns(const uint32_t (&lo)[32], const uint32_t (&hi)[32], u32x4 (&codes)[2], uint32_t (&byte)[2]) {
     uint32_t top[2] = {0, 0};
     if constexpr (T::kBytes == 4) {
 #pragma unroll
@@ -145,112 +145,161 @@ __device__ __forceinline__ void quantize_pair(const uint32_t (&lo)[32], const ui
     }
 }
 
-// Tiles of 128 x 128: blocks along the columns, the columns' sums, and on a second read blocks along the rows.
+// Largest of 16 lanes' values, in all of them.
+template <typename M>
+__device__ __forceinline__ uint32_t largest_of_16(uint32_t x, M &&larger) {
+    x = larger(x, static_cast<uint32_t>(__builtin_amdgcn_mov_dpp(static_cast<int>(x), 0xb1, 0xf, 0xf, true)));    // lanes 1 0 3 2
+    x = larger(x, static_cast<uint32_t>(__builtin_amdgcn_mov_dpp(static_cast<int>(x), 0x4e, 0xf, 0xf, true)));    // lanes 2 3 0 1
+    x = larger(x, static_cast<uint32_t>(__builtin_amdgcn_mov_dpp(static_cast<int>(x), 0x141, 0xf, 0xf, true)));   // eight lanes mirrored
+    return larger(x, static_cast<uint32_t>(__builtin_amdgcn_mov_dpp(static_cast<int>(x), 0x140, 0xf, 0xf, true)));   // sixteen lanes mirrored
+}
+
+// The same registers along the rows, of which 16 lanes hold a block: a lane's two codes of row i go to codes[i * 64 + lane], the scale of row i and block b to scales[i * 4 + b].
 template <typename T>
-__global__ __launch_bounds__(256) void mx4_tiles_kernel(QuantArgs qa, uint32_t tiles_r, uint32_t tiles_c) {
+__device__ __forceinline__ void quantize_rows(const uint32_t (&lo)[32], const uint32_t (&hi)[32], uint8_t *codes, uint8_t *scales, uint32_t lane) {
+    auto one = [&](uint32_t i, uint32_t top) {
+        const uint32_t byte = mx4_scale<T>(top);
+        const float unit = mx4_unit(byte);
+        uint32_t c;
+        if constexpr (T::kBytes == 4) c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, __uint_as_float(lo[i]), __uint_as_float(hi[i]), unit, 0);
+        else c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(0u, __builtin_bit_cast(bf16x2, lo[i]), unit, 0);
+        codes[i * 64 + lane] = static_cast<uint8_t>(byte == kMx4NaN ? 0u : c);
+        if ((lane & 15u) == 0) scales[i * 4 + (lane >> 4)] = static_cast<uint8_t>(byte);
+    };
+    if constexpr (T::kBytes == 4) {
+#pragma unroll
+        for (uint32_t i = 0; i < 32; ++i) one(i, largest_of_16(max(lo[i] & 0x7fffffffu, hi[i] & 0x7fffffffu), [](uint32_t x, uint32_t y) { return max(x, y); }));
+    } else {
+        auto larger = [](uint32_t x, uint32_t y) { return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, x), __builtin_bit_cast(u16x2, y))); };
+#pragma unroll
+        for (uint32_t i = 0; i < 32; i += 2) {   // two rows' largest in a register
+            const uint32_t x = lo[i] & 0x7fff7fffu, y = lo[i + 1] & 0x7fff7fffu;
+            const uint32_t top = largest_of_16(larger(__builtin_amdgcn_perm(y, x, 0x05040100u), __builtin_amdgcn_perm(y, x, 0x07060302u)), larger);
+            one(i, top & 0xffffu);
+            one(i + 1, top >> 16);
+        }
+    }
+}
+
+// Tiles of 256 x 128: blocks along the columns, along the rows, the columns' sums.
+template <typename T>
+__global__ __launch_bounds__(512) void mx4_tiles_kernel(QuantArgs qa, uint32_t tiles_r, uint32_t tiles_c) {
     typedef typename T::type E;
-    constexpr uint32_t kPitch = 80;            // bytes of a column's codes in LDS, 64 and padding
-    __shared__ __attribute__((aligned(16))) uint8_t codes_lds[kTile * kPitch];
-    __shared__ uint8_t scales_lds[kTile * 4];
-    __shared__ float sums_lds[4][kTile];
-    const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    // neighbours down a column, whose codes share a cache line, one after the other on the same die
+    constexpr uint32_t kPitch = 144;           // bytes of a column's codes in LDS, 128 and padding
+    __shared__ __attribute__((aligned(16))) uint8_t codes_lds[kWide * kPitch];
+    __shared__ __attribute__((aligned(16))) uint8_t rows_lds[8][32 * 64];
+    __shared__ __attribute__((aligned(16))) uint8_t scales_lds[kWide * 8];
+    __shared__ __attribute__((aligned(16))) uint8_t row_scales_lds[8][32 * 4];
+    __shared__ float sums_lds[8][kWide];
     if (qa.also.image && blockIdx.x >= tiles_r * tiles_c) {
         reorder_scales(qa.also, blockIdx.x - tiles_r * tiles_c);
         return;
     }
-    const uint32_t total = tiles_r * tiles_c, q = total / 8, rest = total % 8, die = blockIdx.x % 8;
-    const uint32_t id = die * q + min(die, rest) + blockIdx.x / 8;
-    const uint32_t tr = id % tiles_r, tc = id / tiles_r;
-    const uint32_t r0 = tr * kTile + 32 * wave, c0 = tc * kTile, col = c0 + 2 * lane;
+    const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t tr = blockIdx.x / tiles_c, tc = blockIdx.x % tiles_c;
+    const uint32_t r0 = tr * kHigh + 32 * wave, c0 = tc * kWide, col = c0 + 2 * lane;
     const uint32_t height = r0 < qa.rows ? min(32u, qa.rows - r0) : 0u;
     const E *x = static_cast<const E *>(qa.x);
-    const uint32_t padded_t = mx4_padded(qa.rows);
 
-    uint32_t lo[32], hi[32];                   // bf16: both columns in lo
-    if (height == 32 && c0 + kTile <= qa.cols) {
-        const E *from = x + r0 * qa.ldx + col;
+    uint32_t lo[32], hi[32];
+#pragma unroll
+    for (uint32_t i = 0; i < 32; ++i) lo[i] = hi[i] = 0;
+    auto put = [&](uint32_t i, const E *from) {   // both columns, from any address
+        uint32_t w[T::kBytes / 2];
+        __builtin_memcpy(w, from, 2 * T::kBytes);
+        lo[i] = w[0];
+        if constexpr (T::kBytes == 4) hi[i] = w[1];
+    };
+    if (height == 32 && c0 + kWide <= qa.cols) {
+#pragma unroll
+        for (uint32_t i = 0; i < 32; ++i) put(i, x + (r0 + i) * qa.ldx + col);
+    } else if (height > 0 && qa.cols > 1) {    // at the edges: what lies outside is read in the last row or the last two columns, and is zero
+        const uint32_t at = min(col, qa.cols - 2);
+        const bool in0 = col < qa.cols, in1 = col + 1 < qa.cols, shifted = col + 1 == qa.cols;
+#pragma unroll
+        for (uint32_t i = 0; i < 32; ++i) put(i, x + (r0 + min(i, height - 1)) * qa.ldx + at);
 #pragma unroll
         for (uint32_t i = 0; i < 32; ++i) {
-            uint32_t w[T::kBytes / 2];
-            __builtin_memcpy(w, from + i * qa.ldx, 2 * T::kBytes);
-            lo[i] = w[0];
-            if constexpr (T::kBytes == 4) hi[i] = w[1];
-        }
-    } else if (height > 0) {                   // at the edges: what lies outside is read at the last row or column, and is zero
-        const E *from0 = x + r0 * qa.ldx + min(col, qa.cols - 1), *from1 = x + r0 * qa.ldx + min(col + 1, qa.cols - 1);
-        const bool in0 = col < qa.cols, in1 = col + 1 < qa.cols;
-#pragma unroll
-        for (uint32_t i = 0; i < 32; ++i) {
-            const uint64_t at = min(i, height - 1) * qa.ldx;
-            const E v0 = from0[at], v1 = from1[at];
+            const bool in = i < height;
             if constexpr (T::kBytes == 4) {
-                lo[i] = in0 && i < height ? __builtin_bit_cast(uint32_t, v0) : 0u;
-                hi[i] = in1 && i < height ? __builtin_bit_cast(uint32_t, v1) : 0u;
+                lo[i] = in && in0 ? (shifted ? hi[i] : lo[i]) : 0u;
+                hi[i] = in && in1 ? hi[i] : 0u;
             } else {
-                lo[i] = (in0 && i < height ? v0 : 0u) | (in1 && i < height ? static_cast<uint32_t>(v1) << 16 : 0u);
+                lo[i] = in && in0 ? (shifted ? lo[i] >> 16 : lo[i]) : 0u;
             }
         }
-    } else {
+    } else if (height > 0 && lane == 0) {
 #pragma unroll
-        for (uint32_t i = 0; i < 32; ++i) lo[i] = hi[i] = 0;
+        for (uint32_t i = 0; i < 32; ++i)
+            if (i < height) {
+                const E v = x[(r0 + i) * qa.ldx];
+                if constexpr (T::kBytes == 4) lo[i] = __float_as_uint(v);
+                else lo[i] = v;
+            }
     }
     if (qa.codes_t) {
         u32x4 codes[2];
         uint32_t byte[2];
-        quantize_pair<T>(lo, hi, codes, byte);
+        quantize_columns<T>(lo, hi, codes, byte);
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
             *reinterpret_cast<u32x4 *>(codes_lds + (2 * lane + c) * kPitch + 16 * wave) = codes[c];
-            scales_lds[(2 * lane + c) * 4 + wave] = static_cast<uint8_t>(byte[c]);
+            scales_lds[(2 * lane + c) * 8 + (qa.images ? mx4_image_byte(wave) : wave)] = static_cast<uint8_t>(byte[c]);
         }
     }
+    if (qa.codes) quantize_rows<T>(lo, hi, rows_lds[wave], row_scales_lds[wave], lane);
     if (qa.colsum) {
         float s0 = 0.0f, s1 = 0.0f;
 #pragma unroll
         for (int i = 0; i < 32; ++i) {
-            s0 += T::kBytes == 4 ? __builtin_bit_cast(float, lo[i]) : bf16_low(lo[i]);
-            s1 += T::kBytes == 4 ? __builtin_bit_cast(float, hi[i]) : bf16_high(lo[i]);
+            s0 += T::kBytes == 4 ? __uint_as_float(lo[i]) : bf16_low(lo[i]);
+            s1 += T::kBytes == 4 ? __uint_as_float(hi[i]) : bf16_high(lo[i]);
         }
         sums_lds[wave][2 * lane] = s0;
         sums_lds[wave][2 * lane + 1] = s1;
     }
     __syncthreads();
     if (qa.codes_t) {
+        const uint32_t pitch = mx4_padded(qa.rows) / 2, begin = tr * (kHigh / 2), there = min(pitch - begin, kHigh / 2);   // bytes of a column, of those in this tile
 #pragma unroll
-        for (uint32_t p = threadIdx.x; p < 4 * kTile; p += 256) {
-            const uint32_t c = p / 4;
-            if (c0 + c < qa.cols)
-                *reinterpret_cast<u32x4 *>(qa.codes_t + static_cast<uint64_t>(c0 + c) * (padded_t / 2) + tr * (kTile / 2) + 16 * (p % 4)) =
-                    *reinterpret_cast<const u32x4 *>(codes_lds + c * kPitch + 16 * (p % 4));
+        for (uint32_t p = threadIdx.x; p < 8 * kWide; p += 512) {
+            const uint32_t c = p / 8, at = 16 * (p % 8);
+            if (c0 + c < qa.cols && at < there)
+                *reinterpret_cast<u32x4 *>(qa.codes_t + static_cast<uint64_t>(c0 + c) * pitch + begin + at) = *reinterpret_cast<const u32x4 *>(codes_lds + c * kPitch + at);
         }
-        const uint32_t c = threadIdx.x;
-        if (c < kTile && c0 + c < qa.cols) {
-            const uint32_t bytes = *reinterpret_cast<const uint32_t *>(scales_lds + 4 * c);
+        const uint32_t c = threadIdx.x / 2, half = threadIdx.x % 2;
+        if (threadIdx.x < 2 * kWide && c0 + c < qa.cols) {
+            const uint32_t bytes = reinterpret_cast<const uint32_t *>(scales_lds)[threadIdx.x];
+            if (qa.images) reinterpret_cast<uint32_t *>(qa.scales_t + tr * mx4_image_pitch(qa.cols))[2 * (c0 + c) + half] = bytes;
+            else if (64 * half < there) reinterpret_cast<uint32_t *>(qa.scales_t + static_cast<uint64_t>(c0 + c) * (pitch / 16))[2 * tr + half] = bytes;
+        }
+    }
+    if (qa.codes) {                            // 64 bytes of a row (all of them: rows are padded to 128 values)
+        const uint32_t pitch = mx4_padded(qa.cols) / 2;
+#pragma unroll
+        for (uint32_t k = 0; k < 2; ++k) {
+            const uint32_t i = 16 * k + lane / 4, at = 16 * (lane % 4);
+            if (i < height) *reinterpret_cast<u32x4 *>(qa.codes + static_cast<uint64_t>(r0 + i) * pitch + 64 * tc + at) = *reinterpret_cast<const u32x4 *>(rows_lds[wave] + 64 * i + at);
+        }
+        if (lane < height) {
+            const uint32_t bytes = reinterpret_cast<const uint32_t *>(row_scales_lds[wave])[lane];
             if (!qa.images) {
-                *reinterpret_cast<uint32_t *>(qa.scales_t + static_cast<uint64_t>(c0 + c) * (padded_t / 32) + 4 * tr) = bytes;
-            } else {
-                uint16_t *to = reinterpret_cast<uint16_t *>(qa.scales_t + (tr / 2) * mx4_image_pitch(qa.cols) + 8ull * (c0 + c));
-                to[tr % 2] = static_cast<uint16_t>(bytes);
-                to[2 + tr % 2] = static_cast<uint16_t>(bytes >> 16);
-                if (tr % 2 == 0 && tr + 1 == tiles_r) to[1] = to[3] = 0;
+                reinterpret_cast<uint32_t *>(qa.scales + static_cast<uint64_t>(r0 + lane) * (pitch / 16))[tc] = bytes;
+            } else {                           // blocks 0, 1 and 2, 3 of a first or second half
+                uint16_t *to = reinterpret_cast<uint16_t *>(qa.scales + (tc / 2) * mx4_image_pitch(qa.rows) + 8ull * (r0 + lane));
+                to[tc % 2] = static_cast<uint16_t>(bytes);
+                to[2 + tc % 2] = static_cast<uint16_t>(bytes >> 16);
+                if (tc % 2 == 0 && tc + 1 == tiles_c) to[1] = to[3] = 0;
             }
         }
     }
     if (qa.colsum) {
         const uint32_t c = threadIdx.x;
-        if (c < kTile && c0 + c < qa.cols)
-            qa.colsum[static_cast<uint64_t>(tr) * qa.cols + c0 + c] = (sums_lds[0][c] + sums_lds[1][c]) + (sums_lds[2][c] + sums_lds[3][c]);
-    }
-    if (qa.codes || qa.values) {
-        const uint32_t at = c0 + 8 * (lane & 15u);
+        if (c < kWide && c0 + c < qa.cols) {
+            float s = sums_lds[0][c];
 #pragma unroll
-        for (uint32_t i = 0; i < 8; ++i) {
-            const uint32_t r = 4 * i + (lane >> 4);
-            Eight<T> v;
-            v.clear();
-            if (r < height && at < qa.cols) v.load(x + (r0 + r) * qa.ldx + at, qa.cols - at);
-            quantize_eight<T>(qa, v, r0 + r, at, mx4_padded(qa.cols), r < height);
+            for (int w = 1; w < 8; ++w) s += sums_lds[w][c];
+            qa.colsum[static_cast<uint64_t>(tr) * qa.cols + c0 + c] = s;
         }
     }
 }
@@ -258,9 +307,13 @@ __global__ __launch_bounds__(256) void mx4_tiles_kernel(QuantArgs qa, uint32_t t
 template <typename T>
 static int launch(QuantArgs qa, hipStream_t st) {
     if (qa.codes_t || qa.colsum) {
-        const uint32_t tiles_r = (qa.rows + kTile - 1) / kTile, tiles_c = (qa.cols + kTile - 1) / kTile;
-        mx4_tiles_kernel<T><<<dim3(tiles_r * tiles_c + reorder_blocks(qa.also)), dim3(256), 0, st>>>(qa, tiles_r, tiles_c);
-        return static_cast<int>(hipGetLastError());
+        QuantArgs ta = qa;
+        if (qa.values) ta.codes = ta.scales = nullptr;   // these along the rows, with the values
+        const uint32_t tiles_r = (qa.rows + kHigh - 1) / kHigh, tiles_c = (qa.cols + kWide - 1) / kWide;
+        mx4_tiles_kernel<T><<<dim3(tiles_r * tiles_c + reorder_blocks(qa.also)), dim3(512), 0, st>>>(ta, tiles_r, tiles_c);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess || !qa.values) return static_cast<int>(e);
+        qa.also.image = nullptr;
     }
     const uint32_t eights = mx4_padded(qa.cols) / 8, most = (1u << 30) / eights;   // rows of one launch
     for (uint32_t first = 0; first < qa.rows; first += most) {
