@@ -64,15 +64,15 @@ struct Mx4TileArgs {
     uint32_t tiles_m, tiles_n, splits, stages_per_split;
 };
 
-// WM x WN waves of TM x TN matrix tiles, OCC waves per SIMD.  SPLIT: the contraction is cut into parts, whose results go to g.parts in fp32.
-template <int WM, int WN, int TM, int TN, int S, int OCC, typename T, bool SPLIT>
-__global__ __attribute__((amdgpu_flat_work_group_size(64 * WM * WN, 64 * WM * WN))) __attribute__((amdgpu_waves_per_eu(OCC, OCC)))
+// WM x WN waves of TM x TN matrix tiles, and LOADERS that load for all (0: every wave loads its share), OCC waves per SIMD.  SPLIT: the contraction is cut into parts, whose results go to g.parts in fp32.
+template <int WM, int WN, int TM, int TN, int LOADERS, int S, int OCC, typename T, bool SPLIT>
+__global__ __attribute__((amdgpu_flat_work_group_size(64 * (WM * WN + LOADERS), 64 * (WM * WN + LOADERS)))) __attribute__((amdgpu_waves_per_eu(OCC, OCC)))
 void mx4_gemm_kernel(Mx4TileArgs ta) {
-    constexpr int NW = WM * WN, BM = 32 * TM * WM, BN = 32 * TN * WN;
-    constexpr int kALoads = BM / 8 / NW, kBLoads = BN / 8 / NW, kLoads = kALoads + kBLoads + 1;
-    constexpr uint32_t kB = BM * 128, kS = kB + BN * 128, kStage = kS + (BM + BN) * 8, kScaleLoads = (BM + BN) / 128, kCorners = S * kStage;
+    constexpr int NW = WM * WN, kLoaders = LOADERS > 0 ? LOADERS : NW, BM = 32 * TM * WM, BN = 32 * TN * WN;
+    constexpr int kALoads = BM / 8 / kLoaders, kBLoads = BN / 8 / kLoaders, kLoads = kALoads + kBLoads + 1;
+    constexpr uint32_t kB = BM * 128, kS = kB + BN * 128, kStage = kS + (BM + BN) * 8, kScaleLoads = (BM + BN + 127) / 128, kCorners = S * kStage;
     constexpr int kStores = TM * TN * (T::kBytes == 2 && !SPLIT ? 2 : 4);
-    static_assert(BM % (8 * NW) == 0 && BN % (8 * NW) == 0 && NW % 4 == 0 && kScaleLoads >= 1 && 256 % BM == 0 && 256 % BN == 0, "whole loads, one swizzle per wave");
+    static_assert(BM % (8 * kLoaders) == 0 && BN % (8 * kLoaders) == 0 && kScaleLoads <= kLoaders && 256 % BM == 0 && 256 % BN == 0, "whole loads");
     __shared__ __attribute__((aligned(1024))) uint8_t lds[kCorners + NW * kCorner];
     const Mx4GemmArgs &g = ta.g;
     const uint32_t lds0 = lds_offset(lds);
@@ -95,18 +95,22 @@ void mx4_gemm_kernel(Mx4TileArgs ta) {
         return p;
     };
 
-    // ---- global -> LDS: load i of a wave is the rows 8 (wave + NW i) .. + 8 of an operand, lane l's piece l % 8 of row l / 8 (before the swizzle).  Rows past the end: the last one again.
+    // ---- global -> LDS: load i of a loader is the rows 8 (loader + kLoaders i) .. + 8 of an operand, lane l's piece l % 8 of row l / 8 (before the swizzle).  Rows past the end: the last one
+    // again.
+    const uint32_t loader = LOADERS > 0 ? wave - NW : wave;   // (LOADERS > 0: of the waves that load)
     const uint8_t *a_from, *b_from, *s_from;
     uint32_t off[kALoads + kBLoads];
-    const uint32_t a_piece = 16 * ((lane & 7u) ^ ((lane >> 4) + 4 * (wave & 1u)));                  // row / 2 % 8
-    const uint32_t b_piece = 16 * ((lane & 7u) ^ ((lane >> 4) + 4 * ((wave >> 1) & 1u)));           // row / 2 % 4 + 4 (row / 16 % 2)
-    const uint32_t s_unit = wave % kScaleLoads, s_row = 2 * (64 * s_unit + lane);                   // two rows' scales a lane (some waves bring the same)
+    auto load_row = [&](uint32_t i) { return 8 * (loader + kLoaders * i) + (lane >> 3); };
+    auto a_piece = [&](uint32_t i) { return 16 * ((lane & 7u) ^ (load_row(i) >> 1 & 7u)); };
+    auto b_piece = [&](uint32_t i) { return 16 * ((lane & 7u) ^ ((load_row(i) >> 1 & 3u) + 4 * (load_row(i) >> 4 & 1u))); };
+    const uint32_t s_unit = loader % kScaleLoads, s_row = 2 * (64 * s_unit + lane);                 // two rows' scales a lane (some waves bring the same)
     const uint64_t s_pitch = mx4_image_pitch(s_row < BM ? g.M : g.N);
+    const uint64_t s_lanes = __ballot(s_row < BM + BN);
     uint32_t ask_item = blockIdx.x, ask_stage, ask_end;
     uint64_t lanes = ~0ull;                    // that load: none once everything has been asked for
     auto upper_is_lower = [&]() {              // before half a stage
 #pragma unroll
-        for (uint32_t i = 0; i < kALoads + kBLoads; ++i) off[i] -= i < kALoads ? a_piece & 64u : b_piece & 64u;
+        for (uint32_t i = 0; i < kALoads + kBLoads; ++i) off[i] -= (i < kALoads ? a_piece(i) : b_piece(i - kALoads)) & 64u;
     };
     auto ask_for = [&](uint32_t item) {
         const Place p = locate(item);
@@ -115,23 +119,23 @@ void mx4_gemm_kernel(Mx4TileArgs ta) {
         s_from = (s_row < BM ? g.a.scales + 8ull * (p.m0 + s_row) : g.b.scales + 8ull * (p.n0 + s_row - BM)) + p.first * s_pitch;
         const uint32_t last_m = g.M - 1 - p.m0, last_n = g.N - 1 - p.n0;
 #pragma unroll
-        for (uint32_t i = 0; i < kALoads; ++i) off[i] = min(8 * (wave + NW * i) + (lane >> 3), last_m) * row_bytes + a_piece;
+        for (uint32_t i = 0; i < kALoads; ++i) off[i] = min(load_row(i), last_m) * row_bytes + a_piece(i);
 #pragma unroll
-        for (uint32_t i = 0; i < kBLoads; ++i) off[kALoads + i] = min(8 * (wave + NW * i) + (lane >> 3), last_n) * row_bytes + b_piece;
+        for (uint32_t i = 0; i < kBLoads; ++i) off[kALoads + i] = min(load_row(i), last_n) * row_bytes + b_piece(i);
         ask_stage = p.first;
         ask_end = p.first + p.stages;
         if (ask_stage == half_at) upper_is_lower();
     };
-    const uint32_t codes_to = lds0 + 1024 * wave, scales_to = lds0 + kS + 1024 * s_unit;
+    const uint32_t codes_to = lds0 + 1024 * loader, scales_to = lds0 + kS + 1024 * s_unit;
     struct From {
         const uint8_t *a, *b;
     };
     auto from_now = [&]() { return From{in_scalars(a_from), in_scalars(b_from)}; };
     auto load_one = [&](const From &from, uint32_t at, auto index) {
         constexpr uint32_t I = decltype(index)::value;
-        if constexpr (I < kALoads) load_pieces<1024 * NW * I>(from.a, off[I], codes_to + at, lanes);
-        else if constexpr (I < kALoads + kBLoads) load_pieces<kB + 1024 * NW * (I - kALoads)>(from.b, off[I], codes_to + at, lanes);
-        else load_pieces<0>(s_from, scales_to + at, lanes);
+        if constexpr (I < kALoads) load_pieces<1024 * kLoaders * I>(from.a, off[I], codes_to + at, lanes);
+        else if constexpr (I < kALoads + kBLoads) load_pieces<kB + 1024 * kLoaders * (I - kALoads)>(from.b, off[I], codes_to + at, lanes);
+        else load_pieces<0>(s_from, scales_to + at, lanes & s_lanes);
     };
     auto load_stage = [&](uint32_t at) {
         const From from = from_now();
@@ -150,6 +154,26 @@ void mx4_gemm_kernel(Mx4TileArgs ta) {
             if (ask_stage == half_at) upper_is_lower();
         }
     };
+
+    uint32_t far = (S - 1) * kStage;           // the stage that is asked for
+    if (LOADERS > 0 && wave >= NW) {                 // as many barriers as the other waves, which have one for every stage and one before the first
+        ask_for(ask_item);
+#pragma unroll
+        for (uint32_t i = 0; i < S - 1; ++i) {
+            load_stage(i * kStage);
+            next_stage();
+        }
+        uint32_t stages = 0;
+        for (uint32_t item = blockIdx.x; item < items; item += gridDim.x) stages += locate(item).stages;
+        for (uint32_t j = 0; j <= stages; ++j) {
+            if (lanes != 0) wait_loads_and_sync<(S - 2) * kLoads>();
+            else wait_loads_and_sync<0>();
+            load_stage(far);
+            next_stage();
+            far = far == (S - 1) * kStage ? 0 : far + kStage;
+        }
+        return;
+    }
 
     // ---- LDS -> fragments
     const uint32_t r = lane & 31u, h = lane >> 5;
@@ -178,11 +202,11 @@ void mx4_gemm_kernel(Mx4TileArgs ta) {
         else sa[s][I - TN] = *reinterpret_cast<const uint32_t *>(lds + at + sa_at + 256 * (I - TN));
     };
     constexpr int kReads = TM + TN, kProducts = TM * TN;
-    uint32_t cur = 0, far = (S - 1) * kStage;  // the stage that is read, the one that is asked for
+    uint32_t cur = 0;                          // the stage that is read
     // The products of step s, and beside them the reads of the next step; after a stage's last one of the next stage, with its scales, and the loads of the stage that is asked for.
     auto multiply = [&](auto step) {
         constexpr uint32_t s = decltype(step)::value, N = (s + 1) % 4;
-        constexpr int kR = s == 3 ? 2 * kReads : kReads, kL = s == 3 ? kLoads : 0;
+        constexpr int kR = s == 3 ? 2 * kReads : kReads, kL = s == 3 && LOADERS == 0 ? kLoads : 0;
         const From from = kL > 0 ? from_now() : From{};
         for_constants<kProducts>([&](auto product) {
             constexpr int P = decltype(product)::value, i = P / TN, j = P % TN;
@@ -203,24 +227,29 @@ void mx4_gemm_kernel(Mx4TileArgs ta) {
     uint32_t behind = 0;                       // so many stages yet that were asked for before the last stores
     auto wait_for_next = [&]() {
         constexpr int kLater = (S - 2) * kLoads;
-        if (lanes == 0) wait_loads_and_sync<0>();
+        if (LOADERS > 0) sync_lds();
+        else if (lanes == 0) wait_loads_and_sync<0>();
         else if (behind > 0) wait_loads_and_sync<(kLater + kStores < 63 ? kLater + kStores : 63)>();
         else wait_loads_and_sync<kLater>();
         behind -= behind > 0 ? 1 : 0;
         cur = cur == (S - 1) * kStage ? 0 : cur + kStage;
-        far = far == (S - 1) * kStage ? 0 : far + kStage;
+        if (LOADERS == 0) far = far == (S - 1) * kStage ? 0 : far + kStage;
     };
 
-    ask_for(ask_item);
+    if constexpr (LOADERS > 0) {
+        sync_lds();
+    } else {
+        ask_for(ask_item);
 #pragma unroll
-    for (uint32_t i = 0; i < S - 1; ++i) {
-        load_stage(i * kStage);
+        for (uint32_t i = 0; i < S - 1; ++i) {
+            load_stage(i * kStage);
+            next_stage();
+        }
+        if (lanes != 0) wait_loads_and_sync<(S - 2) * kLoads>();
+        else wait_loads_and_sync<0>();
+        load_stage(far);
         next_stage();
     }
-    if (lanes != 0) wait_loads_and_sync<(S - 2) * kLoads>();
-    else wait_loads_and_sync<0>();
-    load_stage(far);
-    next_stage();
     for_constants<kReads>([&](auto i) {
         read_one(0, UintTag<0>{}, i);
         read_scale(0, i, UintTag<0>{});
@@ -239,7 +268,7 @@ void mx4_gemm_kernel(Mx4TileArgs ta) {
             multiply(UintTag<2>{});
             wait_for_next();
             multiply(UintTag<3>{});
-            next_stage();
+            if (LOADERS == 0) next_stage();
 #pragma unroll
             for (int i = 0; i < TM; ++i) sa[0][i] = sa[1][i];
 #pragma unroll
@@ -304,7 +333,7 @@ void mx4_gemm_kernel(Mx4TileArgs ta) {
                         const u32x4 w = *reinterpret_cast<const u32x4 *>(corner + (kRows * k + s_row) * kPitch + 4 * (lane % kLanes) * 4);
                         const uint32_t m = p.m0 + 32 * (TM * wm + i) + kPass * pass + kRows * k + s_row;
                         typename Out::type *to = c + m * ldc + n;
-                        if (stored) {
+                        if (stored || (m < g.M && n + kRun <= g.N)) {
                             __builtin_memcpy(to, &w, 16);
                         } else if (m < g.M) {
 #pragma unroll
@@ -349,24 +378,51 @@ __global__ __launch_bounds__(256) void mx4_join_kernel(Mx4GemmArgs g, uint32_t s
     store_run<T, 4>(static_cast<typename T::type *>(g.c) + m * g.ldc + n, v, left);
 }
 
+// Which tile a product takes, and into how many parts its contraction is cut, by an estimate of the time in us: `base` is a launch; `alone` a stage of workgroups that nothing else slows down,
+// `resident` of them on a compute unit; `busy` what a stage costs per workgroup of a unit where all units have some (of the last workgroups' unevenness over the units `uneven` counts); `store` the
+// stores of 256 tiles.  Fitted to 170 sizes (100 for the largest tile) of 33 .. 16384 x 64 .. 8192 x 64 .. 8192, bf16 results: 6 - 11 % (standard deviation).  On these the chosen tile takes
+// 1.2 % longer than the best one on average, at worst 18 % (7231 x 309 x 7868).  16384 x 8192 x 8192: 256 x 256 545 us, 128 x 128 604, 128 x 64 836; 8192 x 4096 x 1024: 32, 28, 35;
+// 1003 x 971 x 243: 13, 5.6, 4.5, 64 x 64 4.1.
+// Cutting the contraction costs a second launch, 3.2 us, and the parts' way through memory; it is worth that for few tiles of a long one (456 x 92 x 5377: 9.8 -> 8.6 us in four parts).
+struct Mx4Tile {
+    uint32_t bm, bn, resident;
+    double base, alone, busy, uneven, store;
+};
+static constexpr Mx4Tile kMx4Tiles[] = {
+    {256, 256, 1, 3.0, 1.118, 1.831, 0.593, 12.4}, {128, 128, 2, 3.6, 0.425, 0.586, 0.729, 1.147}, {128, 64, 2, 3.0, 0.48, 0.378, 1.0, 0.774}, {64, 64, 2, 3.0, 0.278, 0.231, 1.0, 0.52},
+};
 struct Mx4Choice {
     int tile;
-    uint32_t bm, bn, splits;
+    uint32_t splits;
 };
 static Mx4Choice choose(uint32_t M, uint32_t N, uint32_t K) {
     const uint32_t stages = (K + 255) / 256;
-    const uint32_t sizes[5][2] = {{256, 256}, {256, 128}, {128, 128}, {128, 64}, {64, 64}};
-    Mx4Choice c{4, 64, 64, 1};
-    for (int i = 0; i < 5; ++i) {
-        c = Mx4Choice{i, sizes[i][0], sizes[i][1], 1};
-        if (static_cast<uint64_t>((M + c.bm - 1) / c.bm) * ((N + c.bn - 1) / c.bn) >= 256) return c;
+    Mx4Choice best{-1, 1};
+    double best_cost = 0.0;
+    for (int i = 0; i < 4; ++i) {
+        const Mx4Tile &t = kMx4Tiles[i];
+        const uint64_t tiles = static_cast<uint64_t>((M + t.bm - 1) / t.bm) * ((N + t.bn - 1) / t.bn);
+        for (uint32_t splits = 1; splits <= 16; splits *= 2) {
+            if (splits > 1 && (tiles * splits > 256 || splits > stages)) break;
+            const uint64_t items = tiles * splits, units = (items + 255) / 256, rounds = (items + 256 * t.resident - 1) / (256 * t.resident);
+            const double per_unit = static_cast<double>(items) / 256.0, steps = (stages + splits - 1) / splits;
+            const double alone = t.alone * steps * static_cast<double>(rounds), busy = t.busy * steps * (per_unit + t.uneven * (static_cast<double>(units) - per_unit));
+            double cost = t.base + (alone > busy ? alone : busy) + t.store * (per_unit > 1.0 ? per_unit : 1.0);
+            if (splits > 1) cost += 3.2 + 2e-6 * splits * M * N;   // (8 bytes of a part at 4 TB/s)
+            if (best.tile < 0 || cost < best_cost) {
+                best = Mx4Choice{i, splits};
+                best_cost = cost;
+            }
+        }
     }
-    const uint32_t tiles = ((M + 63) / 64) * ((N + 63) / 64);
-    uint32_t splits = 256 / tiles;
-    if (splits > stages / 4) splits = stages / 4;
-    if (splits > 8) splits = 8;
-    c.splits = splits < 1 ? 1 : splits;
-    return c;
+    const uint32_t each = (stages + best.splits - 1) / best.splits;
+    best.splits = (stages + each - 1) / each;
+    return best;
+}
+// Host only, not part of the interface: the tile's index, and 16 times the parts, that a product takes.
+extern "C" int omc_internal_mx4_tile(uint32_t M, uint32_t N, uint32_t K) {
+    const Mx4Choice c = choose(M, N, K);
+    return c.tile + 16 * static_cast<int>(c.splits);
 }
 
 size_t mx4_gemm_workspace(uint32_t M, uint32_t N, uint32_t K) {
@@ -374,34 +430,31 @@ size_t mx4_gemm_workspace(uint32_t M, uint32_t N, uint32_t K) {
     return c.splits > 1 ? 4ull * c.splits * M * N : 0;
 }
 
-template <int WM, int WN, int TM, int TN, int S, int OCC, typename T>
+template <int WM, int WN, int TM, int TN, int LOADERS, int S, int OCC, typename T>
 static void launch_tile(const Mx4TileArgs &ta, hipStream_t st) {
-    constexpr uint32_t kLds = 32 * (TM * WM + TN * WN) * S * 136 + WM * WN * kCorner, kByLds = 163840 / kLds, kByWaves = 4 * OCC / (WM * WN);
+    constexpr uint32_t kLds = 32 * (TM * WM + TN * WN) * S * 136 + WM * WN * kCorner, kByLds = 163840 / kLds, kByWaves = 4 * OCC / (WM * WN + LOADERS);
     const uint32_t items = ta.tiles_m * ta.tiles_n * ta.splits, most = 256 * (kByLds < kByWaves ? kByLds : kByWaves);
-    const dim3 grid(items < most ? items : most), block(64 * WM * WN);
-    if (ta.splits > 1) mx4_gemm_kernel<WM, WN, TM, TN, S, OCC, T, true><<<grid, block, 0, st>>>(ta);
-    else mx4_gemm_kernel<WM, WN, TM, TN, S, OCC, T, false><<<grid, block, 0, st>>>(ta);
+    const dim3 grid(items < most ? items : most), block(64 * (WM * WN + LOADERS));
+    if (ta.splits > 1) mx4_gemm_kernel<WM, WN, TM, TN, LOADERS, S, OCC, T, true><<<grid, block, 0, st>>>(ta);
+    else mx4_gemm_kernel<WM, WN, TM, TN, LOADERS, S, OCC, T, false><<<grid, block, 0, st>>>(ta);
 }
 
 template <typename T>
 static int launch(const Mx4GemmArgs &ga, hipStream_t st) {
-    Mx4Choice c = choose(ga.M, ga.N, ga.K);
-#ifdef OMC_FORCE
-    c = OMC_FORCE;
-#endif
-    const uint32_t stages = (ga.K + 255) / 256, each = (stages + c.splits - 1) / c.splits, splits = (stages + each - 1) / each;
-    const Mx4TileArgs ta{ga, (ga.M + c.bm - 1) / c.bm, (ga.N + c.bn - 1) / c.bn, splits, each};
+    const Mx4Choice c = choose(ga.M, ga.N, ga.K);
+    const Mx4Tile &t = kMx4Tiles[c.tile];
+    const uint32_t stages = (ga.K + 255) / 256;
+    const Mx4TileArgs ta{ga, (ga.M + t.bm - 1) / t.bm, (ga.N + t.bn - 1) / t.bn, c.splits, (stages + c.splits - 1) / c.splits};
     switch (c.tile) {
-        case 0: launch_tile<2, 2, 4, 4, 2, 1, T>(ta, st); break;
-        case 1: launch_tile<4, 2, 2, 2, 2, 2, T>(ta, st); break;
-        case 2: launch_tile<2, 2, 2, 2, 2, 2, T>(ta, st); break;
-        case 3: launch_tile<2, 2, 2, 1, 2, 2, T>(ta, st); break;
-        default: launch_tile<2, 2, 1, 1, 4, 2, T>(ta, st); break;
+        case 0: launch_tile<2, 2, 4, 4, 0, 2, 1, T>(ta, st); break;
+        case 1: launch_tile<2, 2, 2, 2, 4, 2, 4, T>(ta, st); break;
+        case 2: launch_tile<2, 2, 2, 1, 0, 2, 2, T>(ta, st); break;
+        default: launch_tile<2, 2, 1, 1, 0, 4, 2, T>(ta, st); break;
     }
-    if (splits > 1) {
+    if (c.splits > 1) {
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return static_cast<int>(e);
-        mx4_join_kernel<T><<<dim3((ga.N + 255) / 256, (ga.M + 3) / 4), dim3(256), 0, st>>>(ga, splits);
+        mx4_join_kernel<T><<<dim3((ga.N + 255) / 256, (ga.M + 3) / 4), dim3(256), 0, st>>>(ga, c.splits);
     }
     return static_cast<int>(hipGetLastError());
 }

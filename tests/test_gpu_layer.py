@@ -459,3 +459,54 @@ def test_offsets_past_32_bits():
         a = ref.quantize(ref.as64(f))[2]
         check(y[:, -70:], a @ w.T, ref.product_bound(a, w, cols), F32)
         assert (y[:, :-70] == 0).all()
+
+
+def values_on_device(codes, scales, rows, cols):
+    """fp64 values of codes and scales that lie on the device."""
+    c = codes.view(rows, -1)
+    k = torch.stack((c & 15, c >> 4), -1).view(rows, -1).long()
+    grid = torch.tensor(np.concatenate((ref.GRID, -ref.GRID)), device="cuda")
+    unit = torch.exp2(scales.view(rows, -1).double() - 127.0).repeat_interleave(32, 1)
+    return (grid[k] * unit)[:, :cols]
+
+
+# Every tile, with fewer and with more of them than the chip holds at a time, whole and odd numbers of 128s, and contractions in parts: (tile, cut, several in turn).
+PRODUCTS = [((0, False, False), (7242, 1702, 3983)), ((0, False, False), (2213, 5436, 3864)), ((0, False, True), (7859, 3827, 3283)), ((0, False, True), (3814, 7658, 3103)),
+            ((1, False, False), (1069, 4825, 131)), ((1, False, False), (653, 7529, 33)), ((1, False, True), (2457, 3302, 130)), ((1, False, True), (4624, 1681, 34)),
+            ((1, True, False), (70, 8513, 8934)), ((1, True, False), (69, 8432, 8525)), ((1, True, False), (512, 512, 65536)),
+            ((2, False, False), (8366, 138, 132)), ((2, False, False), (8356, 131, 33)), ((2, False, True), (406, 8690, 133)), ((2, False, True), (531, 6706, 33)),
+            ((3, False, False), (36, 34, 129)), ((3, False, True), (257, 6724, 461)), ((3, False, True), (282, 6605, 289)), ((3, True, False), (34, 37, 3758)), ((3, True, False), (33, 35, 3698))]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("kind,shape", PRODUCTS)
+def test_every_tile(kind, shape, dtype):
+    M, N, K = shape
+    assert ref.product_tile(M, N, K) == kind
+    a, b = [[torch.from_numpy(x.reshape(-1)).cuda() for x in random_codes(rows, K, rows + K)] for rows in (M, N)]
+    bias = torch.randn(N, device="cuda", generator=torch.Generator("cuda").manual_seed(1))
+    cw, c = empty(M, N, dtype, 3)
+    whole, ws = workspace(omc.omc_mx4_gemm_workspace_bytes(M, N, K))
+    omc.omc_mx4_gemm(*a, *b, bias, c, K, ws)
+    av, bv = values_on_device(*a, M, K), values_on_device(*b, N, K)
+    want, bound = av @ bv.t() + bias.double(), ref.product_bound_of(av.abs() @ bv.abs().t(), K) + 2.0 ** -23 * bias.abs().double()
+    limit = bound + (want.abs() + bound) * (2.0 ** -8 if dtype is BF16 else 2.0 ** -23)
+    assert ((c.double() - want).abs() <= limit).all()
+    untouched(cw, N)
+    guarded(whole, ws)
+
+
+def random_codes(rows, cols, seed):
+    return random_mx4(rows, cols, seed)[:2] if rows * cols < 1 << 22 else quick_mx4(rows, cols, seed)
+
+
+def quick_mx4(rows, cols, seed):
+    """random_mx4 without its values."""
+    rng = np.random.default_rng(seed)
+    wide, blocks = ref.padded(cols), -(-cols // 32)
+    codes = rng.integers(0, 256, (rows, wide // 2), dtype=np.uint8)
+    scales = rng.integers(110, 140, (rows, wide // 32), dtype=np.uint8)
+    k = np.arange(wide)
+    codes &= ((k[0::2] < cols) * 15 + (k[1::2] < cols) * 240).astype(np.uint8)
+    scales[:, blocks:] = 0
+    return codes, scales
