@@ -38,10 +38,13 @@ struct QuantArgs {
     uint64_t ldv;
     float *colsum;                 // partial sums of the columns, one row of them for every 256 rows of x; may be null
     bool images;                   // scales and scales_t in the tiles' order
-    Mx4Reorder also;               // another matrix' scales, by the same launch
+    Mx4Reorder also;               // another matrix' scales, by the same launch (along rows only; see launch_mx4_tiles)
 };
+// Several matrices in one launch, in any directions but without values, and another one's scales.
+constexpr uint32_t kMostJobs = 3;
+int launch_mx4_tiles(const QuantArgs *args, uint32_t count, const Mx4Reorder &also, bool bf16, void *stream);
 int launch_mx4_reorder(const Mx4Reorder &a, const Mx4Reorder &b, void *stream);
-int launch_mx4_quantize(const QuantArgs &qa, bool bf16, void *stream);
+int launch_mx4_quantize(const QuantArgs &qa, bool bf16, void *stream);   // no sums
 
 struct Mx4GemmArgs {
     Mx4 a, b;

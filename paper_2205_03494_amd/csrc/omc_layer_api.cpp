@@ -177,34 +177,39 @@ omc_status omc_mx4_linear_backward(const void *dY, uint64_t lddy, const void *X,
     if (!aligned(ws, 16)) return OMC_ERR_ALIGN;
     const bool bf16 = type == OMC_BF16;
 
-    // dY's rounding in one pass, unless its two products want their scales in different orders
+    // all roundings in one launch; dY's in one pass, unless its two products want their scales in different orders
     const bool dx_tiles = !few(M), dw_tiles = !few(K);
-    QuantArgs qa{dY, lddy, M, N, nullptr, nullptr, nullptr, nullptr, nullptr, 0, dbias ? l.sums : nullptr, dx_tiles, {}};
+    const Mx4Reorder weights = dX && dx_tiles ? Mx4Reorder{bytes(w_scales), l.w_image, K, N} : Mx4Reorder{};
+    QuantArgs jobs[kMostJobs];
+    uint32_t count = 1;
+    jobs[0] = QuantArgs{dY, lddy, M, N, nullptr, nullptr, nullptr, nullptr, nullptr, 0, dbias ? l.sums : nullptr, dx_tiles, {}};
     if (dX) {
-        qa.codes = l.dy;
-        qa.scales = l.dy_scales;
-        if (dx_tiles) qa.also = Mx4Reorder{bytes(w_scales), l.w_image, K, N};
+        jobs[0].codes = l.dy;
+        jobs[0].scales = l.dy_scales;
     }
-    int rc = 0;
-    if (dW && (!dX || dx_tiles == dw_tiles)) {
-        qa.codes_t = l.dy_t;
-        qa.scales_t = l.dy_t_scales;
-        qa.images = dw_tiles;
-    } else if (dW) {
-        const QuantArgs ta{dY, lddy, M, N, nullptr, nullptr, l.dy_t, l.dy_t_scales, nullptr, 0, nullptr, dw_tiles, {}};
-        rc = launch_mx4_quantize(ta, bf16, stream);
+    if (dW) {
+        QuantArgs &along_columns = !dX || dx_tiles == dw_tiles ? jobs[0] : jobs[count++];
+        if (&along_columns != jobs) along_columns = QuantArgs{dY, lddy, M, N, nullptr, nullptr, nullptr, nullptr, nullptr, 0, nullptr, dw_tiles, {}};
+        along_columns.codes_t = l.dy_t;
+        along_columns.scales_t = l.dy_t_scales;
+        along_columns.images = dw_tiles;
+        jobs[count++] = QuantArgs{X, ldx, M, K, nullptr, nullptr, l.x_t, l.x_t_scales, nullptr, 0, nullptr, dw_tiles, {}};
     }
-    if (rc == 0) rc = launch_mx4_quantize(qa, bf16, stream);
+    int rc;
+    if (!dW && !dbias) {
+        jobs[0].also = weights;
+        rc = launch_mx4_quantize(jobs[0], bf16, stream);
+    } else {
+        rc = launch_mx4_tiles(jobs, count, weights, bf16, stream);
+    }
     if (rc == 0 && dbias) rc = launch_column_sums(l.sums, (M + 255) / 256, N, N, dbias, nullptr, stream);
     if (rc == 0 && dX) {
         const Mx4GemmArgs ga{{l.dy, l.dy_scales}, {bytes(w_codes), dx_tiles ? l.w_image : bytes(w_scales)}, nullptr, dX, lddx, M, K, N, l.parts};
         rc = launch_product(ga, dx_type == OMC_BF16, stream);
     }
     if (rc == 0 && dW) {
-        const QuantArgs xa{X, ldx, M, K, nullptr, nullptr, l.x_t, l.x_t_scales, nullptr, 0, nullptr, dw_tiles, {}};
-        rc = launch_mx4_quantize(xa, bf16, stream);
         const Mx4GemmArgs ga{{l.x_t, l.x_t_scales}, {l.dy_t, l.dy_t_scales}, nullptr, dW, N, K, N, M, l.parts};
-        if (rc == 0) rc = launch_product(ga, false, stream);
+        rc = launch_product(ga, false, stream);
     }
     return from_hip(rc);
 }

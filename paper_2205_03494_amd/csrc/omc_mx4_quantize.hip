@@ -6,6 +6,8 @@
 // Along columns a wave takes 32 rows x 128 columns, a lane two columns of them, so that a lane holds two whole blocks and no lane needs another's
 // values; the codes of a workgroup's 256 rows go through LDS, so that 128 bytes of a column are written together.  Where both directions are asked for, 16 lanes compare
 // their largest magnitudes of a row, from the same registers.
+#include <type_traits>
+
 #include "omc_mx4.h"
 
 namespace omc {
@@ -145,58 +147,114 @@ __device__ __forceinline__ void quantize_columns(const uint32_t (&lo)[32], const
     }
 }
 
-// Largest of 16 lanes' values, in all of them.
-template <typename M>
-__device__ __forceinline__ uint32_t largest_of_16(uint32_t x, M &&larger) {
-    x = larger(x, static_cast<uint32_t>(__builtin_amdgcn_mov_dpp(static_cast<int>(x), 0xb1, 0xf, 0xf, true)));    // lanes 1 0 3 2
-    x = larger(x, static_cast<uint32_t>(__builtin_amdgcn_mov_dpp(static_cast<int>(x), 0x4e, 0xf, 0xf, true)));    // lanes 2 3 0 1
-    x = larger(x, static_cast<uint32_t>(__builtin_amdgcn_mov_dpp(static_cast<int>(x), 0x141, 0xf, 0xf, true)));   // eight lanes mirrored
-    return larger(x, static_cast<uint32_t>(__builtin_amdgcn_mov_dpp(static_cast<int>(x), 0x140, 0xf, 0xf, true)));   // sixteen lanes mirrored
+// Largest magnitudes of 16 lanes' columns, two rows (halves) in each of 16 registers: lane l of the 16 gets those of rows 2 l and 2 l + 1.  Every exchange halves the registers: a lane keeps the
+// half that its bit of the lane number names, and its partner, which has the same bits above that one, gets the other.
+__device__ __forceinline__ uint32_t largest_of_16(uint32_t (&x)[16], uint32_t lane) {
+    auto exchange = [&](auto count, auto control, uint32_t bit) {
+        constexpr int N = decltype(count)::value;
+        const bool upper = (lane & bit) != 0;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const uint32_t keep = upper ? x[i + N] : x[i], give = upper ? x[i] : x[i + N];
+            const uint32_t got = static_cast<uint32_t>(__builtin_amdgcn_mov_dpp(static_cast<int>(give), decltype(control)::value, 0xf, 0xf, true));
+            x[i] = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, keep), __builtin_bit_cast(u16x2, got)));
+        }
+    };
+    typedef std::integral_constant<int, 0x140> Mirror16;     // lane ^ 15
+    typedef std::integral_constant<int, 0x141> Mirror8;      // lane ^ 7
+    typedef std::integral_constant<int, 0x1b> Mirror4;       // lane ^ 3
+    typedef std::integral_constant<int, 0xb1> Mirror2;       // lane ^ 1
+    exchange(std::integral_constant<int, 8>{}, Mirror16{}, 8u);
+    exchange(std::integral_constant<int, 4>{}, Mirror8{}, 4u);
+    exchange(std::integral_constant<int, 2>{}, Mirror4{}, 2u);
+    exchange(std::integral_constant<int, 1>{}, Mirror2{}, 1u);
+    return x[0];
 }
 
-// The same registers along the rows, of which 16 lanes hold a block: a lane's two codes of row i go to codes[i * 64 + lane], the scale of row i and block b to scales[i * 4 + b].
-template <typename T>
-__device__ __forceinline__ void quantize_rows(const uint32_t (&lo)[32], const uint32_t (&hi)[32], uint8_t *codes, uint8_t *scales, uint32_t lane) {
-    auto one = [&](uint32_t i, uint32_t top) {
-        const uint32_t byte = mx4_scale<T>(top);
-        const float unit = mx4_unit(byte);
-        uint32_t c;
-        if constexpr (T::kBytes == 4) c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, __uint_as_float(lo[i]), __uint_as_float(hi[i]), unit, 0);
-        else c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(0u, __builtin_bit_cast(bf16x2, lo[i]), unit, 0);
-        codes[i * 64 + lane] = static_cast<uint8_t>(byte == kMx4NaN ? 0u : c);
-        if ((lane & 15u) == 0) scales[i * 4 + (lane >> 4)] = static_cast<uint8_t>(byte);
-    };
-    if constexpr (T::kBytes == 4) {
-#pragma unroll
-        for (uint32_t i = 0; i < 32; ++i) one(i, largest_of_16(max(lo[i] & 0x7fffffffu, hi[i] & 0x7fffffffu), [](uint32_t x, uint32_t y) { return max(x, y); }));
-    } else {
-        auto larger = [](uint32_t x, uint32_t y) { return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, x), __builtin_bit_cast(u16x2, y))); };
-#pragma unroll
-        for (uint32_t i = 0; i < 32; i += 2) {   // two rows' largest in a register
-            const uint32_t x = lo[i] & 0x7fff7fffu, y = lo[i + 1] & 0x7fff7fffu;
-            const uint32_t top = largest_of_16(larger(__builtin_amdgcn_perm(y, x, 0x05040100u), __builtin_amdgcn_perm(y, x, 0x07060302u)), larger);
-            one(i, top & 0xffffu);
-            one(i + 1, top >> 16);
-        }
+template <int J>
+__device__ __forceinline__ uint32_t of_lane(uint32_t x) {   // lane J's of the 16
+    return static_cast<uint32_t>(__builtin_amdgcn_mov_dpp(static_cast<int>(x), 0x150 + J, 0xf, 0xf, true));
+}
+template <int FROM, int TO, typename F>
+__device__ __forceinline__ void for_each(F &&f) {
+    if constexpr (FROM < TO) {
+        f(std::integral_constant<int, FROM>{});
+        for_each<FROM + 1, TO>(f);
     }
 }
+
+// The same registers along the rows, of which 16 lanes hold a block.  A lane's codes, two columns of four rows a dword, go to codes[(row / 4) * 64 + lane], the scale of row i and block b to
+// scales[i * 4 + b].  (Of fp32 values the upper halves do for the largest magnitude: its exponent is all that is asked for.)
+template <typename T>
+__device__ __forceinline__ void quantize_rows(const uint32_t (&lo)[32], const uint32_t (&hi)[32], uint32_t *codes, uint8_t *scales, uint32_t lane) {
+    uint32_t tops[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        uint32_t x, y;                         // rows 2 i and 2 i + 1 of either column
+        if constexpr (T::kBytes == 4) {
+            x = __builtin_amdgcn_perm(lo[2 * i + 1], lo[2 * i], 0x07060302u);
+            y = __builtin_amdgcn_perm(hi[2 * i + 1], hi[2 * i], 0x07060302u);
+        } else {
+            x = __builtin_amdgcn_perm(lo[2 * i + 1], lo[2 * i], 0x05040100u);
+            y = __builtin_amdgcn_perm(lo[2 * i + 1], lo[2 * i], 0x07060302u);
+        }
+        tops[i] = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, x & 0x7fff7fffu), __builtin_bit_cast(u16x2, y & 0x7fff7fffu)));
+    }
+    const uint32_t mine = largest_of_16(tops, lane);
+    const uint32_t first = mx4_scale<BF16>(mine & 0xffffu), second = mx4_scale<BF16>(mine >> 16);
+    scales[8 * (lane & 15u) + (lane >> 4)] = static_cast<uint8_t>(first);
+    scales[8 * (lane & 15u) + 4 + (lane >> 4)] = static_cast<uint8_t>(second);
+    const uint32_t both = second << 23 | first;
+    const bool any_nan = __any(first == kMx4NaN || second == kMx4NaN);
+    for_each<0, 8>([&](auto four) {            // of four rows
+        constexpr int G = decltype(four)::value;
+        uint32_t c = 0;
+        for_each<0, 4>([&](auto in) {
+            constexpr int J = decltype(in)::value, I = 4 * G + J;
+            const uint32_t scale = of_lane<I / 2>(both);
+            const float unit = __uint_as_float(I % 2 == 0 ? scale << 23 : scale & 0xff800000u);
+            if constexpr (T::kBytes == 4) c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, __uint_as_float(lo[I]), __uint_as_float(hi[I]), unit, J);
+            else c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, lo[I]), unit, J);
+            if (any_nan && __float_as_uint(unit) == kMx4NaN << 23) c &= ~(0xffu << (8 * J));
+        });
+        codes[64 * G + lane] = c;
+    });
+}
+
+// Several matrices' tiles in one launch, then another one's scales.
+struct TileJobs {
+    QuantArgs job[kMostJobs];
+    uint32_t tiles_c[kMostJobs], end[kMostJobs];   // tiles across; the job's workgroups end here
+    Mx4Reorder also;
+};
 
 // Tiles of 256 x 128: blocks along the columns, along the rows, the columns' sums.
 template <typename T>
-__global__ __launch_bounds__(512) void mx4_tiles_kernel(QuantArgs qa, uint32_t tiles_r, uint32_t tiles_c) {
+__global__ __launch_bounds__(512) void mx4_tiles_kernel(TileJobs jobs) {
     typedef typename T::type E;
     constexpr uint32_t kPitch = 144;           // bytes of a column's codes in LDS, 128 and padding
     __shared__ __attribute__((aligned(16))) uint8_t codes_lds[kWide * kPitch];
-    __shared__ __attribute__((aligned(16))) uint8_t rows_lds[8][32 * 64];
+    __shared__ __attribute__((aligned(16))) uint32_t rows_lds[8][8 * 64];
     __shared__ __attribute__((aligned(16))) uint8_t scales_lds[kWide * 8];
     __shared__ __attribute__((aligned(16))) uint8_t row_scales_lds[8][32 * 4];
     __shared__ float sums_lds[8][kWide];
-    if (qa.also.image && blockIdx.x >= tiles_r * tiles_c) {
-        reorder_scales(qa.also, blockIdx.x - tiles_r * tiles_c);
+    uint32_t begin = 0, which = 0;
+#pragma unroll
+    for (uint32_t j = 0; j < kMostJobs; ++j)
+        if (blockIdx.x >= jobs.end[j]) {
+            begin = jobs.end[j];
+            which = j + 1;
+        }
+    if (which == kMostJobs) {
+        reorder_scales(jobs.also, blockIdx.x - begin);
         return;
     }
+    const QuantArgs &qa = jobs.job[which];
+    const uint32_t tiles_c = jobs.tiles_c[which], total = jobs.end[which] - begin, block = blockIdx.x - begin;
     const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const uint32_t tr = blockIdx.x / tiles_c, tc = blockIdx.x % tiles_c;
+    // a run of the tiles to every die: 64 bytes of a row's codes are half a cache line, whose other half the next tile has (4096 x 4095 along columns 9.5 us, dealt out one by one 10.9)
+    const uint32_t q = total / 8, rest = total % 8, die = block % 8, id = die * q + min(die, rest) + block / 8;
+    const uint32_t tr = id / tiles_c, tc = id % tiles_c;
     const uint32_t r0 = tr * kHigh + 32 * wave, c0 = tc * kWide, col = c0 + 2 * lane;
     const uint32_t height = r0 < qa.rows ? min(32u, qa.rows - r0) : 0u;
     const E *x = static_cast<const E *>(qa.x);
@@ -278,8 +336,15 @@ __global__ __launch_bounds__(512) void mx4_tiles_kernel(QuantArgs qa, uint32_t t
         const uint32_t pitch = mx4_padded(qa.cols) / 2;
 #pragma unroll
         for (uint32_t k = 0; k < 2; ++k) {
-            const uint32_t i = 16 * k + lane / 4, at = 16 * (lane % 4);
-            if (i < height) *reinterpret_cast<u32x4 *>(qa.codes + static_cast<uint64_t>(r0 + i) * pitch + 64 * tc + at) = *reinterpret_cast<const u32x4 *>(rows_lds[wave] + 64 * i + at);
+            const uint32_t group = 4 * k + (lane >> 4), at = 4 * (lane & 15u);   // four lanes' codes of four rows, to four rows' of eight columns
+            const u32x4 d = *reinterpret_cast<const u32x4 *>(rows_lds[wave] + 64 * group + at);
+            const uint32_t x0 = __builtin_amdgcn_perm(d[1], d[0], 0x05010400u), x1 = __builtin_amdgcn_perm(d[3], d[2], 0x05010400u);
+            const uint32_t x2 = __builtin_amdgcn_perm(d[1], d[0], 0x07030602u), x3 = __builtin_amdgcn_perm(d[3], d[2], 0x07030602u);
+            const uint32_t row[4] = {__builtin_amdgcn_perm(x1, x0, 0x05040100u), __builtin_amdgcn_perm(x1, x0, 0x07060302u), __builtin_amdgcn_perm(x3, x2, 0x05040100u),
+                                     __builtin_amdgcn_perm(x3, x2, 0x07060302u)};
+#pragma unroll
+            for (uint32_t j = 0; j < 4; ++j)
+                if (4 * group + j < height) *reinterpret_cast<uint32_t *>(qa.codes + static_cast<uint64_t>(r0 + 4 * group + j) * pitch + 64 * tc + at) = row[j];
         }
         if (lane < height) {
             const uint32_t bytes = reinterpret_cast<const uint32_t *>(row_scales_lds[wave])[lane];
@@ -305,15 +370,33 @@ __global__ __launch_bounds__(512) void mx4_tiles_kernel(QuantArgs qa, uint32_t t
 }
 
 template <typename T>
+static int launch_tiles(const QuantArgs *args, uint32_t count, const Mx4Reorder &also, hipStream_t st) {
+    TileJobs jobs{};
+    uint32_t end = 0;
+    for (uint32_t j = 0; j < kMostJobs; ++j) {
+        if (j < count) {
+            jobs.job[j] = args[j];
+            jobs.tiles_c[j] = (args[j].cols + kWide - 1) / kWide;
+            end += (args[j].rows + kHigh - 1) / kHigh * jobs.tiles_c[j];
+        }
+        jobs.end[j] = end;
+    }
+    jobs.also = also;
+    mx4_tiles_kernel<T><<<dim3(end + reorder_blocks(also)), dim3(512), 0, st>>>(jobs);
+    return static_cast<int>(hipGetLastError());
+}
+int launch_mx4_tiles(const QuantArgs *args, uint32_t count, const Mx4Reorder &also, bool bf16, void *stream) {
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    return bf16 ? launch_tiles<BF16>(args, count, also, st) : launch_tiles<F32>(args, count, also, st);
+}
+
+template <typename T>
 static int launch(QuantArgs qa, hipStream_t st) {
-    if (qa.codes_t || qa.colsum) {
+    if (qa.codes_t) {
         QuantArgs ta = qa;
         if (qa.values) ta.codes = ta.scales = nullptr;   // these along the rows, with the values
-        const uint32_t tiles_r = (qa.rows + kHigh - 1) / kHigh, tiles_c = (qa.cols + kWide - 1) / kWide;
-        mx4_tiles_kernel<T><<<dim3(tiles_r * tiles_c + reorder_blocks(qa.also)), dim3(512), 0, st>>>(ta, tiles_r, tiles_c);
-        const hipError_t e = hipGetLastError();
-        if (e != hipSuccess || !qa.values) return static_cast<int>(e);
-        qa.also.image = nullptr;
+        const int rc = launch_tiles<T>(&ta, 1, Mx4Reorder{}, st);
+        if (rc != 0 || !qa.values) return rc;
     }
     const uint32_t eights = mx4_padded(qa.cols) / 8, most = (1u << 30) / eights;   // rows of one launch
     for (uint32_t first = 0; first < qa.rows; first += most) {

@@ -462,39 +462,44 @@ def omc_aggregate_mean(agg: AggregatePlan, arenas: Sequence[torch.Tensor], sb_ta
 # --------------------------------------------------------------------------- a linear layer in 4-bit microscaled floats, and layer norm
 OMC_F32, OMC_BF16 = 0, 1
 _TYPES = {torch.float32: OMC_F32, torch.bfloat16: OMC_BF16}
+_float32, _uint8 = torch.float32, torch.uint8
 
 
 def _matrix(t: torch.Tensor):
     """(pointer, type, row stride) of a device matrix whose rows are contiguous."""
-    if not t.is_cuda or t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1):
+    shape, strides, kind = t.shape, t.stride(), _TYPES.get(t.dtype)
+    if len(shape) != 2 or not t.is_cuda or (strides[1] != 1 and shape[1] > 1):
         raise ValueError("a device matrix with contiguous rows is expected")
-    kind = _TYPES.get(t.dtype)
     if kind is None:
         raise ValueError(f"fp32 or bfloat16 is expected, not {t.dtype}")
-    rows, cols = t.shape
-    return t.data_ptr(), kind, t.stride(0) if rows > 1 else cols
+    return t.data_ptr(), kind, strides[0] if shape[0] > 1 else shape[1]
 
 
 def _rows_like(t: torch.Tensor, rows: int, cols: int):
-    if t.shape[0] != rows or t.shape[1] != cols:
+    if t.shape != (rows, cols):
         raise ValueError(f"{rows} x {cols} is expected, not {tuple(t.shape)}")
     return _matrix(t)
 
 
+def _array(t: Optional[torch.Tensor], n: int, dtype):
+    """Pointer of a contiguous device tensor of n elements; None for None."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.numel() != n or not t.is_cuda or not t.is_contiguous():
+        raise ValueError(f"a contiguous device tensor of {n} {dtype} is expected")
+    return t.data_ptr()
+
+
 def _floats(t: Optional[torch.Tensor], n: int):
-    if t is None:
-        return None
-    if t.dtype != torch.float32 or t.numel() != n:
-        raise ValueError(f"{n} fp32 values are expected")
-    return _ptr(t)
+    return None if t is None else _array(t, n, _float32)
 
 
-def _bytes(t: Optional[torch.Tensor], n: int):
-    if t is None:
-        return None
-    if t.dtype != torch.uint8 or t.numel() != n:
-        raise ValueError(f"{n} bytes are expected")
-    return _ptr(t)
+def _codes(t: Optional[torch.Tensor], rows: int, cols: int):
+    return None if t is None else _array(t, rows * ((cols + 127) // 128) * 64, _uint8)
+
+
+def _scales(t: Optional[torch.Tensor], rows: int, cols: int):
+    return None if t is None else _array(t, rows * ((cols + 127) // 128) * 4, _uint8)
 
 
 def _space(ws: Optional[torch.Tensor]):
@@ -535,8 +540,8 @@ def omc_mx4_quantize(x: torch.Tensor, codes: Optional[torch.Tensor] = None, scal
     pv, vkind, ldv = (None, kind, 0) if values is None else _rows_like(values, rows, cols)
     if vkind != kind:
         raise ValueError("values have x's type")
-    _check(_mx4_quantize(px, kind, rows, cols, ldx, _bytes(codes, _mx4_codes(rows, cols)), _bytes(scales, _mx4_scales(rows, cols)),
-                         _bytes(codes_t, _mx4_codes(cols, rows)), _bytes(scales_t, _mx4_scales(cols, rows)), pv, ldv,
+    _check(_mx4_quantize(px, kind, rows, cols, ldx, _codes(codes, rows, cols), _scales(scales, rows, cols),
+                         _codes(codes_t, cols, rows), _scales(scales_t, cols, rows), pv, ldv,
                          _stream(stream)), "omc_mx4_quantize")
 
 
@@ -545,8 +550,8 @@ def omc_mx4_gemm(a_codes: torch.Tensor, a_scales: torch.Tensor, b_codes: torch.T
     """Cout [M, N] in fp32 or bf16 = A [M x K] B [N x K]^T + bias."""
     M, N = Cout.shape
     pc, kind, ldc = _matrix(Cout)
-    _check(_mx4_gemm(_bytes(a_codes, _mx4_codes(M, K)), _bytes(a_scales, _mx4_scales(M, K)), _bytes(b_codes, _mx4_codes(N, K)),
-                     _bytes(b_scales, _mx4_scales(N, K)), _floats(bias, N), pc, kind, ldc, M, N, K, *_space(ws),
+    _check(_mx4_gemm(_codes(a_codes, M, K), _scales(a_scales, M, K), _codes(b_codes, N, K),
+                     _scales(b_scales, N, K), _floats(bias, N), pc, kind, ldc, M, N, K, *_space(ws),
                      _stream(stream)), "omc_mx4_gemm")
 
 
@@ -557,7 +562,7 @@ def omc_mx4_linear(X: torch.Tensor, w_codes: torch.Tensor, w_scales: torch.Tenso
     N = Y.shape[1]
     px, xkind, ldx = _matrix(X)
     py, ykind, ldy = _rows_like(Y, M, N)
-    _check(_mx4_linear(px, xkind, ldx, _bytes(w_codes, _mx4_codes(N, K)), _bytes(w_scales, _mx4_scales(N, K)), _floats(bias, N), py,
+    _check(_mx4_linear(px, xkind, ldx, _codes(w_codes, N, K), _scales(w_scales, N, K), _floats(bias, N), py,
                        ykind, ldy, M, N, K, *_space(ws), _stream(stream)), "omc_mx4_linear")
 
 
@@ -573,7 +578,7 @@ def omc_mx4_linear_backward(dY: torch.Tensor, X: Optional[torch.Tensor], w_codes
     if xkind != kind:
         raise ValueError("dY and X are of one type")
     pdx, dxkind, lddx = (None, kind, 0) if dX is None else _rows_like(dX, M, K)
-    _check(_mx4_backward(pdy, lddy, px, ldx, kind, _bytes(w_codes, _mx4_codes(K, N)), _bytes(w_scales, _mx4_scales(K, N)), pdx, dxkind,
+    _check(_mx4_backward(pdy, lddy, px, ldx, kind, _codes(w_codes, K, N), _scales(w_scales, K, N), pdx, dxkind,
                          lddx, _floats(dW, K * N), _floats(dbias, N), M, N, K, *_space(ws), _stream(stream)),
            "omc_mx4_linear_backward")
 
