@@ -1,0 +1,139 @@
+"""A Conformer's feed-forward module, x + 1/2 W2 swish(W1 norm(x)), trained and served on 4-bit products.
+
+Its variables live in one packed arena: the two matrices as codes with (s, b), the vectors in fp32 (Sec. 2.4).  A training
+iteration decompresses the set, rounds the matrices to MX4 in both directions, runs forward and backward on the matrix cores in
+4 bits, and hands the fp32 gradients to the decompress -> update -> recompress step (Sec. 2.1).  Run as a program it trains one module on
+a fixed batch and then answers single frames:
+
+    python -m paper_2205_03494_amd.feedforward --width 512 --inner 2048 --frames 1024 --steps 20
+"""
+from __future__ import annotations
+
+import math
+
+import torch
+
+from . import omc
+
+EPS = 1e-5
+
+
+class FeedForward:
+    """width -> inner -> width; `fmt` is the storage format of the matrices."""
+
+    def __init__(self, width: int, inner: int, fmt=None, seed: int = 0):
+        self.width, self.inner = width, inner
+        self.shapes = {"gamma": (width,), "beta": (width,), "w1": (width, inner), "b1": (inner,), "w2": (inner, width), "b2": (width,)}
+        fmt = fmt or omc.fmt(3, 7)
+        table, self.at, data, aux = [], {}, 0, 0
+        for name, shape in self.shapes.items():
+            n, matrix = math.prod(shape), len(shape) == 2
+            table.append(dict(data_offset=data, aux_offset=aux, n=n, fmt=fmt, quantized=matrix))
+            self.at[name] = aux
+            data += omc.omc_packed_bytes(fmt, n) if matrix else -(-4 * n // 16) * 16
+            aux += -(-n // 4) * 4
+        self.plan = omc.omc_plan_build(omc.make_var_table(table))
+        self.arena = torch.zeros(data, dtype=torch.uint8, device="cuda")
+        self.sb = torch.zeros((len(table), 2), device="cuda")
+        self.values, self.grads = torch.zeros(aux, device="cuda"), torch.zeros(aux, device="cuda")
+        self.states = []
+        self.step_ws = torch.empty(self.plan.workspace_bytes, dtype=torch.uint8, device="cuda")
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        for name, fan_in in (("w1", width), ("w2", inner)):
+            self.value(name).normal_(0.0, 1.0 / math.sqrt(fan_in), generator=g)
+        self.value("gamma").fill_(1.0)
+        omc.omc_compress_set(self.values, self.plan, self.arena, self.sb, self.step_ws)
+        self.mx4 = {}
+        for name in ("w1", "w2"):
+            r, c = self.shapes[name]
+            self.mx4[name] = [torch.empty(size(*s), dtype=torch.uint8, device="cuda") for s in ((r, c), (c, r))
+                              for size in (omc.omc_mx4_code_bytes, omc.omc_mx4_scale_bytes)]
+        self.ws = torch.empty(0, dtype=torch.uint8, device="cuda")
+        self.refresh()
+
+    def _view(self, flat: torch.Tensor, name: str) -> torch.Tensor:
+        shape = self.shapes[name]
+        return flat[self.at[name]:self.at[name] + math.prod(shape)].view(shape)
+
+    def value(self, name: str) -> torch.Tensor:
+        """The variable in fp32, as the last refresh decompressed it."""
+        return self._view(self.values, name)
+
+    def grad(self, name: str) -> torch.Tensor:
+        return self._view(self.grads, name)
+
+    def refresh(self) -> None:
+        """The set in fp32 and its matrices in MX4, K x N blocked along N (input gradient) and N x K blocked along K (forward)."""
+        omc.omc_decompress_set(self.arena, self.plan, self.sb, self.values)
+        for name, buffers in self.mx4.items():
+            omc.omc_mx4_quantize(self.value(name), *buffers)
+
+    def _workspace(self, rows: int) -> torch.Tensor:
+        d, f = self.width, self.inner
+        need = max(omc.omc_mx4_linear_workspace_bytes(rows, f, d), omc.omc_mx4_linear_workspace_bytes(rows, d, f),
+                   omc.omc_mx4_linear_backward_workspace_bytes(rows, f, d), omc.omc_mx4_linear_backward_workspace_bytes(rows, d, f),
+                   omc.omc_layer_norm_backward_workspace_bytes(rows, d))
+        if self.ws.numel() < need:
+            self.ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+        return self.ws
+
+    def forward(self, x: torch.Tensor, keep: bool = False) -> torch.Tensor:
+        """x [frames, width] in fp32 -> the module's output in fp32; keep: what backward needs."""
+        rows, half = x.shape[0], torch.bfloat16
+        ws = self._workspace(rows)
+        y, h = torch.empty(rows, self.width, device="cuda", dtype=half), torch.empty(rows, self.inner, device="cuda", dtype=half)
+        z = torch.empty(rows, self.width, device="cuda")
+        mean, rstd = (torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")) if keep else (None, None)
+        omc.omc_layer_norm(x, self.value("gamma"), self.value("beta"), EPS, y, mean, rstd)
+        omc.omc_mx4_linear(y, *self.mx4["w1"][2:], self.value("b1"), h, ws)
+        a = h * torch.sigmoid(h)
+        omc.omc_mx4_linear(a, *self.mx4["w2"][2:], self.value("b2"), z, ws)
+        if keep:
+            self.kept = (x, mean, rstd, y, h, a)
+        return x + 0.5 * z
+
+    def backward(self, dout: torch.Tensor) -> torch.Tensor:
+        """The gradients of all variables into the flat gradient buffer; returns the input's."""
+        x, mean, rstd, y, h, a = self.kept
+        ws = self._workspace(x.shape[0])
+        da, dy, dx = torch.empty_like(h), torch.empty_like(y), torch.empty_like(x)
+        omc.omc_mx4_linear_backward((0.5 * dout).to(a.dtype), a, *self.mx4["w2"][:2], da, self.grad("w2"), self.grad("b2"), ws)
+        s = torch.sigmoid(h.float())
+        dh = (da.float() * s * (1.0 + h.float() * (1.0 - s))).to(h.dtype)
+        omc.omc_mx4_linear_backward(dh, y, *self.mx4["w1"][:2], dy, self.grad("w1"), self.grad("b1"), ws)
+        omc.omc_layer_norm_backward(dy, x, self.value("gamma"), mean, rstd, dx, self.grad("gamma"), self.grad("beta"), ws)
+        return dx + dout
+
+    def step(self, o) -> None:
+        """Decompress -> update -> recompress with the gradients of the last backward pass."""
+        wanted = {omc.OMC_SGD: 0, omc.OMC_MOMENTUM: 1, omc.OMC_ADAM: 2}[o.kind]
+        while len(self.states) < wanted:
+            self.states.append(torch.zeros_like(self.values))
+        first, second = (self.states + [None, None])[:2]
+        omc.omc_step_update_recompress(self.arena, self.plan, self.sb, self.grads, first, second, o, self.step_ws)
+        self.refresh()
+
+
+def main() -> None:
+    import argparse
+    p = argparse.ArgumentParser(description="Train a feed-forward module on 4-bit products, then answer single frames.")
+    for name, default in (("width", 512), ("inner", 2048), ("frames", 1024), ("steps", 20)):
+        p.add_argument("--" + name, type=int, default=default)
+    p.add_argument("--lr", type=float, default=2e-3)
+    a = p.parse_args()
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x = torch.randn(a.frames, a.width, device="cuda", generator=g)
+    target = x + 0.3 * torch.tanh(x.roll(1, 1))
+    module = FeedForward(a.width, a.inner)
+    for t in range(1, a.steps + 1):
+        out = module.forward(x, keep=True)
+        diff = out - target
+        module.backward(diff * (2.0 / diff.numel()))
+        module.step(omc.opt(omc.OMC_ADAM, a.lr, t=t))
+        print(f"step {t}: mean square error {diff.square().mean().item():.6f}", flush=True)
+    frame = torch.cat([module.forward(x[i:i + 1]) for i in range(4)])
+    print(f"four frames one by one, largest difference from the batch: {(frame - module.forward(x)[:4]).abs().max().item():.3g}")
+
+
+if __name__ == "__main__":
+    main()
