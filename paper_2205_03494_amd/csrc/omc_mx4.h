@@ -47,16 +47,38 @@ __device__ __forceinline__ uint16_t to_bf16(float a) { return __builtin_bit_cast
 template <typename T>
 struct Eight {
     uint32_t w[2 * T::kBytes];
-    __device__ __forceinline__ void load(const typename T::type *p, uint32_t left) {   // the first `left` of them, and zeros
-        if (left >= 8) {
-            __builtin_memcpy(w, p, 8 * T::kBytes);
-        } else if constexpr (T::kBytes == 4) {
+    // fetch and then settle: a row's values from col on, and zeros past its end.  There the row's last eight are fetched and moved down, so that all lanes load alike, whole vectors, and
+    // nothing waits between the loads of several pieces.  SHORT: rows may have fewer than eight.
+    template <bool SHORT>
+    __device__ __forceinline__ void fetch(const typename T::type *row, uint32_t col, uint32_t cols) {
+        if (SHORT && cols < 8) {
+            typename T::type v[8];
 #pragma unroll
-            for (uint32_t i = 0; i < 8; ++i) w[i] = i < left ? __builtin_bit_cast(uint32_t, p[i]) : 0u;
+            for (uint32_t i = 0; i < 8; ++i) v[i] = row[i + cols < 8 ? 0u : i + cols - 8];
+            __builtin_memcpy(w, v, 8 * T::kBytes);
         } else {
-#pragma unroll
-            for (uint32_t i = 0; i < 4; ++i) w[i] = (2 * i < left ? p[2 * i] : 0u) | (2 * i + 1 < left ? static_cast<uint32_t>(p[2 * i + 1]) << 16 : 0u);
+            __builtin_memcpy(w, row + min(col, cols - 8), 8 * T::kBytes);
         }
+    }
+    static __device__ __forceinline__ uint32_t missing(uint32_t col, uint32_t cols) { return col + 8 <= cols ? 0u : min(8u, col + 8 - cols); }
+    __device__ __forceinline__ void settle(uint32_t missing) {
+        if (missing == 0) return;
+        constexpr uint32_t kWords = 2 * T::kBytes;
+        if constexpr (T::kBytes == 2) {
+            const uint32_t by = missing & 1u ? 16u : 0u;
+#pragma unroll
+            for (uint32_t i = 0; i < kWords; ++i) w[i] = __builtin_amdgcn_alignbit(i + 1 < kWords ? w[i + 1] : 0u, w[i], by);
+        }
+#pragma unroll
+        for (uint32_t by = 1; by <= kWords; by *= 2) {
+            const bool move = missing & (by * 4 / T::kBytes);
+#pragma unroll
+            for (uint32_t i = 0; i < kWords; ++i) w[i] = move ? (i + by < kWords ? w[i + by] : 0u) : w[i];
+        }
+    }
+    __device__ __forceinline__ void load(const typename T::type *row, uint32_t col, uint32_t cols) {
+        fetch<true>(row, col, cols);
+        settle(missing(col, cols));
     }
     __device__ __forceinline__ void clear() {
 #pragma unroll

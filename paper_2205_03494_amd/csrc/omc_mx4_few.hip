@@ -76,7 +76,7 @@ __global__ __launch_bounds__(512) void mx4_few_kernel(Mx4GemmArgs g, Mx4Rows row
             for (uint32_t k = 0; k < kTogether; ++k) {
                 const uint32_t item = base + k * blockDim.x + threadIdx.x, row = item / eights, col = 8 * (item % eights);
                 v[k].clear();
-                if (item < items && col < g.K) v[k].load(static_cast<const typename X::type *>(rows.x) + row * rows.ldx + col, g.K - col);
+                if (item < items && col < g.K) v[k].load(static_cast<const typename X::type *>(rows.x) + row * rows.ldx, col, g.K);
             }
 #pragma unroll
             for (uint32_t k = 0; k < kTogether; ++k) {

@@ -104,7 +104,7 @@ __global__ __launch_bounds__(256) void mx4_rows_kernel(QuantArgs qa, uint32_t fi
     const uint32_t row = first + item / eights, col = 8 * (item % eights);
     Eight<T> v;
     v.clear();
-    if (mine && col < qa.cols) v.load(static_cast<const typename T::type *>(qa.x) + row * qa.ldx + col, qa.cols - col);
+    if (mine && col < qa.cols) v.load(static_cast<const typename T::type *>(qa.x) + row * qa.ldx, col, qa.cols);
     quantize_eight<T>(qa, v, row, col, padded, mine);
 }
 

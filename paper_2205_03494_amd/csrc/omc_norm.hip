@@ -1,7 +1,8 @@
 // omc_layer_norm and omc_layer_norm_backward.
 //
 // Bound by memory: a row is read once and stays in registers, eight neighbours a lane and piece, between the sum of its values, the sum of their squared distances from the mean, and
-// the result.  A wave takes a row of up to 2048 values, four waves up to 8192, sixteen up to 16384; longer rows are read again for every sum.
+// the result; the next row's loads are on their way meanwhile.  8, 16, 32 or 64 lanes take a row of up to 64, 128, 256 or 1024 values, 2, 4, 8 or 16 waves up to 16384; longer rows are read
+// again for every sum.
 // Backward, a thread keeps the same columns of all rows that its workgroup takes, so that the sums over the rows (dgamma, dbeta) stay in registers too; every workgroup leaves one row of
 // partial sums, which a second kernel adds up in order.
 #include <type_traits>
@@ -10,28 +11,47 @@
 
 namespace omc {
 
-// Sum over the 64 lanes, in all of them; a fixed tree.
-__device__ __forceinline__ float wave_sum(float x) {
-    auto dpp = [](float v, auto control) { return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), decltype(control)::value, 0xf, 0xf, true)); };
-    x += dpp(x, std::integral_constant<int, 0xb1>{});    // lanes 1 0 3 2
-    x += dpp(x, std::integral_constant<int, 0x4e>{});    // lanes 2 3 0 1
-    x += dpp(x, std::integral_constant<int, 0x141>{});   // eight lanes mirrored
-    x += dpp(x, std::integral_constant<int, 0x140>{});   // sixteen lanes mirrored
-    const auto a = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), false, false);
-    x = __uint_as_float(a[0]) + __uint_as_float(a[1]);
-    const auto b = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), false, false);
+template <int CONTROL>
+__device__ __forceinline__ float from_lane(float v) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), CONTROL, 0xf, 0xf, true));
+}
+__device__ __forceinline__ float add_row_pairs(float x) {      // over the two rows of 16 lanes in each half of the wave
+    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(a[0]) + __uint_as_float(a[1]);
+}
+__device__ __forceinline__ float add_halves(float x) {
+    const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
     return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
+// Sum over the LANES neighbours that share a row, in all of them; a fixed tree.
+template <int LANES>
+__device__ __forceinline__ float row_lanes_sum(float x) {
+    x += from_lane<0xb1>(x);                   // lanes 1 0 3 2
+    x += from_lane<0x4e>(x);                   // lanes 2 3 0 1
+    x += from_lane<0x141>(x);                  // eight lanes mirrored
+    if constexpr (LANES >= 16) x += from_lane<0x140>(x);   // sixteen lanes mirrored
+    if constexpr (LANES >= 32) x = add_row_pairs(x);
+    if constexpr (LANES >= 64) x = add_halves(x);
+    return x;
+}
+// Sum over the lanes of a wave that have the same columns of different rows.
+template <int LANES>
+__device__ __forceinline__ float same_columns_sum(float x) {
+    if constexpr (LANES <= 32) x = add_halves(x);
+    if constexpr (LANES <= 16) x = add_row_pairs(x);
+    if constexpr (LANES <= 8) x += from_lane<0x128>(x);    // eight lanes on
+    return x;
+}
 
-// Sums over the WAVES waves that share a row.  Every call takes the next of two places in LDS, so that one barrier a call is enough: who writes a place again has passed
+// Sums over the lanes and the WAVES waves that share a row.  Every call takes the next of two places in LDS, so that one barrier a call is enough: who writes a place again has passed
 // the barrier of the call between, which nobody does before having read it.
-template <int WAVES, int COUNT>
+template <int LANES, int WAVES, int COUNT>
 struct RowSum {
-    float (*places)[WAVES][COUNT];             // [2]
+    float (*places)[16][COUNT];                // [2]
     uint32_t wave, next;
     __device__ __forceinline__ void operator()(float (&x)[COUNT]) {
 #pragma unroll
-        for (int c = 0; c < COUNT; ++c) x[c] = wave_sum(x[c]);
+        for (int c = 0; c < COUNT; ++c) x[c] = row_lanes_sum<LANES>(x[c]);
         if constexpr (WAVES > 1) {
             auto &place = places[next];
             next ^= 1;
@@ -40,50 +60,88 @@ struct RowSum {
                 for (int c = 0; c < COUNT; ++c) place[wave][c] = x[c];
             }
             __syncthreads();
+            const uint32_t first = wave / WAVES * WAVES;
 #pragma unroll
             for (int c = 0; c < COUNT; ++c) {
-                x[c] = place[0][c];
+                x[c] = place[first][c];
 #pragma unroll
-                for (int w = 1; w < WAVES; ++w) x[c] += place[w][c];
+                for (int w = 1; w < WAVES; ++w) x[c] += place[first + w][c];
             }
         }
     }
 };
 
-__device__ __forceinline__ void load_weights(float (&w)[8], const float *p, uint32_t left, float otherwise) {
-    if (p && left >= 8) {
-        __builtin_memcpy(w, p, 32);
+// Eight of gamma or beta from column `col` on, like a row's values; all `otherwise` if there is none.
+template <bool SHORT>
+__device__ __forceinline__ void fetch_weights(Eight<F32> &w, const float *row, uint32_t col, uint32_t cols, float otherwise) {
+    if (row) {
+        w.fetch<SHORT>(row, col, cols);
     } else {
 #pragma unroll
-        for (uint32_t i = 0; i < 8; ++i) w[i] = p && i < left ? p[i] : otherwise;
+        for (int i = 0; i < 8; ++i) w.w[i] = __float_as_uint(otherwise);
     }
 }
 
 __device__ __forceinline__ float reciprocal_deviation(float variance, float eps) { return 1.0f / __builtin_sqrtf(variance + eps); }
 
-// WAVES waves a row, PIECES pieces of eight values a lane; a workgroup of 4 waves (WAVES <= 4) or of WAVES takes rows blockIdx.x, + gridDim.x, ... of its groups.
-template <typename X, typename Y, int WAVES, int PIECES>
-__global__ __launch_bounds__(WAVES < 4 ? 256 : 64 * WAVES) void norm_kernel(NormArgs na) {
-    constexpr int kTogether = WAVES < 4 ? 4 / WAVES : 1;
-    __shared__ float places[2][WAVES][1];
-    const uint32_t wave = threadIdx.x >> 6, cols = na.cols, t = threadIdx.x % (64 * WAVES);
-    RowSum<WAVES, 1> row_sum{places, wave, 0};
-    uint32_t left[PIECES];
-    float gamma[PIECES][8], beta[PIECES][8];
+// How a workgroup's threads are dealt out to rows and columns: LANES lanes (64 if WAVES > 1) of WAVES waves a row, kRows rows at a time; at least four waves.
+// With kAhead a row's values are asked for before the row before it is worked on.  That takes registers, so that fewer waves are there, and pays where a row has many waves, which wait for
+// each other: 8192 x 8192 in bf16 takes 50 us with it, 55 without, 8192 x 1024 8.2 and 7.6.  Backward (kGradAhead) it pays without many waves too, since a wave's sums over the rows
+// leave no room for others: 8192 x 1024 with x in fp32 20 us, 22 without, 8192 x 8192 80 and 90; not at four waves (32768 x 4096: 152 and 147), nor at sixteen, whose registers it exceeds.
+template <int LANES, int WAVES>
+struct Deal {
+    static_assert(LANES == 64 || WAVES == 1, "whole waves share a row");
+    static constexpr int kWaves = WAVES < 4 ? 4 : WAVES, kThreads = 64 * kWaves, kWidth = LANES * WAVES, kRows = kThreads / kWidth;
+    static constexpr bool kAhead = WAVES >= 4, kGradAhead = WAVES <= 2 || WAVES == 8;
+    static constexpr uint32_t kGroups = kAhead ? 512 : 1024, kGradGroups = kGradAhead || WAVES == 16 ? 256 : 512;   // at most
+    static __device__ __forceinline__ uint32_t row() { return threadIdx.x / kWidth; }
+    static __device__ __forceinline__ uint32_t lane() { return threadIdx.x % kWidth; }
+};
+
+template <typename X, typename Y, int LANES, int WAVES, int PIECES, bool SHORT>
+__global__ __launch_bounds__((Deal<LANES, WAVES>::kThreads)) void norm_kernel(NormArgs na) {
+    typedef Deal<LANES, WAVES> D;
+    __shared__ float places[2][16][1];
+    const uint32_t cols = na.cols, t = D::lane(), mine = D::row();
+    RowSum<LANES, WAVES, 1> row_sum{places, threadIdx.x >> 6, 0};
+    uint32_t left[PIECES], missing[PIECES];
+    Eight<F32> gamma[PIECES], beta[PIECES];
+    Eight<X> next[PIECES];
+    auto load = [&](uint32_t row) {            // (the last row once more past the end)
+        const typename X::type *x = static_cast<const typename X::type *>(na.x) + min(row, na.rows - 1) * na.ldx;
+#pragma unroll
+        for (uint32_t p = 0; p < PIECES; ++p) next[p].template fetch<SHORT>(x, 8 * (t + D::kWidth * p), cols);
+    };
 #pragma unroll
     for (uint32_t p = 0; p < PIECES; ++p) {
-        const uint32_t col = 8 * (t + 64 * WAVES * p);
+        const uint32_t col = 8 * (t + D::kWidth * p);
         left[p] = col < cols ? cols - col : 0u;
-        load_weights(gamma[p], na.gamma ? na.gamma + col : nullptr, left[p], 1.0f);
-        load_weights(beta[p], na.beta ? na.beta + col : nullptr, left[p], 0.0f);
+        missing[p] = Eight<X>::missing(col, cols);
+    }
+    load(blockIdx.x * D::kRows + mine);
+#pragma unroll
+    for (uint32_t p = 0; p < PIECES; ++p) {
+        const uint32_t col = 8 * (t + D::kWidth * p);
+        fetch_weights<SHORT>(gamma[p], na.gamma, col, cols, 1.0f);
+        fetch_weights<SHORT>(beta[p], na.beta, col, cols, 0.0f);
+    }
+#pragma unroll
+    for (uint32_t p = 0; p < PIECES; ++p) {
+        if (na.gamma) gamma[p].settle(missing[p]);
+        if (na.beta) beta[p].settle(missing[p]);
     }
     const float count = static_cast<float>(cols);
-    for (uint32_t row = blockIdx.x * kTogether + (WAVES < 4 ? wave / WAVES : 0u); row < na.rows; row += gridDim.x * kTogether) {
-        const typename X::type *x = static_cast<const typename X::type *>(na.x) + row * na.ldx + 8 * t;
+    for (uint32_t base = blockIdx.x * D::kRows; base < na.rows; base += gridDim.x * D::kRows) {
+        const uint32_t row = base + mine;
+        if (!D::kAhead) load(row);
         Eight<X> v[PIECES];
-        float sum[1] = {0.0f};
 #pragma unroll
-        for (uint32_t p = 0; p < PIECES; ++p) v[p].load(x + 512 * WAVES * p, left[p]);
+        for (uint32_t p = 0; p < PIECES; ++p) {
+            v[p] = next[p];
+            v[p].settle(missing[p]);
+        }
+        if (D::kAhead) load(row + gridDim.x * D::kRows);
+        float sum[1] = {0.0f};
 #pragma unroll
         for (uint32_t p = 0; p < PIECES; ++p)
 #pragma unroll
@@ -100,13 +158,14 @@ __global__ __launch_bounds__(WAVES < 4 ? 256 : 64 * WAVES) void norm_kernel(Norm
             }
         row_sum(squares);
         const float rstd = reciprocal_deviation(squares[0] / count, na.eps);
+        if (row >= na.rows) continue;          // (no barrier follows in this turn)
         typename Y::type *y = static_cast<typename Y::type *>(na.y) + row * na.ldy + 8 * t;
 #pragma unroll
         for (uint32_t p = 0; p < PIECES; ++p) {
             float out[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) out[i] = __builtin_fmaf((v[p].value(i) - mean) * rstd, gamma[p][i], beta[p][i]);
-            store_run<Y, 8>(y + 512 * WAVES * p, out, left[p]);
+            for (int i = 0; i < 8; ++i) out[i] = __builtin_fmaf((v[p].value(i) - mean) * rstd, gamma[p].value(i), beta[p].value(i));
+            store_run<Y, 8>(y + 8 * D::kWidth * p, out, left[p]);
         }
         if (t == 0) {
             if (na.mean) na.mean[row] = mean;
@@ -121,7 +180,7 @@ __global__ __launch_bounds__(1024) void norm_long_kernel(NormArgs na) {
     __shared__ float places[2][16][1];
     const uint32_t cols = na.cols;
     const float count = static_cast<float>(cols);
-    RowSum<16, 1> row_sum{places, threadIdx.x >> 6, 0};
+    RowSum<64, 16, 1> row_sum{places, threadIdx.x >> 6, 0};
     for (uint32_t row = blockIdx.x; row < na.rows; row += gridDim.x) {
         const typename X::type *x = static_cast<const typename X::type *>(na.x) + row * na.ldx;
         typename Y::type *y = static_cast<typename Y::type *>(na.y) + row * na.ldy;
@@ -149,91 +208,126 @@ __global__ __launch_bounds__(1024) void norm_long_kernel(NormArgs na) {
 
 // ---- backward
 
-// The partial sums of a workgroup: a row of 2 * cols floats, dgamma's then dbeta's.
-template <typename X, typename Y, int WAVES, int PIECES>
-__global__ __launch_bounds__(WAVES < 4 ? 256 : 64 * WAVES) void norm_grad_kernel(NormGradArgs na) {
-    constexpr int kTogether = WAVES < 4 ? 4 / WAVES : 1;
-    __shared__ float places[2][WAVES][2];
-    __shared__ float joined[kTogether > 1 ? kTogether - 1 : 1][kTogether > 1 ? 64 * WAVES * 16 : 1];
-    const uint32_t wave = threadIdx.x >> 6, cols = na.cols, t = threadIdx.x % (64 * WAVES), mine = WAVES < 4 ? wave / WAVES : 0u;
-    RowSum<WAVES, 2> row_sum{places, wave, 0};
-    uint32_t left[PIECES];
-    float gamma[PIECES][8], dgamma[PIECES][8], dbeta[PIECES][8];
+// The partial sums of a workgroup: a row of 2 * cols floats, dgamma's then dbeta's; of the only workgroup: dgamma and dbeta.
+template <typename X, typename Y, int LANES, int WAVES, int PIECES, bool SHORT>
+__global__ __launch_bounds__((Deal<LANES, WAVES>::kThreads)) void norm_grad_kernel(NormGradArgs na) {
+    typedef Deal<LANES, WAVES> D;
+    constexpr int kSets = D::kWaves / WAVES;   // of waves: as many threads have the same columns, after those of a wave are added
+    __shared__ float places[2][16][2];
+    __shared__ float joined[kSets > 1 ? kSets - 1 : 1][kSets > 1 ? 64 * WAVES * 16 : 1];
+    const uint32_t wave = threadIdx.x >> 6, cols = na.cols, t = D::lane(), mine = D::row();
+    RowSum<LANES, WAVES, 2> row_sum{places, wave, 0};
+    uint32_t left[PIECES], missing[PIECES];
+    Eight<F32> gamma[PIECES];
+    float dgamma[PIECES][8], dbeta[PIECES][8];
+    Eight<X> next_x[PIECES];
+    Eight<Y> next_dy[PIECES];
+    float next_mean, next_rstd;
+    auto load = [&](uint32_t row) {            // (the last row once more past the end)
+        const uint32_t from = min(row, na.rows - 1);
+        const typename X::type *x = static_cast<const typename X::type *>(na.x) + from * na.ldx;
+        const typename Y::type *dy = static_cast<const typename Y::type *>(na.dy) + from * na.lddy;
+#pragma unroll
+        for (uint32_t p = 0; p < PIECES; ++p) {
+            next_x[p].template fetch<SHORT>(x, 8 * (t + D::kWidth * p), cols);
+            next_dy[p].template fetch<SHORT>(dy, 8 * (t + D::kWidth * p), cols);
+        }
+        next_mean = na.mean[from];
+        next_rstd = na.rstd[from];
+    };
 #pragma unroll
     for (uint32_t p = 0; p < PIECES; ++p) {
-        const uint32_t col = 8 * (t + 64 * WAVES * p);
+        const uint32_t col = 8 * (t + D::kWidth * p);
         left[p] = col < cols ? cols - col : 0u;
-        load_weights(gamma[p], na.gamma ? na.gamma + col : nullptr, left[p], 1.0f);
+        missing[p] = Eight<X>::missing(col, cols);
 #pragma unroll
         for (int i = 0; i < 8; ++i) dgamma[p][i] = dbeta[p][i] = 0.0f;
     }
+    if (D::kGradAhead) load(blockIdx.x * D::kRows + mine);
+#pragma unroll
+    for (uint32_t p = 0; p < PIECES; ++p) fetch_weights<SHORT>(gamma[p], na.gamma, 8 * (t + D::kWidth * p), cols, 1.0f);
+    if (na.gamma) {
+#pragma unroll
+        for (uint32_t p = 0; p < PIECES; ++p) gamma[p].settle(missing[p]);
+    }
     const float count = static_cast<float>(cols);
-    for (uint32_t row = blockIdx.x * kTogether + mine; row < na.rows; row += gridDim.x * kTogether) {
-        const typename X::type *x = static_cast<const typename X::type *>(na.x) + row * na.ldx + 8 * t;
-        const typename Y::type *dy = static_cast<const typename Y::type *>(na.dy) + row * na.lddy + 8 * t;
+    for (uint32_t base = blockIdx.x * D::kRows; base < na.rows; base += gridDim.x * D::kRows) {
+        const uint32_t row = base + mine;
+        if (!D::kGradAhead) load(row);
         Eight<X> v[PIECES];
         Eight<Y> g[PIECES];
 #pragma unroll
         for (uint32_t p = 0; p < PIECES; ++p) {
-            v[p].load(x + 512 * WAVES * p, left[p]);
-            g[p].load(dy + 512 * WAVES * p, left[p]);
+            v[p] = next_x[p];
+            g[p] = next_dy[p];
+            v[p].settle(missing[p]);
+            g[p].settle(row < na.rows ? missing[p] : 8u);
         }
-        const float mean = na.mean[row], rstd = na.rstd[row];
+        const float mean = next_mean, rstd = next_rstd;
+        if (D::kGradAhead) load(row + gridDim.x * D::kRows);
         float sums[2] = {0.0f, 0.0f};
 #pragma unroll
         for (uint32_t p = 0; p < PIECES; ++p)
 #pragma unroll
             for (int i = 0; i < 8; ++i) {      // (past the end dy is zero, and x finite)
-                const float hat = (v[p].value(i) - mean) * rstd, d = g[p].value(i), u = d * gamma[p][i];
+                const float hat = (v[p].value(i) - mean) * rstd, d = g[p].value(i), u = d * gamma[p].value(i);
                 sums[0] += u;
                 sums[1] = __builtin_fmaf(u, hat, sums[1]);
                 dgamma[p][i] = __builtin_fmaf(d, hat, dgamma[p][i]);
                 dbeta[p][i] += d;
             }
-        if (na.dx) {
-            row_sum(sums);
-            const float mean_u = sums[0] / count, mean_uh = sums[1] / count;
-            typename X::type *dx = static_cast<typename X::type *>(na.dx) + row * na.lddx + 8 * t;
+        if (!na.dx) continue;
+        row_sum(sums);
+        if (row >= na.rows) continue;
+        const float mean_u = sums[0] / count, mean_uh = sums[1] / count;
+        typename X::type *dx = static_cast<typename X::type *>(na.dx) + row * na.lddx + 8 * t;
 #pragma unroll
-            for (uint32_t p = 0; p < PIECES; ++p) {
-                float out[8];
+        for (uint32_t p = 0; p < PIECES; ++p) {
+            float out[8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float hat = (v[p].value(i) - mean) * rstd;
-                    out[i] = rstd * ((__builtin_fmaf(g[p].value(i), gamma[p][i], -mean_u)) - hat * mean_uh);
-                }
-                store_run<X, 8>(dx + 512 * WAVES * p, out, left[p]);
+            for (int i = 0; i < 8; ++i) {
+                const float hat = (v[p].value(i) - mean) * rstd;
+                out[i] = rstd * ((__builtin_fmaf(g[p].value(i), gamma[p].value(i), -mean_u)) - hat * mean_uh);
             }
+            store_run<X, 8>(dx + 8 * D::kWidth * p, out, left[p]);
         }
     }
     if (!na.parts) return;
-    float *to = na.parts + static_cast<uint64_t>(blockIdx.x) * 2 * cols;
+    const bool only = gridDim.x == 1;
+    float *to_gamma = only ? na.dgamma : na.parts + static_cast<uint64_t>(blockIdx.x) * 2 * cols;
+    float *to_beta = only ? na.dbeta : na.parts + (static_cast<uint64_t>(blockIdx.x) * 2 + 1) * cols;
+    const uint32_t set = wave / WAVES, at = threadIdx.x % (64 * WAVES);
 #pragma unroll
     for (uint32_t p = 0; p < PIECES; ++p) {
-        if constexpr (kTogether > 1) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            dgamma[p][i] = same_columns_sum<LANES>(dgamma[p][i]);
+            dbeta[p][i] = same_columns_sum<LANES>(dbeta[p][i]);
+        }
+        if constexpr (kSets > 1) {
             if (p > 0) __syncthreads();
-            if (mine > 0) {
+            if (set > 0) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    joined[mine - 1][i * (64 * WAVES) + t] = dgamma[p][i];
-                    joined[mine - 1][(8 + i) * (64 * WAVES) + t] = dbeta[p][i];
+                    joined[set - 1][i * (64 * WAVES) + at] = dgamma[p][i];
+                    joined[set - 1][(8 + i) * (64 * WAVES) + at] = dbeta[p][i];
                 }
             }
             __syncthreads();
-            if (mine == 0) {
-#pragma unroll
-                for (int w = 0; w < kTogether - 1; ++w)
+            if (set == 0) {
+#pragma unroll 1
+                for (int w = 0; w < kSets - 1; ++w)
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
-                        dgamma[p][i] += joined[w][i * (64 * WAVES) + t];
-                        dbeta[p][i] += joined[w][(8 + i) * (64 * WAVES) + t];
+                        dgamma[p][i] += joined[w][i * (64 * WAVES) + at];
+                        dbeta[p][i] += joined[w][(8 + i) * (64 * WAVES) + at];
                     }
             }
         }
-        if (mine == 0 && left[p] > 0) {
-            const uint32_t col = 8 * (t + 64 * WAVES * p);
-            store_run<F32, 8>(to + col, dgamma[p], left[p]);
-            store_run<F32, 8>(to + cols + col, dbeta[p], left[p]);
+        if (threadIdx.x < D::kWidth && left[p] > 0) {
+            const uint32_t col = 8 * (t + D::kWidth * p);
+            if (to_gamma) store_run<F32, 8>(to_gamma + col, dgamma[p], left[p]);
+            if (to_beta) store_run<F32, 8>(to_beta + col, dbeta[p], left[p]);
         }
     }
 }
@@ -244,7 +338,7 @@ __global__ __launch_bounds__(1024) void norm_grad_long_kernel(NormGradArgs na) {
     __shared__ float places[2][16][2];
     const uint32_t cols = na.cols;
     const float count = static_cast<float>(cols);
-    RowSum<16, 2> row_sum{places, threadIdx.x >> 6, 0};
+    RowSum<64, 16, 2> row_sum{places, threadIdx.x >> 6, 0};
     for (uint32_t row = blockIdx.x; row < na.rows; row += gridDim.x) {
         const typename X::type *x = static_cast<const typename X::type *>(na.x) + row * na.ldx;
         const typename Y::type *dy = static_cast<const typename Y::type *>(na.dy) + row * na.lddy;
@@ -283,7 +377,22 @@ __global__ __launch_bounds__(256) void norm_grad_columns_kernel(NormGradArgs na)
 }
 
 constexpr uint32_t kLongest = 16384;           // values of a row that stays in registers
-static uint32_t waves_of(uint32_t cols) { return cols <= 2048 ? 1 : cols <= 8192 ? 4 : 16; }
+// call(lanes, waves, pieces, short) of the kernel that rows of this length take.
+template <int V>
+using Int = std::integral_constant<int, V>;
+template <typename F>
+static void by_length(uint32_t cols, F &&call) {
+    if (cols < 8) call(Int<8>{}, Int<1>{}, Int<1>{}, std::true_type{});
+    else if (cols <= 64) call(Int<8>{}, Int<1>{}, Int<1>{}, std::false_type{});
+    else if (cols <= 128) call(Int<16>{}, Int<1>{}, Int<1>{}, std::false_type{});
+    else if (cols <= 256) call(Int<32>{}, Int<1>{}, Int<1>{}, std::false_type{});
+    else if (cols <= 512) call(Int<64>{}, Int<1>{}, Int<1>{}, std::false_type{});
+    else if (cols <= 1024) call(Int<64>{}, Int<1>{}, Int<2>{}, std::false_type{});
+    else if (cols <= 2048) call(Int<64>{}, Int<2>{}, Int<2>{}, std::false_type{});
+    else if (cols <= 4096) call(Int<64>{}, Int<4>{}, Int<2>{}, std::false_type{});
+    else if (cols <= 8192) call(Int<64>{}, Int<8>{}, Int<2>{}, std::false_type{});
+    else call(Int<64>{}, Int<16>{}, Int<2>{}, std::false_type{});
+}
 
 template <typename X, typename Y>
 static int launch_norm(const NormArgs &na, hipStream_t st) {
@@ -291,14 +400,12 @@ static int launch_norm(const NormArgs &na, hipStream_t st) {
         norm_long_kernel<X, Y><<<dim3(na.rows < 4096 ? na.rows : 4096), dim3(1024), 0, st>>>(na);
         return static_cast<int>(hipGetLastError());
     }
-    const uint32_t waves = waves_of(na.cols), together = waves < 4 ? 4 / waves : 1, groups = (na.rows + together - 1) / together;
-    const dim3 grid(groups < 2048 ? groups : 2048), block(waves < 4 ? 256 : 64 * waves);
-    if (na.cols <= 512) norm_kernel<X, Y, 1, 1><<<grid, block, 0, st>>>(na);
-    else if (na.cols <= 1024) norm_kernel<X, Y, 1, 2><<<grid, block, 0, st>>>(na);
-    else if (na.cols <= 2048) norm_kernel<X, Y, 1, 4><<<grid, block, 0, st>>>(na);
-    else if (na.cols <= 4096) norm_kernel<X, Y, 4, 2><<<grid, block, 0, st>>>(na);
-    else if (na.cols <= 8192) norm_kernel<X, Y, 4, 4><<<grid, block, 0, st>>>(na);
-    else norm_kernel<X, Y, 16, 2><<<grid, block, 0, st>>>(na);
+    by_length(na.cols, [&](auto lanes, auto waves, auto pieces, auto few) {
+        constexpr int L = decltype(lanes)::value, W = decltype(waves)::value, P = decltype(pieces)::value;
+        constexpr bool S = decltype(few)::value;
+        const uint32_t groups = (na.rows + Deal<L, W>::kRows - 1) / Deal<L, W>::kRows;
+        norm_kernel<X, Y, L, W, P, S><<<dim3(groups < Deal<L, W>::kGroups ? groups : Deal<L, W>::kGroups), dim3(Deal<L, W>::kThreads), 0, st>>>(na);
+    });
     return static_cast<int>(hipGetLastError());
 }
 int launch_layer_norm(const NormArgs &na, bool x_bf16, bool y_bf16, void *stream) {
@@ -307,12 +414,17 @@ int launch_layer_norm(const NormArgs &na, bool x_bf16, bool y_bf16, void *stream
     return y_bf16 ? launch_norm<F32, BF16>(na, st) : launch_norm<F32, F32>(na, st);
 }
 
-// Rows of partial sums: as many as workgroups.
+// Rows of partial sums, as many as workgroups.  Each costs 16 bytes a column through memory, as much as two to four rows of x, dy and dx: a workgroup has at least four rows.
 static uint32_t grad_groups(uint32_t rows, uint32_t cols) {
     if (cols > kLongest) return rows < 64 ? rows : 64;
-    const uint32_t waves = waves_of(cols), together = waves < 4 ? 4 / waves : 1, groups = (rows + together - 1) / together;
-    const uint32_t most = waves == 16 ? 256 : 512;
-    return groups < most ? groups : most;
+    uint32_t groups = 0;
+    by_length(cols, [&](auto lanes, auto waves, auto, auto) {
+        typedef Deal<decltype(lanes)::value, decltype(waves)::value> D;
+        const uint32_t each = D::kRows < 4 ? 4 : D::kRows;
+        groups = (rows + each - 1) / each;
+        if (groups > D::kGradGroups) groups = D::kGradGroups;
+    });
+    return groups;
 }
 size_t layer_norm_backward_workspace(uint32_t rows, uint32_t cols) { return 8ull * grad_groups(rows, cols) * cols; }
 
@@ -325,14 +437,12 @@ static int launch_grad(const NormGradArgs &given, hipStream_t st) {
         if (na.dx) norm_grad_long_kernel<X, Y><<<dim3(na.rows < 4096 ? na.rows : 4096), dim3(1024), 0, st>>>(na);
         if (na.parts) norm_grad_columns_kernel<X, Y><<<dim3((na.cols + 255) / 256, groups), dim3(256), 0, st>>>(na);
     } else {
-        const uint32_t waves = waves_of(na.cols);
-        const dim3 grid(groups), block(waves < 4 ? 256 : 64 * waves);
-        if (na.cols <= 512) norm_grad_kernel<X, Y, 1, 1><<<grid, block, 0, st>>>(na);
-        else if (na.cols <= 1024) norm_grad_kernel<X, Y, 1, 2><<<grid, block, 0, st>>>(na);
-        else if (na.cols <= 2048) norm_grad_kernel<X, Y, 1, 4><<<grid, block, 0, st>>>(na);
-        else if (na.cols <= 4096) norm_grad_kernel<X, Y, 4, 2><<<grid, block, 0, st>>>(na);
-        else if (na.cols <= 8192) norm_grad_kernel<X, Y, 4, 4><<<grid, block, 0, st>>>(na);
-        else norm_grad_kernel<X, Y, 16, 2><<<grid, block, 0, st>>>(na);
+        by_length(na.cols, [&](auto lanes, auto waves, auto pieces, auto few) {
+            constexpr int L = decltype(lanes)::value, W = decltype(waves)::value, P = decltype(pieces)::value;
+        constexpr bool S = decltype(few)::value;
+            norm_grad_kernel<X, Y, L, W, P, S><<<dim3(groups), dim3(Deal<L, W>::kThreads), 0, st>>>(na);
+        });
+        if (groups == 1) na.parts = nullptr;
     }
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || !na.parts) return static_cast<int>(e);
