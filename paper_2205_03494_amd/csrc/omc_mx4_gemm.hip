@@ -41,13 +41,8 @@ __device__ __forceinline__ const uint8_t *in_scalars(const uint8_t *p) {
     return reinterpret_cast<const uint8_t *>(static_cast<uint64_t>(hi) << 32 | lo);
 }
 
-// Keeps a product between the reads and loads that it is written between: without it the compiler gathers the products behind all of them.  (With one wave a SIMD the sums
-// are in the accumulation registers.)
-template <bool ACCUMULATION>
-__device__ __forceinline__ void stays_here(f32x16 &x) {
-    if constexpr (ACCUMULATION) asm volatile("" : "+a"(x));
-    else asm volatile("" : "+v"(x));
-}
+// Keeps a product between the reads and loads that it is written between: without it the compiler gathers the products behind all of them.
+__device__ __forceinline__ void stays_here(f32x16 &x) { asm volatile("" : "+v"(x)); }
 
 // Tile x of a grid of tiles: as tile_of_block deals them to the workgroups, x for the workgroup's number.
 __device__ __forceinline__ void tile_of(uint32_t x, uint32_t group_rows, uint32_t tiles_m, uint32_t tiles_n, uint32_t &tm, uint32_t &tn) {
@@ -62,6 +57,7 @@ constexpr uint32_t kCorner = 2560;             // LDS of a wave for its results 
 struct Mx4TileArgs {
     Mx4GemmArgs g;
     uint32_t tiles_m, tiles_n, splits, stages_per_split;
+    bool streams;                              // C is more than the caches hold, in whole cache lines
 };
 
 // WM x WN waves of TM x TN matrix tiles, and LOADERS that load for all (0: every wave loads its share), OCC waves per SIMD.  SPLIT: the contraction is cut into parts, whose results go to g.parts in fp32.
@@ -218,7 +214,7 @@ void mx4_gemm_kernel(Mx4TileArgs ta) {
             });
             for_constants<L1 - L0>([&](auto x) { load_one(from, far, UintTag<L0 + decltype(x)::value>{}); });
             acc[i][j] = mx4_multiply_32<s>(b[s & 1][j], sb[0][j], a[s & 1][i], sa[0][i], acc[i][j]);
-            stays_here<OCC == 1>(acc[i][j]);
+            stays_here(acc[i][j]);
             __builtin_amdgcn_sched_barrier(0);
         });
     };
@@ -290,7 +286,7 @@ void mx4_gemm_kernel(Mx4TileArgs ta) {
             ldc = g.ldc;
         }
         const uint32_t s_row = lane / kLanes, s_col = kRun * (lane % kLanes);
-        const bool stored = p.m0 + BM <= g.M && p.n0 + BN <= g.N;   // a whole tile
+        const bool streams = !SPLIT && ta.streams, stored = p.m0 + BM <= g.M && p.n0 + BN <= g.N;   // a whole tile
 #pragma unroll
         for (uint32_t j = 0; j < TN; ++j) {
             const uint32_t n_tile = p.n0 + 32 * (TN * wn + j), n = n_tile + s_col;
@@ -333,7 +329,9 @@ void mx4_gemm_kernel(Mx4TileArgs ta) {
                         const u32x4 w = *reinterpret_cast<const u32x4 *>(corner + (kRows * k + s_row) * kPitch + 4 * (lane % kLanes) * 4);
                         const uint32_t m = p.m0 + 32 * (TM * wm + i) + kPass * pass + kRows * k + s_row;
                         typename Out::type *to = c + m * ldc + n;
-                        if (stored || (m < g.M && n + kRun <= g.N)) {
+                        if (streams && stored) {
+                            __builtin_nontemporal_store(w, reinterpret_cast<u32x4 *>(to));
+                        } else if (stored || (m < g.M && n + kRun <= g.N)) {
                             __builtin_memcpy(to, &w, 16);
                         } else if (m < g.M) {
 #pragma unroll
@@ -380,16 +378,20 @@ __global__ __launch_bounds__(256) void mx4_join_kernel(Mx4GemmArgs g, uint32_t s
 
 // Which tile a product takes, and into how many parts its contraction is cut, by an estimate of the time in us: `base` is a launch; `alone` a stage of workgroups that nothing else slows down,
 // `resident` of them on a compute unit; `busy` what a stage costs per workgroup of a unit where all units have some (of the last workgroups' unevenness over the units `uneven` counts); `store` the
-// stores of 256 tiles.  Fitted to 170 sizes (100 for the largest tile) of 33 .. 16384 x 64 .. 8192 x 64 .. 8192, bf16 results: 6 - 11 % (standard deviation).  On these the chosen tile takes
-// 1.2 % longer than the best one on average, at worst 18 % (7231 x 309 x 7868).  16384 x 8192 x 8192: 256 x 256 545 us, 128 x 128 604, 128 x 64 836; 8192 x 4096 x 1024: 32, 28, 35;
-// 1003 x 971 x 243: 13, 5.6, 4.5, 64 x 64 4.1.
-// Cutting the contraction costs a second launch, 3.2 us, and the parts' way through memory; it is worth that for few tiles of a long one (456 x 92 x 5377: 9.8 -> 8.6 us in four parts).
+// stores of 256 tiles.  Fitted to 188 sizes (130 for the largest tile) of 33 .. 16384 x 64 .. 8192 x 64 .. 8192, bf16 results: 8 - 10 % (standard deviation).  On these the chosen tile takes
+// 6.5 % longer than the best of eight that were tried.  16384 x 8192 x 8192: 256 x 256 510 us, 128 x 128 630, 64 x 64 940; 8192 x 4096 x 1024: 30, 30, 42; 4096 x 1024 x 8192: 47, 22, 30;
+// 1003 x 971 x 243: 9.6, 5.1, 4.0.
+// The largest tile's eight waves load for themselves; beside the others are four that only load (64 x 8192 x 8192 in tiles of 64 x 64: 12.8 us without them, 10 with).  128 x 128 has three stages
+// and the unit for itself: a stage more on its way counts for more than a second workgroup with two stages where each unit has one tile (4096 x 1024 x 8192: 26 us), and for less in a
+// row of tiles with few stages each (8192 x 4096 x 1024: 29 us).
+// Cutting the contraction costs a second launch, 3.2 us, and the parts' way through memory; it is worth that for few tiles of a very long one.
 struct Mx4Tile {
     uint32_t bm, bn, resident;
+    bool cut;
     double base, alone, busy, uneven, store;
 };
 static constexpr Mx4Tile kMx4Tiles[] = {
-    {256, 256, 1, 3.0, 1.118, 1.831, 0.593, 12.4}, {128, 128, 2, 3.6, 0.425, 0.586, 0.729, 1.147}, {128, 64, 2, 3.0, 0.48, 0.378, 1.0, 0.774}, {64, 64, 2, 3.0, 0.278, 0.231, 1.0, 0.52},
+    {256, 256, 1, false, -1.274, 0.622, 2.371, 0.397, 9.878}, {128, 128, 1, true, 2.723, 0.344, 0.646, 0.501, 1.638}, {64, 64, 2, true, 2.972, 0.161, 0.224, 0.81, 0.45},
 };
 struct Mx4Choice {
     int tile;
@@ -399,11 +401,11 @@ static Mx4Choice choose(uint32_t M, uint32_t N, uint32_t K) {
     const uint32_t stages = (K + 255) / 256;
     Mx4Choice best{-1, 1};
     double best_cost = 0.0;
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < 3; ++i) {
         const Mx4Tile &t = kMx4Tiles[i];
         const uint64_t tiles = static_cast<uint64_t>((M + t.bm - 1) / t.bm) * ((N + t.bn - 1) / t.bn);
         for (uint32_t splits = 1; splits <= 16; splits *= 2) {
-            if (splits > 1 && (tiles * splits > 256 || splits > stages)) break;
+            if (splits > 1 && (!t.cut || tiles * splits > 256 || splits > stages)) break;
             const uint64_t items = tiles * splits, units = (items + 255) / 256, rounds = (items + 256 * t.resident - 1) / (256 * t.resident);
             const double per_unit = static_cast<double>(items) / 256.0, steps = (stages + splits - 1) / splits;
             const double alone = t.alone * steps * static_cast<double>(rounds), busy = t.busy * steps * (per_unit + t.uneven * (static_cast<double>(units) - per_unit));
@@ -430,13 +432,18 @@ size_t mx4_gemm_workspace(uint32_t M, uint32_t N, uint32_t K) {
     return c.splits > 1 ? 4ull * c.splits * M * N : 0;
 }
 
-template <int WM, int WN, int TM, int TN, int LOADERS, int S, int OCC, typename T>
+template <int WM, int WN, int TM, int TN, int LOADERS, int S, int OCC, bool CUT, typename T>
 static void launch_tile(const Mx4TileArgs &ta, hipStream_t st) {
     constexpr uint32_t kLds = 32 * (TM * WM + TN * WN) * S * 136 + WM * WN * kCorner, kByLds = 163840 / kLds, kByWaves = 4 * OCC / (WM * WN + LOADERS);
     const uint32_t items = ta.tiles_m * ta.tiles_n * ta.splits, most = 256 * (kByLds < kByWaves ? kByLds : kByWaves);
     const dim3 grid(items < most ? items : most), block(64 * (WM * WN + LOADERS));
-    if (ta.splits > 1) mx4_gemm_kernel<WM, WN, TM, TN, LOADERS, S, OCC, T, true><<<grid, block, 0, st>>>(ta);
-    else mx4_gemm_kernel<WM, WN, TM, TN, LOADERS, S, OCC, T, false><<<grid, block, 0, st>>>(ta);
+    if constexpr (CUT) {
+        if (ta.splits > 1) {
+            mx4_gemm_kernel<WM, WN, TM, TN, LOADERS, S, OCC, T, true><<<grid, block, 0, st>>>(ta);
+            return;
+        }
+    }
+    mx4_gemm_kernel<WM, WN, TM, TN, LOADERS, S, OCC, T, false><<<grid, block, 0, st>>>(ta);
 }
 
 template <typename T>
@@ -444,12 +451,15 @@ static int launch(const Mx4GemmArgs &ga, hipStream_t st) {
     const Mx4Choice c = choose(ga.M, ga.N, ga.K);
     const Mx4Tile &t = kMx4Tiles[c.tile];
     const uint32_t stages = (ga.K + 255) / 256;
-    const Mx4TileArgs ta{ga, (ga.M + t.bm - 1) / t.bm, (ga.N + t.bn - 1) / t.bn, c.splits, (stages + c.splits - 1) / c.splits};
+    // Stores past the caches (8 x 4 MB of L2): 8192 x 4096 in bf16, K of 1024, in tiles of 128 x 128: 31.3 -> 29.8 us; 16384 x 8192 x 8192 in these: 667 -> 630 us.  Of parts of cache
+    // lines it costs more than it gives (2948 x 3118 x 932: 13.8 us, 16 - 23 with it), and 0.3 us where C stays in the caches.
+    const uint64_t pitch = ga.ldc * T::kBytes;
+    const bool streams = ga.M * pitch >= 32u << 20 && (pitch | reinterpret_cast<uintptr_t>(ga.c)) % 128 == 0;
+    const Mx4TileArgs ta{ga, (ga.M + t.bm - 1) / t.bm, (ga.N + t.bn - 1) / t.bn, c.splits, (stages + c.splits - 1) / c.splits, streams};
     switch (c.tile) {
-        case 0: launch_tile<2, 2, 4, 4, 0, 2, 1, T>(ta, st); break;
-        case 1: launch_tile<2, 2, 2, 2, 4, 2, 4, T>(ta, st); break;
-        case 2: launch_tile<2, 2, 2, 1, 0, 2, 2, T>(ta, st); break;
-        default: launch_tile<2, 2, 1, 1, 0, 4, 2, T>(ta, st); break;
+        case 0: launch_tile<4, 2, 2, 4, 0, 2, 2, false, T>(ta, st); break;
+        case 1: launch_tile<2, 4, 2, 1, 4, 3, 3, true, T>(ta, st); break;
+        default: launch_tile<2, 2, 1, 1, 4, 4, 4, true, T>(ta, st); break;
     }
     if (c.splits > 1) {
         const hipError_t e = hipGetLastError();

@@ -81,9 +81,17 @@ def as64(t):
 
 
 def product_tile(M, N, K):
-    """(index of the tile that the product takes, is its contraction cut, more tiles than the chip holds at a time): 256 x 256, 128 x 128, 128 x 64, 64 x 64."""
+    """(index of the tile that the product takes, is its contraction cut, more tiles than the chip holds at a time): 256 x 256, 128 x 128, 64 x 64."""
     fn = omc._lib.omc_internal_mx4_tile
     fn.restype, fn.argtypes = C.c_int, [C.c_uint32] * 3
     tile, parts = fn(M, N, K) % 16, fn(M, N, K) // 16
-    bm, bn, at_a_time = ((256, 256, 256), (128, 128, 512), (128, 64, 512), (64, 64, 512))[tile]
+    bm, bn, at_a_time = ((256, 256, 256), (128, 128, 256), (64, 64, 512))[tile]
     return tile, parts > 1, -(-M // bm) * -(-N // bn) * parts > at_a_time
+
+
+# Products that between them take every tile, with fewer and with more of them than the chip holds at a time, whole and odd numbers of 128s, and contractions in parts.
+PRODUCTS = [(7242, 1702, 3983), (2213, 5436, 3864), (7859, 3827, 3283), (3814, 7658, 3103), (1069, 4825, 131), (653, 7529, 33), (2457, 3302, 130),
+            (4624, 1681, 34), (70, 8513, 8934), (69, 8432, 8525), (512, 512, 65536), (8366, 138, 132), (8356, 131, 33), (406, 8690, 133),
+            (531, 6706, 33), (36, 34, 129), (257, 6724, 461), (282, 6605, 289), (34, 37, 3758), (33, 35, 3698), (1798, 8103, 43), (4013, 7311, 1304),
+            (644, 8567, 35), (2931, 1062, 320), (471, 6654, 1532), (332, 648, 25899), (641, 359, 26001), (34, 33, 5207), (37, 37, 4868),
+            (260, 150, 9001)]

@@ -98,7 +98,6 @@ def test_the_binding_refuses_what_it_cannot_pass_on():
 
 
 def test_every_tile_of_the_product_is_taken():
-    seen = {ref.product_tile(*shape) for shape in ((7242, 1702, 3983), (7859, 3827, 3283), (653, 7529, 33), (2457, 3302, 130), (512, 512, 65536), (8356, 131, 33), (531, 6706, 33),
-                                                   (36, 34, 129), (282, 6605, 289), (33, 35, 3698))}
-    assert {tile for tile, _, _ in seen} == {0, 1, 2, 3}
-    assert {tile for tile, cut, _ in seen if cut} >= {1, 3} and {tile for tile, _, turns in seen if turns} == {0, 1, 2, 3}
+    seen = {ref.product_tile(*shape) for shape in ref.PRODUCTS}
+    assert {(tile, turns) for tile, cut, turns in seen if not cut} == {(tile, turns) for tile in range(3) for turns in (False, True)}
+    assert {tile for tile, cut, _ in seen if cut} == {1, 2}
