@@ -36,12 +36,13 @@ struct QuantArgs {
     uint8_t *codes_t, *scales_t;   // blocks along a column; may be null
     void *values;                  // may be null
     uint64_t ldv;
-    float *colsum;                 // partial sums of the columns, one row of them for every 256 rows of x; may be null
+    float *colsum;                 // partial sums of the columns, a row of them for every tile of rows (mx4_tile_height); may be null
     bool images;                   // scales and scales_t in the tiles' order
     Mx4Reorder also;               // another matrix' scales, by the same launch (along rows only; see launch_mx4_tiles)
 };
 // Several matrices in one launch, in any directions but without values, and another one's scales.
 constexpr uint32_t kMostJobs = 3;
+uint32_t mx4_tile_height(const QuantArgs *args, uint32_t count);   // rows of a tile of such a launch; its columns' sums are that many rows' each, 256 / height to every 256 rows
 int launch_mx4_tiles(const QuantArgs *args, uint32_t count, const Mx4Reorder &also, bool bf16, void *stream);
 int launch_mx4_reorder(const Mx4Reorder &a, const Mx4Reorder &b, void *stream);
 int launch_mx4_quantize(const QuantArgs &qa, bool bf16, void *stream);   // no sums
@@ -57,6 +58,9 @@ struct Mx4GemmArgs {
 // c = a b^T + bias, c in bf16 or fp32; the operands' scales in the tiles' order.
 size_t mx4_gemm_workspace(uint32_t M, uint32_t N, uint32_t K);   // bytes of parts
 int launch_mx4_gemm(const Mx4GemmArgs &ga, bool bf16, void *stream);
+// Two products, the second one's result in fp32, in one launch, and in it dbias, whose columns are the second one's, from `count` rows of partial sums (dbias may be null).
+bool mx4_gemm_pairs(uint32_t M, uint32_t N, uint32_t K, uint32_t M2, uint32_t N2, uint32_t K2);   // may they go together?
+int launch_mx4_pair(const Mx4GemmArgs &ga, bool bf16, const Mx4GemmArgs &gb, const float *parts, uint32_t count, float *dbias, void *stream);
 // The same for few rows of a, with scales in the order of omc.h.  Where mx4_few_rounds, these may come as they are (`rows`), and are rounded on the way.
 constexpr uint32_t kMx4FewRows = 32;
 struct Mx4Rows {

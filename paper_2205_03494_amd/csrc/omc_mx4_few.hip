@@ -155,10 +155,12 @@ __global__ __launch_bounds__(512) void mx4_few_kernel(Mx4GemmArgs g, Mx4Rows row
     }
 }
 
-// LDS that a rounded A may take.
-constexpr uint64_t kFusedBytes = 16384;
+// A is rounded by every workgroup where that is worth less than a launch: up to 16 rows and 8 KB of codes and scales (1 x 4096 x 1024: 3.4 us, 4.5 with a launch before; 16 x 4096 x 1024, 8.7 KB:
+// 5.1 and 4.8; 29 x 4096 x 1024: 7.6 and 5.1).
+constexpr uint32_t kFusedRows = 16;
+constexpr uint64_t kFusedBytes = 8192;
 static uint64_t rounded_bytes(uint32_t M, uint32_t K) { return static_cast<uint64_t>(M) * (mx4_padded(K) / 32) * 17; }
-bool mx4_few_rounds(uint32_t M, uint32_t, uint32_t K) { return M <= kMx4FewRows && rounded_bytes(M, K) <= kFusedBytes; }
+bool mx4_few_rounds(uint32_t M, uint32_t, uint32_t K) { return M <= kFusedRows && rounded_bytes(M, K) <= kFusedBytes; }
 
 template <int MT, int S, bool FUSED, typename T, typename X>
 static int launch_rows(const Mx4GemmArgs &ga, const Mx4Rows &rows, hipStream_t st) {
@@ -172,8 +174,7 @@ static int launch_rows(const Mx4GemmArgs &ga, const Mx4Rows &rows, hipStream_t s
 template <typename T>
 static int launch_typed(const Mx4GemmArgs &ga, const Mx4Rows *rows, hipStream_t st) {
     if (!rows) return ga.M <= 16 ? launch_rows<1, 3, false, T, T>(ga, Mx4Rows{}, st) : launch_rows<2, 2, false, T, T>(ga, Mx4Rows{}, st);
-    if (rows->bf16) return ga.M <= 16 ? launch_rows<1, 4, true, T, BF16>(ga, *rows, st) : launch_rows<2, 4, true, T, BF16>(ga, *rows, st);
-    return ga.M <= 16 ? launch_rows<1, 4, true, T, F32>(ga, *rows, st) : launch_rows<2, 4, true, T, F32>(ga, *rows, st);
+    return rows->bf16 ? launch_rows<1, 4, true, T, BF16>(ga, *rows, st) : launch_rows<1, 4, true, T, F32>(ga, *rows, st);
 }
 
 int launch_mx4_few(const Mx4GemmArgs &ga, const Mx4Rows *rows, bool bf16, void *stream) {

@@ -70,24 +70,25 @@ __device__ __forceinline__ void quantize_eight(const QuantArgs &qa, const Eight<
 }
 
 // 8 bytes of scales of a row, a thread.
+template <uint32_t ROWS>
 __device__ __forceinline__ void reorder_scales(const Mx4Reorder &re, uint32_t block) {
-    const uint32_t k128 = mx4_padded(re.cols) / 128, stages = (k128 + 1) / 2, groups = (re.rows + 255) / 256;
-    const uint32_t stage = block / groups, row = block % groups * 256 + threadIdx.x;
-    if (stage >= stages || row >= re.rows || threadIdx.x >= 256) return;
+    const uint32_t k128 = mx4_padded(re.cols) / 128, stages = (k128 + 1) / 2, groups = (re.rows + ROWS - 1) / ROWS;
+    const uint32_t stage = block / groups, row = block % groups * ROWS + threadIdx.x;
+    if (stage >= stages || row >= re.rows || threadIdx.x >= ROWS) return;
     const uint32_t *from = reinterpret_cast<const uint32_t *>(re.scales) + static_cast<uint64_t>(row) * k128 + 2 * stage;
     const uint32_t lower = from[0], upper = 2 * stage + 1 < k128 ? from[1] : 0u;
     uint32_t *to = reinterpret_cast<uint32_t *>(re.image + stage * mx4_image_pitch(re.rows)) + 2 * row;
     to[0] = (lower & 0xffffu) | upper << 16;
     to[1] = lower >> 16 | (upper & 0xffff0000u);
 }
-static uint32_t reorder_blocks(const Mx4Reorder &re) { return re.image ? (re.rows + 255) / 256 * ((mx4_padded(re.cols) + 255) / 256) : 0u; }
+static uint32_t reorder_blocks(const Mx4Reorder &re, uint32_t rows) { return re.image ? (re.rows + rows - 1) / rows * ((mx4_padded(re.cols) + 255) / 256) : 0u; }
 
 __global__ __launch_bounds__(256) void mx4_reorder_kernel(Mx4Reorder a, Mx4Reorder b, uint32_t blocks_a) {
-    if (blockIdx.x < blocks_a) reorder_scales(a, blockIdx.x);
-    else reorder_scales(b, blockIdx.x - blocks_a);
+    if (blockIdx.x < blocks_a) reorder_scales<256>(a, blockIdx.x);
+    else reorder_scales<256>(b, blockIdx.x - blocks_a);
 }
 int launch_mx4_reorder(const Mx4Reorder &a, const Mx4Reorder &b, void *stream) {
-    const uint32_t blocks_a = reorder_blocks(a), blocks = blocks_a + reorder_blocks(b);
+    const uint32_t blocks_a = reorder_blocks(a, 256), blocks = blocks_a + reorder_blocks(b, 256);
     mx4_reorder_kernel<<<dim3(blocks), dim3(256), 0, static_cast<hipStream_t>(stream)>>>(a, b, blocks_a);
     return static_cast<int>(hipGetLastError());
 }
@@ -96,7 +97,7 @@ int launch_mx4_reorder(const Mx4Reorder &a, const Mx4Reorder &b, void *stream) {
 template <typename T>
 __global__ __launch_bounds__(256) void mx4_rows_kernel(QuantArgs qa, uint32_t first, uint32_t items) {
     if (qa.also.image && blockIdx.x >= (items + 255) / 256) {
-        reorder_scales(qa.also, blockIdx.x - (items + 255) / 256);
+        reorder_scales<256>(qa.also, blockIdx.x - (items + 255) / 256);
         return;
     }
     const uint32_t padded = mx4_padded(qa.cols), eights = padded / 8, item = blockIdx.x * 256 + threadIdx.x;
@@ -108,7 +109,7 @@ __global__ __launch_bounds__(256) void mx4_rows_kernel(QuantArgs qa, uint32_t fi
     quantize_eight<T>(qa, v, row, col, padded, mine);
 }
 
-constexpr uint32_t kHigh = 256, kWide = 128;   // a tile; a wave takes 32 rows of it
+constexpr uint32_t kWide = 128;                // columns of a tile; a wave takes 32 rows of it
 
 // Two columns of 32 rows in a lane (bf16: both in lo): their blocks' codes and scale bytes.
 template <typename T>
@@ -228,16 +229,17 @@ struct TileJobs {
     Mx4Reorder also;
 };
 
-// Tiles of 256 x 128: blocks along the columns, along the rows, the columns' sums.
-template <typename T>
-__global__ __launch_bounds__(512) void mx4_tiles_kernel(TileJobs jobs) {
+// Tiles of HIGH x 128: blocks along the columns, along the rows, the columns' sums.
+template <typename T, uint32_t HIGH>
+__global__ __launch_bounds__(2 * HIGH) void mx4_tiles_kernel(TileJobs jobs) {
     typedef typename T::type E;
-    constexpr uint32_t kPitch = 144;           // bytes of a column's codes in LDS, 128 and padding
+    static_assert(HIGH == 64 || HIGH == 256, "two blocks along a column, or all of a stage's");
+    constexpr uint32_t kWaves = HIGH / 32, kPitch = HIGH / 2 + 16;   // bytes of a column's codes in LDS, with padding
     __shared__ __attribute__((aligned(16))) uint8_t codes_lds[kWide * kPitch];
-    __shared__ __attribute__((aligned(16))) uint32_t rows_lds[8][8 * 64];
-    __shared__ __attribute__((aligned(16))) uint8_t scales_lds[kWide * 8];
-    __shared__ __attribute__((aligned(16))) uint8_t row_scales_lds[8][32 * 4];
-    __shared__ float sums_lds[8][kWide];
+    __shared__ __attribute__((aligned(16))) uint32_t rows_lds[kWaves][8 * 64];
+    __shared__ __attribute__((aligned(16))) uint8_t scales_lds[kWide * kWaves];
+    __shared__ __attribute__((aligned(16))) uint8_t row_scales_lds[kWaves][32 * 4];
+    __shared__ float sums_lds[kWaves][kWide];
     uint32_t begin = 0, which = 0;
 #pragma unroll
     for (uint32_t j = 0; j < kMostJobs; ++j)
@@ -246,7 +248,7 @@ __global__ __launch_bounds__(512) void mx4_tiles_kernel(TileJobs jobs) {
             which = j + 1;
         }
     if (which == kMostJobs) {
-        reorder_scales(jobs.also, blockIdx.x - begin);
+        reorder_scales<(HIGH < 256 ? 128 : 256)>(jobs.also, blockIdx.x - begin);
         return;
     }
     const QuantArgs &qa = jobs.job[which];
@@ -255,7 +257,7 @@ __global__ __launch_bounds__(512) void mx4_tiles_kernel(TileJobs jobs) {
     // a run of the tiles to every die: 64 bytes of a row's codes are half a cache line, whose other half the next tile has (4096 x 4095 along columns 9.5 us, dealt out one by one 10.9)
     const uint32_t q = total / 8, rest = total % 8, die = block % 8, id = die * q + min(die, rest) + block / 8;
     const uint32_t tr = id / tiles_c, tc = id % tiles_c;
-    const uint32_t r0 = tr * kHigh + 32 * wave, c0 = tc * kWide, col = c0 + 2 * lane;
+    const uint32_t r0 = tr * HIGH + 32 * wave, c0 = tc * kWide, col = c0 + 2 * lane;
     const uint32_t height = r0 < qa.rows ? min(32u, qa.rows - r0) : 0u;
     const E *x = static_cast<const E *>(qa.x);
 
@@ -302,7 +304,7 @@ __global__ __launch_bounds__(512) void mx4_tiles_kernel(TileJobs jobs) {
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
             *reinterpret_cast<u32x4 *>(codes_lds + (2 * lane + c) * kPitch + 16 * wave) = codes[c];
-            scales_lds[(2 * lane + c) * 8 + (qa.images ? mx4_image_byte(wave) : wave)] = static_cast<uint8_t>(byte[c]);
+            scales_lds[(2 * lane + c) * kWaves + (qa.images ? mx4_image_byte(wave) : wave)] = static_cast<uint8_t>(byte[c]);
         }
     }
     if (qa.codes) quantize_rows<T>(lo, hi, rows_lds[wave], row_scales_lds[wave], lane);
@@ -318,18 +320,27 @@ __global__ __launch_bounds__(512) void mx4_tiles_kernel(TileJobs jobs) {
     }
     __syncthreads();
     if (qa.codes_t) {
-        const uint32_t pitch = mx4_padded(qa.rows) / 2, begin = tr * (kHigh / 2), there = min(pitch - begin, kHigh / 2);   // bytes of a column, of those in this tile
+        const uint32_t pitch = mx4_padded(qa.rows) / 2, from = tr * (HIGH / 2), there = from < pitch ? min(pitch - from, HIGH / 2) : 0u;   // bytes of a column, of those in this tile
 #pragma unroll
-        for (uint32_t p = threadIdx.x; p < 8 * kWide; p += 512) {
-            const uint32_t c = p / 8, at = 16 * (p % 8);
+        for (uint32_t p = threadIdx.x; p < kWaves * kWide; p += 2 * HIGH) {
+            const uint32_t c = p / kWaves, at = 16 * (p % kWaves);
             if (c0 + c < qa.cols && at < there)
-                *reinterpret_cast<u32x4 *>(qa.codes_t + static_cast<uint64_t>(c0 + c) * pitch + begin + at) = *reinterpret_cast<const u32x4 *>(codes_lds + c * kPitch + at);
+                *reinterpret_cast<u32x4 *>(qa.codes_t + static_cast<uint64_t>(c0 + c) * pitch + from + at) = *reinterpret_cast<const u32x4 *>(codes_lds + c * kPitch + at);
         }
-        const uint32_t c = threadIdx.x / 2, half = threadIdx.x % 2;
-        if (threadIdx.x < 2 * kWide && c0 + c < qa.cols) {
-            const uint32_t bytes = reinterpret_cast<const uint32_t *>(scales_lds)[threadIdx.x];
-            if (qa.images) reinterpret_cast<uint32_t *>(qa.scales_t + tr * mx4_image_pitch(qa.cols))[2 * (c0 + c) + half] = bytes;
-            else if (64 * half < there) reinterpret_cast<uint32_t *>(qa.scales_t + static_cast<uint64_t>(c0 + c) * (pitch / 16))[2 * tr + half] = bytes;
+        if constexpr (HIGH == 256) {
+            const uint32_t c = threadIdx.x / 2, half = threadIdx.x % 2;
+            if (threadIdx.x < 2 * kWide && c0 + c < qa.cols) {
+                const uint32_t bytes = reinterpret_cast<const uint32_t *>(scales_lds)[threadIdx.x];
+                if (qa.images) reinterpret_cast<uint32_t *>(qa.scales_t + tr * mx4_image_pitch(qa.cols))[2 * (c0 + c) + half] = bytes;
+                else if (64 * half < there) reinterpret_cast<uint32_t *>(qa.scales_t + static_cast<uint64_t>(c0 + c) * (pitch / 16))[2 * tr + half] = bytes;
+            }
+        } else {
+            const uint32_t c = threadIdx.x;
+            if (c0 + c < qa.cols) {
+                const uint16_t bytes = reinterpret_cast<const uint16_t *>(scales_lds)[c];
+                if (qa.images) reinterpret_cast<uint16_t *>(qa.scales_t + (tr / 4) * mx4_image_pitch(qa.cols) + 8ull * (c0 + c))[mx4_image_byte(2 * (tr % 4)) / 2] = bytes;
+                else if (there > 0) reinterpret_cast<uint16_t *>(qa.scales_t + static_cast<uint64_t>(c0 + c) * (pitch / 16))[tr] = bytes;
+            }
         }
     }
     if (qa.codes) {                            // 64 bytes of a row (all of them: rows are padded to 128 values)
@@ -363,27 +374,39 @@ __global__ __launch_bounds__(512) void mx4_tiles_kernel(TileJobs jobs) {
         if (c < kWide && c0 + c < qa.cols) {
             float s = sums_lds[0][c];
 #pragma unroll
-            for (int w = 1; w < 8; ++w) s += sums_lds[w][c];
+            for (uint32_t w = 1; w < kWaves; ++w) s += sums_lds[w][c];
             qa.colsum[static_cast<uint64_t>(tr) * qa.cols + c0 + c] = s;
         }
     }
 }
 
-template <typename T>
-static int launch_tiles(const QuantArgs *args, uint32_t count, const Mx4Reorder &also, hipStream_t st) {
+// Fewer tiles of 256 rows than compute units: tiles of 64 (1000 x 777, both directions: 6.9 -> 5.5 us; 2048 x 2048 in fp32: 7.0 -> 6.4).  Of many these would store quarters of cache lines along the
+// columns (512 x 16384: 8.7 us, 10.1 with them).
+uint32_t mx4_tile_height(const QuantArgs *args, uint32_t count) {
+    uint64_t tiles = 0;
+    for (uint32_t j = 0; j < count; ++j) tiles += static_cast<uint64_t>((args[j].rows + 255) / 256) * ((args[j].cols + kWide - 1) / kWide);
+    return tiles < 256 ? 64 : 256;
+}
+// Whole stages of 256 rows in either tile's height, so that an image is written whole.
+template <typename T, uint32_t HIGH>
+static int launch_tiles_of(const QuantArgs *args, uint32_t count, const Mx4Reorder &also, hipStream_t st) {
     TileJobs jobs{};
     uint32_t end = 0;
     for (uint32_t j = 0; j < kMostJobs; ++j) {
         if (j < count) {
             jobs.job[j] = args[j];
             jobs.tiles_c[j] = (args[j].cols + kWide - 1) / kWide;
-            end += (args[j].rows + kHigh - 1) / kHigh * jobs.tiles_c[j];
+            end += (args[j].rows + 255) / 256 * (256 / HIGH) * jobs.tiles_c[j];
         }
         jobs.end[j] = end;
     }
     jobs.also = also;
-    mx4_tiles_kernel<T><<<dim3(end + reorder_blocks(also)), dim3(512), 0, st>>>(jobs);
+    mx4_tiles_kernel<T, HIGH><<<dim3(end + reorder_blocks(also, HIGH < 256 ? 128 : 256)), dim3(2 * HIGH), 0, st>>>(jobs);
     return static_cast<int>(hipGetLastError());
+}
+template <typename T>
+static int launch_tiles(const QuantArgs *args, uint32_t count, const Mx4Reorder &also, hipStream_t st) {
+    return mx4_tile_height(args, count) == 64 ? launch_tiles_of<T, 64>(args, count, also, st) : launch_tiles_of<T, 256>(args, count, also, st);
 }
 int launch_mx4_tiles(const QuantArgs *args, uint32_t count, const Mx4Reorder &also, bool bf16, void *stream) {
     hipStream_t st = static_cast<hipStream_t>(stream);
@@ -401,7 +424,7 @@ static int launch(QuantArgs qa, hipStream_t st) {
     const uint32_t eights = mx4_padded(qa.cols) / 8, most = (1u << 30) / eights;   // rows of one launch
     for (uint32_t first = 0; first < qa.rows; first += most) {
         const uint32_t items = (qa.rows - first < most ? qa.rows - first : most) * eights;
-        mx4_rows_kernel<T><<<dim3((items + 255) / 256 + reorder_blocks(qa.also)), dim3(256), 0, st>>>(qa, first, items);
+        mx4_rows_kernel<T><<<dim3((items + 255) / 256 + reorder_blocks(qa.also, 256)), dim3(256), 0, st>>>(qa, first, items);
         qa.also.image = nullptr;
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess || qa.rows - first <= most) return static_cast<int>(e);

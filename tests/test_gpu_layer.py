@@ -69,7 +69,7 @@ def same_values(got, want):
     assert np.array_equal(np.nan_to_num(got), np.nan_to_num(want))
 
 
-SHAPES = [(1, 1, 0), (1, 31, 0), (2, 32, 1), (5, 33, 0), (33, 64, 3), (127, 128, 0), (128, 130, 1), (131, 257, 7), (300, 100, 0), (64, 2056, 5), (513, 640, 0)]
+SHAPES = [(1, 1, 0), (1, 31, 0), (2, 32, 1), (5, 33, 0), (33, 64, 3), (127, 128, 0), (128, 130, 1), (131, 257, 7), (300, 100, 0), (64, 2056, 5), (513, 640, 0), (4100, 2190, 1)]
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
@@ -205,7 +205,8 @@ def test_rows_that_are_not_finite_stay_alone(M):
         check(y, a @ w.T, ref.product_bound(a, w, K), F32)
 
 
-BACKWARD = [(1, 1, 1, 0), (1, 64, 96, 0), (3, 33, 65, 1), (40, 96, 300, 0), (128, 64, 64, 0), (129, 257, 130, 3), (300, 520, 70, 0), (1003, 243, 97, 1), (2100, 128, 384, 0)]
+BACKWARD = [(1, 1, 1, 0), (1, 64, 96, 0), (3, 33, 65, 1), (40, 96, 300, 0), (128, 64, 64, 0), (129, 257, 130, 3), (300, 520, 70, 0), (1003, 243, 97, 1), (2100, 128, 384, 0), (257, 65, 700, 1),
+            (4001, 600, 1500, 0), (140001, 33, 40, 0)]
 
 
 @pytest.mark.parametrize("dtype,dx_type", [(BF16, BF16), (F32, F32), (BF16, F32)])
@@ -267,7 +268,8 @@ def _loss(x, cw, sw, b, dy, ws):
 
 
 NORM = [(1, 1, 0), (1, 512, 0), (2, 7, 1), (3, 64, 0), (5, 511, 1), (9, 513, 0), (33, 1000, 3), (4, 1024, 0), (7, 2047, 1), (6, 2056, 0), (5, 4096, 0), (3, 5001, 2),
-        (4, 8192, 0), (3, 8195, 1), (2, 16384, 0), (3, 16385, 0), (2, 40000, 1), (2500, 96, 0), (9000, 40, 0)]
+        (4, 8192, 0), (3, 8195, 1), (2, 16384, 0), (3, 16385, 0), (2, 40000, 1), (2500, 96, 0), (9000, 40, 0),
+        (70, 8, 0), (2, 9, 0), (130, 65, 1), (100, 129, 0), (700, 200, 1), (2300, 1100, 1), (1200, 3000, 0), (1000, 5000, 1), (600, 10001, 0)]
 TYPES = [(F32, F32), (F32, BF16), (BF16, BF16), (BF16, F32)]
 
 
