@@ -52,10 +52,14 @@ struct Eight {
     template <bool SHORT>
     __device__ __forceinline__ void fetch(const typename T::type *row, uint32_t col, uint32_t cols) {
         if (SHORT && cols < 8) {
-            typename T::type v[8];
+            clear();
+#pragma unroll 1                               // (unrolled, its loads would be merged with the others', and these be cut into elements)
+            for (uint32_t i = 0; i < cols; ++i) {   // from above
 #pragma unroll
-            for (uint32_t i = 0; i < 8; ++i) v[i] = row[i + cols < 8 ? 0u : i + cols - 8];
-            __builtin_memcpy(w, v, 8 * T::kBytes);
+                for (uint32_t k = 0; k + 1 < 2 * T::kBytes; ++k) w[k] = T::kBytes == 4 ? w[k + 1] : w[k + 1] << 16 | w[k] >> 16;
+                if constexpr (T::kBytes == 4) w[7] = __float_as_uint(row[i]);
+                else w[3] = static_cast<uint32_t>(row[i]) << 16 | w[3] >> 16;
+            }
         } else {
             __builtin_memcpy(w, row + min(col, cols - 8), 8 * T::kBytes);
         }
