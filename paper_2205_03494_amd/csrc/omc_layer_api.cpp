@@ -68,7 +68,7 @@ static LinearLayout linear_layout(uint8_t *ws, uint32_t M, uint32_t N, uint32_t 
     return l;
 }
 
-// The two products go different ways if M or K is small: dX's first operand has M rows, dW's K.
+// Either product may go in tiles or, if its first operand has few rows (dX's M, dW's K), the other way; the larger image has room for the scales in either order.
 struct BackwardLayout {
     uint8_t *dy, *dy_scales, *dy_t, *dy_t_scales, *x_t, *x_t_scales, *w_image;
     float *sums, *parts;
@@ -78,12 +78,12 @@ static BackwardLayout backward_layout(uint8_t *ws, uint32_t M, uint32_t N, uint3
     BackwardLayout l{};
     Parts p{ws};
     l.dy = p.take(mx4_code_bytes(M, N));
-    l.dy_scales = p.take(scale_bytes(M, M, N));
+    l.dy_scales = p.take(mx4_image_bytes(M, N));
     l.dy_t = p.take(mx4_code_bytes(N, M));
-    l.dy_t_scales = p.take(scale_bytes(K, N, M));
+    l.dy_t_scales = p.take(mx4_image_bytes(N, M));
     l.x_t = p.take(mx4_code_bytes(K, M));
-    l.x_t_scales = p.take(scale_bytes(K, K, M));
-    if (!few(M)) l.w_image = p.take(mx4_image_bytes(K, N));
+    l.x_t_scales = p.take(mx4_image_bytes(K, M));
+    l.w_image = p.take(mx4_image_bytes(K, N));
     l.sums = reinterpret_cast<float *>(p.take(4ull * ((M + 255) / 256 * 4) * N));
     const uint64_t dx = parts_bytes(M, K, N), dw = parts_bytes(K, N, M);
     l.parts = reinterpret_cast<float *>(p.take(dx > dw ? dx : dw));
@@ -178,7 +178,8 @@ omc_status omc_mx4_linear_backward(const void *dY, uint64_t lddy, const void *X,
     const bool bf16 = type == OMC_BF16;
 
     // all roundings in one launch; dY's in one pass, unless its two products want their scales in different orders
-    const bool dx_tiles = !few(M), dw_tiles = !few(K);
+    const int together = dX && dW ? mx4_pair_tile(M, K, N, K, N, M, dbias != nullptr) : -1;
+    const bool dx_tiles = together >= 0 || !few(M), dw_tiles = together >= 0 || !few(K);
     const Mx4Reorder weights = dX && dx_tiles ? Mx4Reorder{bytes(w_scales), l.w_image, K, N} : Mx4Reorder{};
     QuantArgs jobs[kMostJobs];
     uint32_t count = 1;
@@ -206,8 +207,7 @@ omc_status omc_mx4_linear_backward(const void *dY, uint64_t lddy, const void *X,
     const uint32_t sum_rows = (M + 255) / 256 * (256 / mx4_tile_height(jobs, count));
     const Mx4GemmArgs for_dx{{l.dy, l.dy_scales}, {bytes(w_codes), dx_tiles ? l.w_image : bytes(w_scales)}, nullptr, dX, lddx, M, K, N, l.parts};
     const Mx4GemmArgs for_dw{{l.x_t, l.x_t_scales}, {l.dy_t, l.dy_t_scales}, nullptr, dW, N, K, N, M, l.parts};
-    if (dX && dW && dx_tiles && dw_tiles && mx4_gemm_pairs(M, K, N, K, N, M))
-        return from_hip(launch_mx4_pair(for_dx, dx_type == OMC_BF16, for_dw, l.sums, sum_rows, dbias, stream));
+    if (together >= 0) return from_hip(launch_mx4_pair(together, for_dx, dx_type == OMC_BF16, for_dw, l.sums, sum_rows, dbias, stream));
     if (dbias) rc = launch_column_sums(l.sums, sum_rows, N, N, dbias, nullptr, stream);
     if (rc == 0 && dX) rc = launch_product(for_dx, dx_type == OMC_BF16, stream);
     if (rc == 0 && dW) rc = launch_product(for_dw, false, stream);

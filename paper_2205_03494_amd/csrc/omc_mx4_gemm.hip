@@ -61,7 +61,7 @@ struct Mx4TileArgs {
     bool streams;                              // C is more than the caches hold, in whole cache lines
 };
 
-// Two products whose tiles one launch deals out, the second one's after the first one's, which writes fp32; and in workgroups behind theirs, which are `groups`, sums of columns.
+// Two products whose tiles one launch deals out, the second one's, whose result is fp32, after the first one's; in workgroups behind theirs, which are `groups`, sums of columns.
 struct Mx4PairArgs {
     Mx4TileArgs first, second;
     uint32_t groups;
@@ -86,14 +86,15 @@ void mx4_gemm_kernel(typename std::conditional<PAIR, Mx4PairArgs, Mx4TileArgs>::
             auto of = [which](auto a, auto b) { return which == 0 ? a : b; };
             return Mx4TileArgs{{{of(x.g.a.codes, y.g.a.codes), of(x.g.a.scales, y.g.a.scales)}, {of(x.g.b.codes, y.g.b.codes), of(x.g.b.scales, y.g.b.scales)}, of(x.g.bias, y.g.bias),
                                 of(x.g.c, y.g.c), of(x.g.ldc, y.g.ldc), of(x.g.M, y.g.M), of(x.g.N, y.g.N), of(x.g.K, y.g.K), nullptr},
-                               of(x.tiles_m, y.tiles_m), of(x.tiles_n, y.tiles_n), 1, of(x.stages_per_split, y.stages_per_split), false};
+                               of(x.tiles_m, y.tiles_m), of(x.tiles_n, y.tiles_n), 1, of(x.stages_per_split, y.stages_per_split), of(x.streams, y.streams)};
         } else {
             return ta;
         }
     };
     const uint32_t lds0 = lds_offset(lds);
     const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave / WN, wn = wave % WN;
-    uint32_t groups = gridDim.x, tiles_first = product(0).tiles_m * product(0).tiles_n, items = SPLIT ? tiles_first * product(0).splits : tiles_first;
+    const uint32_t tiles_first = product(0).tiles_m * product(0).tiles_n;
+    uint32_t groups = gridDim.x, items = SPLIT ? tiles_first * product(0).splits : tiles_first;
     if constexpr (PAIR) {
         groups = ta.groups;
         items += ta.second.tiles_m * ta.second.tiles_n;
@@ -435,28 +436,29 @@ struct Mx4Tile {
 static constexpr Mx4Tile kMx4Tiles[] = {
     {256, 256, 1, false, -1.274, 0.622, 2.371, 0.397, 9.878}, {128, 128, 1, true, 2.723, 0.344, 0.646, 0.501, 1.638}, {64, 64, 2, true, 2.972, 0.161, 0.224, 0.81, 0.45},
 };
+static double cost(const Mx4Tile &t, uint32_t splits, uint32_t M, uint32_t N, uint32_t K) {
+    const uint32_t stages = (K + 255) / 256;
+    const uint64_t items = static_cast<uint64_t>((M + t.bm - 1) / t.bm) * ((N + t.bn - 1) / t.bn) * splits, units = (items + 255) / 256, rounds = (items + 256 * t.resident - 1) / (256 * t.resident);
+    const double per_unit = static_cast<double>(items) / 256.0, steps = (stages + splits - 1) / splits;
+    const double alone = t.alone * steps * static_cast<double>(rounds), busy = t.busy * steps * (per_unit + t.uneven * (static_cast<double>(units) - per_unit));
+    const double whole = t.base + (alone > busy ? alone : busy) + t.store * (per_unit > 1.0 ? per_unit : 1.0);
+    return splits > 1 ? whole + 3.2 + 2e-6 * splits * M * N : whole;   // (8 bytes of a part at 4 TB/s)
+}
 struct Mx4Choice {
     int tile;
     uint32_t splits;
+    double cost;
 };
 static Mx4Choice choose(uint32_t M, uint32_t N, uint32_t K) {
     const uint32_t stages = (K + 255) / 256;
-    Mx4Choice best{-1, 1};
-    double best_cost = 0.0;
+    Mx4Choice best{-1, 1, 0.0};
     for (int i = 0; i < 3; ++i) {
         const Mx4Tile &t = kMx4Tiles[i];
         const uint64_t tiles = static_cast<uint64_t>((M + t.bm - 1) / t.bm) * ((N + t.bn - 1) / t.bn);
         for (uint32_t splits = 1; splits <= 16; splits *= 2) {
             if (splits > 1 && (!t.cut || tiles * splits > 256 || splits > stages)) break;
-            const uint64_t items = tiles * splits, units = (items + 255) / 256, rounds = (items + 256 * t.resident - 1) / (256 * t.resident);
-            const double per_unit = static_cast<double>(items) / 256.0, steps = (stages + splits - 1) / splits;
-            const double alone = t.alone * steps * static_cast<double>(rounds), busy = t.busy * steps * (per_unit + t.uneven * (static_cast<double>(units) - per_unit));
-            double cost = t.base + (alone > busy ? alone : busy) + t.store * (per_unit > 1.0 ? per_unit : 1.0);
-            if (splits > 1) cost += 3.2 + 2e-6 * splits * M * N;   // (8 bytes of a part at 4 TB/s)
-            if (best.tile < 0 || cost < best_cost) {
-                best = Mx4Choice{i, splits};
-                best_cost = cost;
-            }
+            const double c = cost(t, splits, M, N, K);
+            if (best.tile < 0 || c < best.cost) best = Mx4Choice{i, splits, c};
         }
     }
     const uint32_t each = (stages + best.splits - 1) / best.splits;
@@ -488,15 +490,20 @@ static void launch_tile(const Mx4TileArgs &ta, hipStream_t st) {
     mx4_gemm_kernel<WM, WN, TM, TN, LOADERS, S, OCC, T, false, false><<<grid, block, 0, st>>>(ta);
 }
 
+// Stores past the caches (8 x 4 MB of L2): 8192 x 4096 in bf16, K of 1024, in tiles of 128 x 128: 31.3 -> 29.8 us; 16384 x 8192 x 8192 in these: 667 -> 630 us.  Of parts of cache lines it costs more
+// than it gives (2948 x 3118 x 932: 13.8 us, 16 - 23 with it), and 0.3 us where C stays in the caches.
+template <typename T>
+static bool past_caches(const Mx4GemmArgs &g) {
+    const uint64_t pitch = g.ldc * T::kBytes;
+    return g.M * pitch >= 32u << 20 && (pitch | reinterpret_cast<uintptr_t>(g.c)) % 128 == 0;
+}
+
 template <typename T>
 static int launch(const Mx4GemmArgs &ga, hipStream_t st) {
     const Mx4Choice c = choose(ga.M, ga.N, ga.K);
     const Mx4Tile &t = kMx4Tiles[c.tile];
     const uint32_t stages = (ga.K + 255) / 256;
-    // Stores past the caches (8 x 4 MB of L2): 8192 x 4096 in bf16, K of 1024, in tiles of 128 x 128: 31.3 -> 29.8 us; 16384 x 8192 x 8192 in these: 667 -> 630 us.  Of parts of cache
-    // lines it costs more than it gives (2948 x 3118 x 932: 13.8 us, 16 - 23 with it), and 0.3 us where C stays in the caches.
-    const uint64_t pitch = ga.ldc * T::kBytes;
-    const bool streams = ga.M * pitch >= 32u << 20 && (pitch | reinterpret_cast<uintptr_t>(ga.c)) % 128 == 0;
+    const bool streams = past_caches<T>(ga);
     const Mx4TileArgs ta{ga, (ga.M + t.bm - 1) / t.bm, (ga.N + t.bn - 1) / t.bn, c.splits, (stages + c.splits - 1) / c.splits, streams};
     switch (c.tile) {
         case 0: launch_tile<4, 2, 2, 4, 0, 2, 2, false, T>(ta, st); break;
@@ -511,24 +518,40 @@ static int launch(const Mx4GemmArgs &ga, hipStream_t st) {
     return static_cast<int>(hipGetLastError());
 }
 
-// Both in the smallest tiles, uncut: a launch for each would be most of their time (64 x 64 x 64, backward of a linear layer with its bias: 13.4 us in four launches, 8.9 in two).
-bool mx4_gemm_pairs(uint32_t M, uint32_t N, uint32_t K, uint32_t M2, uint32_t N2, uint32_t K2) {
-    const Mx4Choice a = choose(M, N, K), b = choose(M2, N2, K2);
-    return a.tile == 2 && b.tile == 2 && a.splits == 1 && b.splits == 1;
+// The tile in which both go together, uncut, or -1 where by the estimate each takes less in its best one, with a launch of its own and one for the sums.  Backward of a linear layer with its bias,
+// 64 x 64 x 64: 13.4 us in four launches, 8.9 in two; 1003 x 971 x 243 in fp32: 16.9 and 11.1; 4057 x 832 x 562 in bf16: 24.4 and 19.2;
+// 8192 x 1024 x 4096: 78.7 and 75.3; 4096 x 2048 x 2048: 46.2 and 41.3.
+int mx4_pair_tile(uint32_t M, uint32_t N, uint32_t K, uint32_t M2, uint32_t N2, uint32_t K2, bool sums) {
+    double best = choose(M, N, K).cost + choose(M2, N2, K2).cost + (sums ? 2.5 : 0.0);
+    int tile = -1;
+    for (int i = 1; i < 3; ++i) {
+        const double c = cost(kMx4Tiles[i], 1, M, N, K) + cost(kMx4Tiles[i], 1, M2, N2, K2) - kMx4Tiles[i].base;
+        if (c <= best) {
+            best = c;
+            tile = i;
+        }
+    }
+    return tile;
 }
+// Host only, not part of the interface: that tile's index for the backward pass of a linear layer.
+extern "C" int omc_internal_mx4_pair_tile(uint32_t M, uint32_t N, uint32_t K) { return mx4_pair_tile(M, K, N, K, N, M, true); }
+
 template <typename T>
-static int launch_pair(const Mx4GemmArgs &ga, const Mx4GemmArgs &gb, const ColumnSums &sums, hipStream_t st) {
-    auto tiles = [](const Mx4GemmArgs &g) { return Mx4TileArgs{g, (g.M + 63) / 64, (g.N + 63) / 64, 1, (g.K + 255) / 256, false}; };
-    Mx4PairArgs pa{tiles(ga), tiles(gb), 0, sums};
+static int launch_pair(int tile, const Mx4GemmArgs &ga, const Mx4GemmArgs &gb, const ColumnSums &sums, hipStream_t st) {
+    const uint32_t b = kMx4Tiles[tile].bm, most = 256 * kMx4Tiles[tile].resident;
+    auto tiles = [b](const Mx4GemmArgs &g, bool streams) { return Mx4TileArgs{g, (g.M + b - 1) / b, (g.N + b - 1) / b, 1, (g.K + 255) / 256, streams}; };
+    Mx4PairArgs pa{tiles(ga, past_caches<T>(ga)), tiles(gb, past_caches<F32>(gb)), 0, sums};
     const uint32_t items = pa.first.tiles_m * pa.first.tiles_n + pa.second.tiles_m * pa.second.tiles_n;
-    pa.groups = items < 512 ? items : 512;
-    mx4_gemm_kernel<2, 2, 1, 1, 4, 4, 4, T, false, true><<<dim3(pa.groups + (sums.width + 31) / 32), dim3(512), 0, st>>>(pa);
+    pa.groups = items < most ? items : most;
+    const dim3 grid(pa.groups + (sums.width + 31) / 32);
+    if (tile == 1) mx4_gemm_kernel<2, 4, 2, 1, 4, 3, 3, T, false, true><<<grid, dim3(768), 0, st>>>(pa);
+    else mx4_gemm_kernel<2, 2, 1, 1, 4, 4, 4, T, false, true><<<grid, dim3(512), 0, st>>>(pa);
     return static_cast<int>(hipGetLastError());
 }
-int launch_mx4_pair(const Mx4GemmArgs &ga, bool bf16, const Mx4GemmArgs &gb, const float *parts, uint32_t count, float *dbias, void *stream) {
+int launch_mx4_pair(int tile, const Mx4GemmArgs &ga, bool bf16, const Mx4GemmArgs &gb, const float *parts, uint32_t count, float *dbias, void *stream) {
     hipStream_t st = static_cast<hipStream_t>(stream);
     const ColumnSums sums{parts, count, dbias ? gb.N : 0, dbias ? gb.N : 0, dbias, nullptr};
-    return bf16 ? launch_pair<BF16>(ga, gb, sums, st) : launch_pair<F32>(ga, gb, sums, st);
+    return bf16 ? launch_pair<BF16>(tile, ga, gb, sums, st) : launch_pair<F32>(tile, ga, gb, sums, st);
 }
 
 int launch_mx4_gemm(const Mx4GemmArgs &ga, bool bf16, void *stream) {

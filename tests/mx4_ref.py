@@ -89,9 +89,20 @@ def product_tile(M, N, K):
     return tile, parts > 1, -(-M // bm) * -(-N // bn) * parts > at_a_time
 
 
+def pair_tile(M, N, K):
+    """Index of the tile in which both products of a backward pass go together; -1: each in a launch of its own."""
+    fn = omc._lib.omc_internal_mx4_pair_tile
+    fn.restype, fn.argtypes = C.c_int, [C.c_uint32] * 3
+    return fn(M, N, K)
+
+
 # Products that between them take every tile, with fewer and with more of them than the chip holds at a time, whole and odd numbers of 128s, and contractions in parts.
 PRODUCTS = [(7242, 1702, 3983), (2213, 5436, 3864), (7859, 3827, 3283), (3814, 7658, 3103), (1069, 4825, 131), (653, 7529, 33), (2457, 3302, 130),
             (4624, 1681, 34), (70, 8513, 8934), (69, 8432, 8525), (512, 512, 65536), (8366, 138, 132), (8356, 131, 33), (406, 8690, 133),
             (531, 6706, 33), (36, 34, 129), (257, 6724, 461), (282, 6605, 289), (34, 37, 3758), (33, 35, 3698), (1798, 8103, 43), (4013, 7311, 1304),
             (644, 8567, 35), (2931, 1062, 320), (471, 6654, 1532), (332, 648, 25899), (641, 359, 26001), (34, 33, 5207), (37, 37, 4868),
             (260, 150, 9001)]
+
+# Backward passes: few rows in either product, both together in either tile, apart.
+BACKWARD = [(1, 1, 1, 0), (1, 64, 96, 0), (3, 33, 65, 1), (40, 96, 300, 0), (128, 64, 64, 0), (129, 257, 130, 3), (300, 520, 70, 0), (1003, 243, 97, 1),
+            (2100, 128, 384, 0), (257, 65, 700, 1), (4001, 600, 1500, 0), (140001, 33, 40, 0), (2990, 1100, 1555, 1), (2048, 8192, 2304, 0)]

@@ -101,3 +101,7 @@ def test_every_tile_of_the_product_is_taken():
     seen = {ref.product_tile(*shape) for shape in ref.PRODUCTS}
     assert {(tile, turns) for tile, cut, turns in seen if not cut} == {(tile, turns) for tile in range(3) for turns in (False, True)}
     assert {tile for tile, cut, _ in seen if cut} == {1, 2}
+
+
+def test_backward_passes_go_together_and_apart():
+    assert {ref.pair_tile(M, N, K) for M, N, K, _ in ref.BACKWARD if M > 32 and K > 32} == {-1, 1, 2}
