@@ -229,6 +229,25 @@ def test_linear_backward(M, N, K, pad, dtype, dx_type):
         guarded(whole, ws)
 
 
+def test_backward_of_few_rows_and_a_large_matrix_is_its_products():
+    M, N, K = 20, 8192, 8192
+    g = torch.Generator("cuda").manual_seed(2)
+    x, dy = [torch.randn(M, n, device="cuda", generator=g).bfloat16() for n in (K, N)]
+    w = torch.randn(K, N, device="cuda", generator=g)
+    codes = lambda rows, cols: [torch.empty(f(rows, cols), dtype=torch.uint8, device="cuda") for f in (omc.omc_mx4_code_bytes, omc.omc_mx4_scale_bytes)]
+    wq, dyq, dyt, xt = codes(K, N), codes(M, N), codes(N, M), codes(K, M)
+    omc.omc_mx4_quantize(w, *wq)
+    omc.omc_mx4_quantize(dy, *dyq, *dyt)
+    omc.omc_mx4_quantize(x, None, None, *xt)
+    dx, dw, dbias = torch.empty(M, K, device="cuda"), torch.empty(K, N, device="cuda"), torch.empty(N, device="cuda")
+    omc.omc_mx4_linear_backward(dy, x, *wq, dx, dw, dbias, workspace(omc.omc_mx4_linear_backward_workspace_bytes(M, N, K))[1])
+    for got, a, b, rows, cols, along in ((dx, dyq, wq, M, K, N), (dw, xt, dyt, K, N, M)):
+        want = torch.empty(rows, cols, device="cuda")
+        omc.omc_mx4_gemm(*a, *b, None, want, along, workspace(omc.omc_mx4_gemm_workspace_bytes(rows, cols, along))[1])
+        assert torch.equal(got, want)
+    assert ((dbias.double() - dy.double().sum(0)).abs() <= 64 * 2.0 ** -24 * dy.double().abs().sum(0)).all()
+
+
 def test_linear_backward_against_differences():
     """On values that MX4 holds exactly in both directions the layer is linear and its gradients are exact: differences give the same numbers."""
     rng = np.random.default_rng(11)
