@@ -306,13 +306,16 @@ void mx4_gemm_kernel(typename std::conditional<PAIR, Mx4PairArgs, Mx4TileArgs>::
             for (int i = 0; i < TN; ++i) sb[0][i] = sb[1][i];
         }
 
-        // ---- through the wave's own corner of LDS, so that a row's 64 (bf16) or 128 bytes (fp32) of a tile are stored together
+        // ---- through the wave's own corner of LDS, so that 128 bytes of a row are stored together (64 of a bf16 result where a wave has one tile across): halves of cache lines from two tiles in turn
+        // made 12 - 18 % more traffic to memory, and 8192 x 4096 x 1024 took 28.4 us, 27 with whole ones
         const Mx4TileArgs of = product(p.which);
         const Mx4GemmArgs &g = of.g;
         const bool stored = p.m0 + BM <= g.M && p.n0 + BN <= g.N;   // a whole tile
         auto store = [&](auto type) {
             typedef decltype(type) Out;
-            constexpr uint32_t kRun = 16 / Out::kBytes, kLanes = 32 / kRun, kRows = 64 / kLanes, kPitch = 32 * Out::kBytes + 16, kPass = Out::kBytes == 2 ? 32 : 16;
+            constexpr uint32_t kTogether = Out::kBytes == 2 && TN % 2 == 0 ? 2 : 1;   // tiles side by side: 64 columns in bf16 are a cache line
+            constexpr uint32_t kRun = 16 / Out::kBytes, kLanes = 32 * kTogether / kRun, kRows = 64 / kLanes, kPitch = 32 * kTogether * Out::kBytes + 16;
+            constexpr uint32_t kPass = kPitch > 80 ? 16 : 32;
             static_assert(kPass * kPitch <= kCorner, "fits");
             uint8_t *corner = lds + kCorners + wave * kCorner;
             typename Out::type *c;
@@ -327,20 +330,24 @@ void mx4_gemm_kernel(typename std::conditional<PAIR, Mx4PairArgs, Mx4TileArgs>::
             const uint32_t s_row = lane / kLanes, s_col = kRun * (lane % kLanes);
             const bool streams = !SPLIT && of.streams;
 #pragma unroll
-            for (uint32_t j = 0; j < TN; ++j) {
-                const uint32_t n_tile = p.n0 + 32 * (TN * wn + j), n = n_tile + s_col;
-                float bias[16];               // of the lane's 16 columns, by scalar loads, which wait for none of the loads on their way
+            for (uint32_t j0 = 0; j0 < TN; j0 += kTogether) {
+                const uint32_t n = p.n0 + 32 * (TN * wn + j0) + s_col;
+                float bias[kTogether][16];    // of the lane's 16 columns, by scalar loads, which wait for none of the loads on their way
                 const bool whole_bias = !SPLIT && g.bias && stored;
-                if (whole_bias) {
-                    const __attribute__((address_space(4))) float *from = reinterpret_cast<const __attribute__((address_space(4))) float *>(reinterpret_cast<uintptr_t>(g.bias + n_tile));
 #pragma unroll
-                    for (uint32_t e = 0; e < 16; ++e) bias[e] = h == 0 ? from[e] : from[16 + e];
-                } else {
+                for (uint32_t jj = 0; jj < kTogether; ++jj) {
+                    const uint32_t n_tile = p.n0 + 32 * (TN * wn + j0 + jj);
+                    if (whole_bias) {
+                        const __attribute__((address_space(4))) float *from = reinterpret_cast<const __attribute__((address_space(4))) float *>(reinterpret_cast<uintptr_t>(g.bias + n_tile));
 #pragma unroll
-                    for (uint32_t e = 0; e < 16; ++e) bias[e] = 0.0f;
-                    if (!SPLIT && g.bias) {
+                        for (uint32_t e = 0; e < 16; ++e) bias[jj][e] = h == 0 ? from[e] : from[16 + e];
+                    } else {
 #pragma unroll
-                        for (uint32_t e = 0; e < 16; ++e) bias[e] = g.bias[min(n_tile + 16 * h + e, g.N - 1)];
+                        for (uint32_t e = 0; e < 16; ++e) bias[jj][e] = 0.0f;
+                        if (!SPLIT && g.bias) {
+#pragma unroll
+                            for (uint32_t e = 0; e < 16; ++e) bias[jj][e] = g.bias[min(n_tile + 16 * h + e, g.N - 1)];
+                        }
                     }
                 }
 #pragma unroll
@@ -348,24 +355,27 @@ void mx4_gemm_kernel(typename std::conditional<PAIR, Mx4PairArgs, Mx4TileArgs>::
 #pragma unroll
                     for (uint32_t pass = 0; pass < 32 / kPass; ++pass) {
                         if (kPass == 32 || r / kPass == pass) {
-                            float v[16];
 #pragma unroll
-                            for (uint32_t e = 0; e < 16; ++e) v[e] = acc[i][j][e] + bias[e];
-                            uint8_t *to = corner + (r % kPass) * kPitch + 16 * h * Out::kBytes;
-                            if constexpr (Out::kBytes == 4) {
+                            for (uint32_t jj = 0; jj < kTogether; ++jj) {
+                                float v[16];
 #pragma unroll
-                                for (uint32_t e = 0; e < 4; ++e) *reinterpret_cast<f32x4 *>(to + 16 * e) = f32x4{v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]};
-                            } else {
+                                for (uint32_t e = 0; e < 16; ++e) v[e] = acc[i][j0 + jj][e] + bias[jj][e];
+                                uint8_t *to = corner + (r % kPass) * kPitch + (32 * jj + 16 * h) * Out::kBytes;
+                                if constexpr (Out::kBytes == 4) {
 #pragma unroll
-                                for (uint32_t e = 0; e < 2; ++e)
-                                    *reinterpret_cast<u32x4 *>(to + 16 * e) = u32x4{to_bf16_pair(v[8 * e], v[8 * e + 1]), to_bf16_pair(v[8 * e + 2], v[8 * e + 3]),
-                                                                                    to_bf16_pair(v[8 * e + 4], v[8 * e + 5]), to_bf16_pair(v[8 * e + 6], v[8 * e + 7])};
+                                    for (uint32_t e = 0; e < 4; ++e) *reinterpret_cast<f32x4 *>(to + 16 * e) = f32x4{v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]};
+                                } else {
+#pragma unroll
+                                    for (uint32_t e = 0; e < 2; ++e)
+                                        *reinterpret_cast<u32x4 *>(to + 16 * e) = u32x4{to_bf16_pair(v[8 * e], v[8 * e + 1]), to_bf16_pair(v[8 * e + 2], v[8 * e + 3]),
+                                                                                        to_bf16_pair(v[8 * e + 4], v[8 * e + 5]), to_bf16_pair(v[8 * e + 6], v[8 * e + 7])};
+                                }
                             }
                         }
                         lanes_exchange();
 #pragma unroll
                         for (uint32_t k = 0; k < kPass / kRows; ++k) {
-                            const u32x4 w = *reinterpret_cast<const u32x4 *>(corner + (kRows * k + s_row) * kPitch + 4 * (lane % kLanes) * 4);
+                            const u32x4 w = *reinterpret_cast<const u32x4 *>(corner + (kRows * k + s_row) * kPitch + 16 * (lane % kLanes));
                             const uint32_t m = p.m0 + 32 * (TM * wm + i) + kPass * pass + kRows * k + s_row;
                             typename Out::type *to = c + m * ldc + n;
                             if (streams && stored) {
@@ -421,9 +431,9 @@ __global__ __launch_bounds__(256) void mx4_join_kernel(Mx4GemmArgs g, uint32_t s
 
 // Which tile a product takes, and into how many parts its contraction is cut, by an estimate of the time in us: `base` is a launch; `alone` a stage of workgroups that nothing else slows down,
 // `resident` of them on a compute unit; `busy` what a stage costs per workgroup of a unit where all units have some (of the last workgroups' unevenness over the units `uneven` counts); `store` the
-// stores of 256 tiles.  Fitted to 188 sizes (130 for the largest tile) of 33 .. 16384 x 64 .. 8192 x 64 .. 8192, bf16 results: 8 - 10 % (standard deviation).  On these the chosen tile takes
-// 6.5 % longer than the best of eight that were tried.  16384 x 8192 x 8192: 256 x 256 510 us, 128 x 128 630, 64 x 64 940; 8192 x 4096 x 1024: 30, 30, 42; 4096 x 1024 x 8192: 47, 22, 30;
-// 1003 x 971 x 243: 9.6, 5.1, 4.0.
+// stores of 256 tiles, `store_lines` where a row of C is whole cache lines.  Fitted to 408 sizes (301 for the largest tile) of 33 .. 16384 x 64 .. 8192 x 64 .. 8192, half of them with whole lines,
+// bf16 results: 6 - 9 % (standard deviation).  On these the chosen tile takes 0.7 % longer than the best one, at worst 17 % (13450 x 3516 x 1101), but for some of a few us.
+// 16384 x 8192 x 8192: 256 x 256 480 - 500 us, 128 x 128 628, 64 x 64 940; 8192 x 4096 x 1024: 27 - 30, 28 - 33, 42; 4096 x 1024 x 8192: 49, 22, 32; 1003 x 971 x 243: 10.4, 5.1, 4.1.
 // The largest tile's eight waves load for themselves; beside the others are four that only load (64 x 8192 x 8192 in tiles of 64 x 64: 12.8 us without them, 10 with).  128 x 128 has three stages
 // and the unit for itself: a stage more on its way counts for more than a second workgroup with two stages where each unit has one tile (4096 x 1024 x 8192: 26 us), and for less in a
 // row of tiles with few stages each (8192 x 4096 x 1024: 29 us).
@@ -431,17 +441,17 @@ __global__ __launch_bounds__(256) void mx4_join_kernel(Mx4GemmArgs g, uint32_t s
 struct Mx4Tile {
     uint32_t bm, bn, resident;
     bool cut;
-    double base, alone, busy, uneven, store;
+    double base, alone, busy, uneven, store, store_lines;
 };
 static constexpr Mx4Tile kMx4Tiles[] = {
-    {256, 256, 1, false, -1.274, 0.622, 2.371, 0.397, 9.878}, {128, 128, 1, true, 2.723, 0.344, 0.646, 0.501, 1.638}, {64, 64, 2, true, 2.972, 0.161, 0.224, 0.81, 0.45},
+    {256, 256, 1, false, -0.109, 1.199, 2.024, 0.591, 10.182, 8.107}, {128, 128, 1, true, 2.632, 0.085, 0.597, 0.566, 1.92, 1.404}, {64, 64, 2, true, 2.979, 0.012, 0.229, 0.848, 0.519, 0.46},
 };
 static double cost(const Mx4Tile &t, uint32_t splits, uint32_t M, uint32_t N, uint32_t K) {
     const uint32_t stages = (K + 255) / 256;
     const uint64_t items = static_cast<uint64_t>((M + t.bm - 1) / t.bm) * ((N + t.bn - 1) / t.bn) * splits, units = (items + 255) / 256, rounds = (items + 256 * t.resident - 1) / (256 * t.resident);
     const double per_unit = static_cast<double>(items) / 256.0, steps = (stages + splits - 1) / splits;
     const double alone = t.alone * steps * static_cast<double>(rounds), busy = t.busy * steps * (per_unit + t.uneven * (static_cast<double>(units) - per_unit));
-    const double whole = t.base + (alone > busy ? alone : busy) + t.store * (per_unit > 1.0 ? per_unit : 1.0);
+    const double whole = t.base + (alone > busy ? alone : busy) + (N % 64 == 0 ? t.store_lines : t.store) * (per_unit > 1.0 ? per_unit : 1.0);
     return splits > 1 ? whole + 3.2 + 2e-6 * splits * M * N : whole;   // (8 bytes of a part at 4 TB/s)
 }
 struct Mx4Choice {
