@@ -80,8 +80,9 @@ struct Eight {
             for (uint32_t i = 0; i < kWords; ++i) w[i] = move ? (i + by < kWords ? w[i + by] : 0u) : w[i];
         }
     }
+    template <bool SHORT = true>
     __device__ __forceinline__ void load(const typename T::type *row, uint32_t col, uint32_t cols) {
-        fetch<true>(row, col, cols);
+        fetch<SHORT>(row, col, cols);
         settle(missing(col, cols));
     }
     __device__ __forceinline__ void clear() {

@@ -10,6 +10,9 @@
 // Pieces are XOR-swizzled on their way in, so that the 16 that one read takes at a time lie on different ones of the 64 banks.  The B operand comes first in the instruction, and its
 // tiles' row i is column 16 (i / 4 % 2) + 4 (i / 8) + i % 4: a lane then holds 16 neighbours of a row of C.
 //
+// 16384 x 8192 x 8192: 480 - 500 us, 4.5 PFLOP/s, the matrix cores busy 59 % of the time at a clock that the power limit sets: the instructions alone take 325 us, reading their fragments adds 65, the
+// loads 60.  8192 x 4096 x 1024: 27 - 30 us; stores alone 13, products 10, loads 7, which all but add up.
+//
 // The fragments of a step are read while the step before is multiplied; a stage's last step is multiplied behind the barrier of the next one, under that one's first reads and loads.  A
 // workgroup goes on to its next tile without a break: the loads run ahead of the products by S - 1 stages, whosever they are, and a tile's stores pass under the next one's products.
 #include <type_traits>
@@ -402,7 +405,7 @@ void mx4_gemm_kernel(typename std::conditional<PAIR, Mx4PairArgs, Mx4TileArgs>::
     }
 }
 
-// The parts of a split contraction, added in order.
+// The parts of a split contraction, added in order.  512 x 512 x 65536 in four parts: 5.0 us after a product of 25.
 template <typename T>
 __global__ __launch_bounds__(256) void mx4_join_kernel(Mx4GemmArgs g, uint32_t splits) {
     const uint32_t n = 4 * (blockIdx.x * 64 + (threadIdx.x & 63u)), m = blockIdx.y * 4 + (threadIdx.x >> 6);

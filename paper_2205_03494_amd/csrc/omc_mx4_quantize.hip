@@ -6,6 +6,8 @@
 // Along columns a wave takes 32 rows x 128 columns, a lane two columns of them, so that a lane holds two whole blocks and no lane needs another's
 // values; the codes of a workgroup's 256 rows go through LDS, so that 128 bytes of a column are written together.  Where both directions are asked for, 16 lanes compare
 // their largest magnitudes of a row, from the same registers.
+// 8192 x 4096 from memory: along rows 28 us in fp32 (5.4 TB/s), 18.5 in bf16 (4.6); along columns 32 and 21; both 37 and 30 (3.4 TB/s: codes of 64 and scales of 2 bytes a row and tile are parts
+// of cache lines; tiles of 128 x 256 take as long).  16384 x 8192 in bf16 along rows, with the rounded values: 100 us, 6.1 TB/s.
 #include <type_traits>
 
 #include "omc_mx4.h"
@@ -83,6 +85,7 @@ __device__ __forceinline__ void reorder_scales(const Mx4Reorder &re, uint32_t bl
 }
 static uint32_t reorder_blocks(const Mx4Reorder &re, uint32_t rows) { return re.image ? (re.rows + rows - 1) / rows * ((mx4_padded(re.cols) + 255) / 256) : 0u; }
 
+// 24576 rows of 8192 values: 8.8 us, as a launch of its own (omc_mx4_gemm); elsewhere it is part of a rounding's.
 __global__ __launch_bounds__(256) void mx4_reorder_kernel(Mx4Reorder a, Mx4Reorder b, uint32_t blocks_a) {
     if (blockIdx.x < blocks_a) reorder_scales<256>(a, blockIdx.x);
     else reorder_scales<256>(b, blockIdx.x - blocks_a);
