@@ -3,7 +3,7 @@
 // y = (x - mean) rstd gamma + beta; backward, with h = (x - mean) rstd and u = dy gamma: dx = rstd (u - mean(u) - h mean(u h)), dgamma = sum over rows of dy h, dbeta of dy.
 //
 // Bound by memory: a row is read once and stays in registers, eight neighbours a lane and piece, between the sum of its values, the sum of their squared distances from the mean, and
-// the result.  Forward, 32768 x 4096 in bf16 93 - 99 us, 5.6 TB/s; 8192 x 1024, fp32 to bf16, 9.5 us, 5.3 TB/s; 1 x 512 2.1 us, of which an empty launch takes 2.0 in a graph.  Backward, 32768 x 4096
+// the result.  Forward, 32768 x 4096 in bf16 93 - 99 us, 5.6 TB/s; 8192 x 1024, fp32 to bf16, 9.5 us, 5.3 TB/s; 1 x 512 2.1 us.  Backward, 32768 x 4096
 // 143 us and 5 for the sums of partial sums, 5.6 TB/s; 8192 x 1024 with x in fp32 20 us; 1 x 512 2.5 us.  8, 16, 32 or 64 lanes take a row of up to 64, 128, 256 or 1024 values, 2, 4, 8 or 16 waves up to 16384; longer rows are read
 // again for every sum.
 // Backward, a thread keeps the same columns of all rows that its workgroup takes, so that the sums over the rows (dgamma, dbeta) stay in registers too; every workgroup leaves one row of
