@@ -103,6 +103,9 @@ PRODUCTS = [(7242, 1702, 3983), (2213, 5436, 3864), (7859, 3827, 3283), (3814, 7
             (644, 8567, 35), (2931, 1062, 320), (471, 6654, 1532), (332, 648, 25899), (641, 359, 26001), (34, 33, 5207), (37, 37, 4868),
             (260, 150, 9001)]
 
+# Results of 32 MB and more in bf16, whose rows are whole cache lines, in every tile; whole tiles and not.
+LARGE_RESULTS = [(8192, 2048, 300), (8190, 2112, 1000), (4097, 4096, 300), (262145, 64, 40)]
+
 # Backward passes: few rows in either product, both together in either tile, apart.
 BACKWARD = [(1, 1, 1, 0), (1, 64, 96, 0), (3, 33, 65, 1), (40, 96, 300, 0), (128, 64, 64, 0), (129, 257, 130, 3), (300, 520, 70, 0), (1003, 243, 97, 1),
             (2100, 128, 384, 0), (257, 65, 700, 1), (4001, 600, 1500, 0), (140001, 33, 40, 0), (2990, 1100, 1555, 1), (2048, 8192, 2304, 0),

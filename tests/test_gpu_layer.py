@@ -491,10 +491,19 @@ def values_on_device(codes, scales, rows, cols):
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("shape", ref.PRODUCTS)
 def test_every_tile(shape, dtype):
-    M, N, K = shape
+    product_is_right(*shape, dtype, 3)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("shape", ref.LARGE_RESULTS)
+def test_results_larger_than_the_caches(shape, dtype):
+    product_is_right(*shape, dtype, 0)
+
+
+def product_is_right(M, N, K, dtype, pad):
     a, b = [[torch.from_numpy(x.reshape(-1)).cuda() for x in random_codes(rows, K, rows + K)] for rows in (M, N)]
     bias = torch.randn(N, device="cuda", generator=torch.Generator("cuda").manual_seed(1))
-    cw, c = empty(M, N, dtype, 3)
+    cw, c = empty(M, N, dtype, pad)
     whole, ws = workspace(omc.omc_mx4_gemm_workspace_bytes(M, N, K))
     omc.omc_mx4_gemm(*a, *b, bias, c, K, ws)
     av, bv = values_on_device(*a, M, K), values_on_device(*b, N, K)

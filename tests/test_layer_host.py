@@ -105,3 +105,7 @@ def test_every_tile_of_the_product_is_taken():
 
 def test_backward_passes_go_together_and_apart():
     assert {ref.pair_tile(M, N, K) for M, N, K, _ in ref.BACKWARD} == {-1, 1, 2} and ref.pair_tile(50001, 33, 20) == ref.pair_tile(20, 8192, 8192) == -1
+
+
+def test_large_results_in_every_tile():
+    assert {ref.product_tile(*shape)[0] for shape in ref.LARGE_RESULTS} == {0, 1, 2} and all(2 * M * N >= 1 << 25 and N % 64 == 0 for M, N, _ in ref.LARGE_RESULTS)
