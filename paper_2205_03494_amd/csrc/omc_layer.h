@@ -55,11 +55,13 @@ struct Mx4GemmArgs {
     uint32_t M, N, K;
     float *parts;                  // partial results of a split contraction
 };
-// c = a b^T + bias, c in bf16 or fp32; the operands' scales in the tiles' order.
+// c = a b^T + bias, c in bf16 or fp32; the operands' scales in the tiles' order.  whole: the contraction is not cut.
 size_t mx4_gemm_workspace(uint32_t M, uint32_t N, uint32_t K);   // bytes of parts
-int launch_mx4_gemm(const Mx4GemmArgs &ga, bool bf16, void *stream);
+int launch_mx4_gemm(const Mx4GemmArgs &ga, bool whole, bool bf16, void *stream);
+// Of a layer's backward pass, dX[M x K] over N and dW[K x N] over M: are both products uncut and in tiles; the tile in which such should go together, -1: each in a launch of its own.
+bool mx4_backward_whole(uint32_t M, uint32_t N, uint32_t K);
+int mx4_pair_tile(uint32_t M, uint32_t N, uint32_t K, bool sums);
 // Two products, the second one's result in fp32, in one launch, and in it dbias, whose columns are the second one's, from `count` rows of partial sums (dbias may be null).
-int mx4_pair_tile(uint32_t M, uint32_t N, uint32_t K, uint32_t M2, uint32_t N2, uint32_t K2, bool sums);   // the tile they should take together; -1: each its own launch
 int launch_mx4_pair(int tile, const Mx4GemmArgs &ga, bool bf16, const Mx4GemmArgs &gb, const float *parts, uint32_t count, float *dbias, void *stream);
 // The same for few rows of a, with scales in the order of omc.h.  Where mx4_few_rounds, these may come as they are (`rows`), and are rounded on the way.
 constexpr uint32_t kMx4FewRows = 32;

@@ -32,7 +32,7 @@ static bool few(uint32_t M) { return M <= kMx4FewRows; }
 static uint64_t scale_bytes(uint32_t M, uint32_t rows, uint32_t K) { return few(M) ? mx4_scale_bytes(rows, K) : mx4_image_bytes(rows, K); }
 static uint64_t parts_bytes(uint32_t M, uint32_t N, uint32_t K) { return few(M) ? 0 : mx4_gemm_workspace(M, N, K); }
 static int launch_product(const Mx4GemmArgs &ga, bool bf16, void *stream) {
-    return few(ga.M) ? launch_mx4_few(ga, nullptr, bf16, stream) : launch_mx4_gemm(ga, bf16, stream);
+    return few(ga.M) ? launch_mx4_few(ga, nullptr, bf16, stream) : launch_mx4_gemm(ga, false, bf16, stream);
 }
 
 struct GemmLayout {
@@ -178,8 +178,8 @@ omc_status omc_mx4_linear_backward(const void *dY, uint64_t lddy, const void *X,
     const bool bf16 = type == OMC_BF16;
 
     // all roundings in one launch; dY's in one pass, unless its two products want their scales in different orders
-    const int together = dX && dW ? mx4_pair_tile(M, K, N, K, N, M, dbias != nullptr) : -1;
-    const bool dx_tiles = together >= 0 || !few(M), dw_tiles = together >= 0 || !few(K);
+    const bool whole = mx4_backward_whole(M, N, K), dx_tiles = whole || !few(M), dw_tiles = whole || !few(K);
+    const int together = whole && dX && dW ? mx4_pair_tile(M, N, K, dbias != nullptr) : -1;
     const Mx4Reorder weights = dX && dx_tiles ? Mx4Reorder{bytes(w_scales), l.w_image, K, N} : Mx4Reorder{};
     QuantArgs jobs[kMostJobs];
     uint32_t count = 1;
@@ -209,8 +209,8 @@ omc_status omc_mx4_linear_backward(const void *dY, uint64_t lddy, const void *X,
     const Mx4GemmArgs for_dw{{l.x_t, l.x_t_scales}, {l.dy_t, l.dy_t_scales}, nullptr, dW, N, K, N, M, l.parts};
     if (together >= 0) return from_hip(launch_mx4_pair(together, for_dx, dx_type == OMC_BF16, for_dw, l.sums, sum_rows, dbias, stream));
     if (dbias) rc = launch_column_sums(l.sums, sum_rows, N, N, dbias, nullptr, stream);
-    if (rc == 0 && dX) rc = launch_product(for_dx, dx_type == OMC_BF16, stream);
-    if (rc == 0 && dW) rc = launch_product(for_dw, false, stream);
+    if (rc == 0 && dX) rc = whole ? launch_mx4_gemm(for_dx, true, dx_type == OMC_BF16, stream) : launch_product(for_dx, dx_type == OMC_BF16, stream);
+    if (rc == 0 && dW) rc = whole ? launch_mx4_gemm(for_dw, true, false, stream) : launch_product(for_dw, false, stream);
     return from_hip(rc);
 }
 

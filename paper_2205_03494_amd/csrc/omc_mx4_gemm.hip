@@ -462,14 +462,14 @@ struct Mx4Choice {
     uint32_t splits;
     double cost;
 };
-static Mx4Choice choose(uint32_t M, uint32_t N, uint32_t K) {
+static Mx4Choice choose(uint32_t M, uint32_t N, uint32_t K, bool whole) {   // whole: not cut
     const uint32_t stages = (K + 255) / 256;
     Mx4Choice best{-1, 1, 0.0};
     for (int i = 0; i < 3; ++i) {
         const Mx4Tile &t = kMx4Tiles[i];
         const uint64_t tiles = static_cast<uint64_t>((M + t.bm - 1) / t.bm) * ((N + t.bn - 1) / t.bn);
         for (uint32_t splits = 1; splits <= 16; splits *= 2) {
-            if (splits > 1 && (!t.cut || tiles * splits > 256 || splits > stages)) break;
+            if (splits > 1 && (whole || !t.cut || tiles * splits > 256 || splits > stages)) break;
             const double c = cost(t, splits, M, N, K);
             if (best.tile < 0 || c < best.cost) best = Mx4Choice{i, splits, c};
         }
@@ -480,12 +480,12 @@ static Mx4Choice choose(uint32_t M, uint32_t N, uint32_t K) {
 }
 // Host only, not part of the interface: the tile's index, and 16 times the parts, that a product takes.
 extern "C" int omc_internal_mx4_tile(uint32_t M, uint32_t N, uint32_t K) {
-    const Mx4Choice c = choose(M, N, K);
+    const Mx4Choice c = choose(M, N, K, false);
     return c.tile + 16 * static_cast<int>(c.splits);
 }
 
 size_t mx4_gemm_workspace(uint32_t M, uint32_t N, uint32_t K) {
-    const Mx4Choice c = choose(M, N, K);
+    const Mx4Choice c = choose(M, N, K, false);
     return c.splits > 1 ? 4ull * c.splits * M * N : 0;
 }
 
@@ -512,8 +512,8 @@ static bool past_caches(const Mx4GemmArgs &g) {
 }
 
 template <typename T>
-static int launch(const Mx4GemmArgs &ga, hipStream_t st) {
-    const Mx4Choice c = choose(ga.M, ga.N, ga.K);
+static int launch(const Mx4GemmArgs &ga, bool whole, hipStream_t st) {
+    const Mx4Choice c = choose(ga.M, ga.N, ga.K, whole);
     const Mx4Tile &t = kMx4Tiles[c.tile];
     const uint32_t stages = (ga.K + 255) / 256;
     const bool streams = past_caches<T>(ga);
@@ -531,23 +531,35 @@ static int launch(const Mx4GemmArgs &ga, hipStream_t st) {
     return static_cast<int>(hipGetLastError());
 }
 
-// The tile in which both go together, uncut, or -1 where by the estimate each takes less in its best one, with a launch of its own and one for the sums.  Backward of a linear layer with its bias,
-// 64 x 64 x 64: 13.4 us in four launches, 8.9 in two; 1003 x 971 x 243 in fp32: 16.9 and 11.1; 4057 x 832 x 562 in bf16: 24.4 and 19.2;
-// 8192 x 1024 x 4096: 78.7 and 75.3; 4096 x 2048 x 2048: 46.2 and 41.3.
-int mx4_pair_tile(uint32_t M, uint32_t N, uint32_t K, uint32_t M2, uint32_t N2, uint32_t K2, bool sums) {
-    double best = choose(M, N, K).cost + choose(M2, N2, K2).cost + (sums ? 2.5 : 0.0);
+// Tile in which two products of M x N over K and M2 x N2 over K2 take the least time together, uncut, and that time.
+static int best_pair(uint32_t M, uint32_t N, uint32_t K, uint32_t M2, uint32_t N2, uint32_t K2, double &time) {
     int tile = -1;
     for (int i = 1; i < 3; ++i) {
         const double c = cost(kMx4Tiles[i], 1, M, N, K) + cost(kMx4Tiles[i], 1, M2, N2, K2) - kMx4Tiles[i].base;
-        if (c <= best) {
-            best = c;
+        if (tile < 0 || c <= time) {
+            time = c;
             tile = i;
         }
     }
     return tile;
 }
-// Host only, not part of the interface: that tile's index for the backward pass of a linear layer.
-extern "C" int omc_internal_mx4_pair_tile(uint32_t M, uint32_t N, uint32_t K) { return mx4_pair_tile(M, K, N, K, N, M, true); }
+// Both products of a backward pass are uncut and in tiles, so that they can go together, where by the estimate that takes no more than each its own way, with a launch of its own and one for dbias' sums.
+// Asked of the sizes alone: tiles add up the contraction in the same order, whichever they are, so that a gradient's bits do not depend on what is asked for beside it.  Backward of a linear layer with its bias,
+// 64 x 64 x 64: 13.4 us in four launches, 8.9 in two; 1003 x 971 x 243 in fp32: 16.9 and 11.1; 4057 x 832 x 562 in bf16: 24.4 and 19.2;
+// 8192 x 1024 x 4096: 78.7 and 75.3; 4096 x 2048 x 2048: 46.2 and 41.3.
+constexpr double kSumsLaunch = 2.5;
+bool mx4_backward_whole(uint32_t M, uint32_t N, uint32_t K) {
+    double together;
+    best_pair(M, K, N, K, N, M, together);
+    return together <= choose(M, K, N, false).cost + choose(K, N, M, false).cost + kSumsLaunch;
+}
+int mx4_pair_tile(uint32_t M, uint32_t N, uint32_t K, bool sums) {
+    double together;
+    const int tile = best_pair(M, K, N, K, N, M, together);
+    return together <= choose(M, K, N, true).cost + choose(K, N, M, true).cost + (sums ? kSumsLaunch : 0.0) ? tile : -1;
+}
+// Host only, not part of the interface: the tile in which both products of a backward pass with its bias go together; -1: each in a launch of its own.
+extern "C" int omc_internal_mx4_pair_tile(uint32_t M, uint32_t N, uint32_t K) { return mx4_backward_whole(M, N, K) ? mx4_pair_tile(M, N, K, true) : -1; }
 
 template <typename T>
 static int launch_pair(int tile, const Mx4GemmArgs &ga, const Mx4GemmArgs &gb, const ColumnSums &sums, hipStream_t st) {
@@ -567,9 +579,9 @@ int launch_mx4_pair(int tile, const Mx4GemmArgs &ga, bool bf16, const Mx4GemmArg
     return bf16 ? launch_pair<BF16>(tile, ga, gb, sums, st) : launch_pair<F32>(tile, ga, gb, sums, st);
 }
 
-int launch_mx4_gemm(const Mx4GemmArgs &ga, bool bf16, void *stream) {
+int launch_mx4_gemm(const Mx4GemmArgs &ga, bool whole, bool bf16, void *stream) {
     hipStream_t st = static_cast<hipStream_t>(stream);
-    return bf16 ? launch<BF16>(ga, st) : launch<F32>(ga, st);
+    return bf16 ? launch<BF16>(ga, whole, st) : launch<F32>(ga, whole, st);
 }
 
 }  // namespace omc
