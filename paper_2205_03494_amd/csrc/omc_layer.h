@@ -28,6 +28,7 @@ struct Mx4Reorder {
     uint32_t rows, cols;
 };
 
+constexpr uint32_t kSumRows = 64;
 struct QuantArgs {
     const void *x;
     uint64_t ldx;
@@ -36,13 +37,12 @@ struct QuantArgs {
     uint8_t *codes_t, *scales_t;   // blocks along a column; may be null
     void *values;                  // may be null
     uint64_t ldv;
-    float *colsum;                 // partial sums of the columns, a row of them for every tile of rows (mx4_tile_height); may be null
+    float *colsum;                 // partial sums of the columns, a row of them for every kSumRows rows (room for whole tiles of 256 rows); may be null
     bool images;                   // scales and scales_t in the tiles' order
     Mx4Reorder also;               // another matrix' scales, by the same launch (along rows only; see launch_mx4_tiles)
 };
 // Several matrices in one launch, in any directions but without values, and another one's scales.
 constexpr uint32_t kMostJobs = 3;
-uint32_t mx4_tile_height(const QuantArgs *args, uint32_t count);   // rows of a tile of such a launch; its columns' sums are that many rows' each, 256 / height to every 256 rows
 int launch_mx4_tiles(const QuantArgs *args, uint32_t count, const Mx4Reorder &also, bool bf16, void *stream);
 int launch_mx4_reorder(const Mx4Reorder &a, const Mx4Reorder &b, void *stream);
 int launch_mx4_quantize(const QuantArgs &qa, bool bf16, void *stream);   // no sums

@@ -84,7 +84,7 @@ static BackwardLayout backward_layout(uint8_t *ws, uint32_t M, uint32_t N, uint3
     l.x_t = p.take(mx4_code_bytes(K, M));
     l.x_t_scales = p.take(mx4_image_bytes(K, M));
     l.w_image = p.take(mx4_image_bytes(K, N));
-    l.sums = reinterpret_cast<float *>(p.take(4ull * ((M + 255) / 256 * 4) * N));
+    l.sums = reinterpret_cast<float *>(p.take(4ull * ((M + 255) / 256 * (256 / kSumRows)) * N));
     const uint64_t dx = parts_bytes(M, K, N), dw = parts_bytes(K, N, M);
     l.parts = reinterpret_cast<float *>(p.take(dx > dw ? dx : dw));
     l.bytes = p.used;
@@ -204,7 +204,7 @@ omc_status omc_mx4_linear_backward(const void *dY, uint64_t lddy, const void *X,
         rc = launch_mx4_tiles(jobs, count, weights, bf16, stream);
     }
     if (rc != 0) return from_hip(rc);
-    const uint32_t sum_rows = (M + 255) / 256 * (256 / mx4_tile_height(jobs, count));
+    const uint32_t sum_rows = (M + kSumRows - 1) / kSumRows;
     const Mx4GemmArgs for_dx{{l.dy, l.dy_scales}, {bytes(w_codes), dx_tiles ? l.w_image : bytes(w_scales)}, nullptr, dX, lddx, M, K, N, l.parts};
     const Mx4GemmArgs for_dw{{l.x_t, l.x_t_scales}, {l.dy_t, l.dy_t_scales}, nullptr, dW, N, K, N, M, l.parts};
     if (together >= 0) return from_hip(launch_mx4_pair(together, for_dx, dx_type == OMC_BF16, for_dw, l.sums, sum_rows, dbias, stream));

@@ -102,7 +102,9 @@ void mx4_gemm_kernel(typename std::conditional<PAIR, Mx4PairArgs, Mx4TileArgs>::
         groups = ta.groups;
         items += ta.second.tiles_m * ta.second.tiles_n;
         if (blockIdx.x >= groups) {
-            column_sums<NW + LOADERS, 4>(ta.sums, blockIdx.x - groups, reinterpret_cast<float(*)[32]>(lds));
+            float(*part)[32] = reinterpret_cast<float(*)[32]>(lds);
+            if (ta.sums.count <= 128) column_sums<NW + LOADERS, 2>(ta.sums, blockIdx.x - groups, part);
+            else column_sums<NW + LOADERS, 8>(ta.sums, blockIdx.x - groups, part);
             return;
         }
     }

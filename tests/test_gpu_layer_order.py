@@ -44,3 +44,12 @@ def test_a_products_gradient_is_the_same_whatever_is_asked_for_beside_it(M, N, K
     for wanted in (("dx",), ("dw",), ("dx", "dw"), ("dx", "dbias"), ("dw", "dbias")):
         for name, got in gradients(*wanted).items():
             assert name == "dbias" or torch.equal(got, whole[name]), (name, "beside", wanted)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("M,N,K", SHAPES)
+def test_dbias_is_the_same_whatever_is_asked_for_beside_it(M, N, K, dtype):
+    gradients = backward_of(M, N, K, dtype)
+    whole = gradients("dx", "dw", "dbias")["dbias"]
+    for wanted in (("dbias",), ("dx", "dbias"), ("dw", "dbias")):
+        assert torch.equal(gradients(*wanted)["dbias"], whole), wanted
