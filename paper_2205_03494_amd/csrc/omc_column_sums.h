@@ -13,11 +13,11 @@ struct ColumnSums {
 
 // A workgroup takes 32 columns and the rows in 16 shares, as many as it has waves at a time: sixteen lanes of a share take two columns each, so that the groups of sixteen lanes read a cache line of 64
 // rows between them, and CHAINS such reads are on their way together.  The chains, the groups of a share and the shares are joined in order.  The order is the same for all numbers of waves, and for all of chains
-// from count / 64 on, or from 8 on: chains without a row add zeros.  Bound by the way to memory and back, since other XCDs' caches hold what it reads: 4 us for 16 rows or 512, of 1024 columns,
+// from count / 64 on, or from 8 on: chains without a row add zeros.  FOURS: a row is four that lie one after the other, added first, in order.  Bound by the way to memory and back, since other XCDs' caches hold what it reads: 4 us for 16 rows or 512, of 1024 columns,
 // against 2.4 us for next to none.
-template <int WAVES, int CHAINS>
+template <int WAVES, int CHAINS, bool FOURS>
 __device__ __forceinline__ void column_sums(const ColumnSums &cs, uint32_t block, float (*part)[32]) {
-    constexpr uint32_t kShares = 16;
+    constexpr uint32_t kShares = 16, kEach = FOURS ? 4 : 1;
     const float *parts = cs.parts;
     const uint32_t count = cs.count, cols = cs.cols, width = cs.width;
     const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, col = block * 32 + 2 * (lane & 15u);
@@ -26,19 +26,28 @@ __device__ __forceinline__ void column_sums(const ColumnSums &cs, uint32_t block
     for (uint32_t share = wave; share < kShares; share += WAVES) {
         const uint32_t mine = 4 * share + (lane >> 4);
         float s[CHAINS][2] = {};
-        for (uint32_t first = 0; first < count; first += 4 * kShares * CHAINS) {
-            float v[CHAINS][2];
+        for (uint32_t first = 0; first + 4 * share < count; first += 4 * kShares * CHAINS) {
+            float v[CHAINS][kEach][2];
 #pragma unroll
-            for (uint32_t c = 0; c < CHAINS; ++c) {
-                const float *from = p + static_cast<uint64_t>(min(first + 4 * kShares * c + mine, count - 1)) * width;
-                v[c][0] = from[0];
-                v[c][1] = from[pair];
-            }
+            for (uint32_t c = 0; c < CHAINS; ++c)
+#pragma unroll
+                for (uint32_t k = 0; k < kEach; ++k) {
+                    const float *from = p + (static_cast<uint64_t>(min(first + 4 * kShares * c + mine, count - 1)) * kEach + k) * width;
+                    v[c][k][0] = from[0];
+                    v[c][k][1] = from[pair];
+                }
+#pragma unroll
+            for (uint32_t c = 0; c < CHAINS; ++c)
+#pragma unroll
+                for (uint32_t k = 1; k < kEach; ++k) {
+                    v[c][0][0] += v[c][k][0];
+                    v[c][0][1] += v[c][k][1];
+                }
 #pragma unroll
             for (uint32_t c = 0; c < CHAINS; ++c) {
                 const bool there = first + 4 * kShares * c + mine < count;
-                s[c][0] += there ? v[c][0] : 0.0f;
-                s[c][1] += there ? v[c][1] : 0.0f;
+                s[c][0] += there ? v[c][0][0] : 0.0f;
+                s[c][1] += there ? v[c][0][1] : 0.0f;
             }
         }
 #pragma unroll

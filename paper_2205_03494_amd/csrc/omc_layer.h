@@ -28,7 +28,6 @@ struct Mx4Reorder {
     uint32_t rows, cols;
 };
 
-constexpr uint32_t kSumRows = 64;
 struct QuantArgs {
     const void *x;
     uint64_t ldx;
@@ -37,12 +36,13 @@ struct QuantArgs {
     uint8_t *codes_t, *scales_t;   // blocks along a column; may be null
     void *values;                  // may be null
     uint64_t ldv;
-    float *colsum;                 // partial sums of the columns, a row of them for every kSumRows rows (room for whole tiles of 256 rows); may be null
+    float *colsum;                 // partial sums of the columns, a row of them for every tile of rows, of whole 256s (mx4_tile_height); may be null
     bool images;                   // scales and scales_t in the tiles' order
     Mx4Reorder also;               // another matrix' scales, by the same launch (along rows only; see launch_mx4_tiles)
 };
 // Several matrices in one launch, in any directions but without values, and another one's scales.
 constexpr uint32_t kMostJobs = 3;
+uint32_t mx4_tile_height(const QuantArgs *args, uint32_t count);   // rows of a tile of such a launch, 64 or 256
 int launch_mx4_tiles(const QuantArgs *args, uint32_t count, const Mx4Reorder &also, bool bf16, void *stream);
 int launch_mx4_reorder(const Mx4Reorder &a, const Mx4Reorder &b, void *stream);
 int launch_mx4_quantize(const QuantArgs &qa, bool bf16, void *stream);   // no sums
@@ -61,8 +61,8 @@ int launch_mx4_gemm(const Mx4GemmArgs &ga, bool whole, bool bf16, void *stream);
 // Of a layer's backward pass, dX[M x K] over N and dW[K x N] over M: are both products uncut and in tiles; the tile in which such should go together, -1: each in a launch of its own.
 bool mx4_backward_whole(uint32_t M, uint32_t N, uint32_t K);
 int mx4_pair_tile(uint32_t M, uint32_t N, uint32_t K, bool sums);
-// Two products, the second one's result in fp32, in one launch, and in it dbias, whose columns are the second one's, from `count` rows of partial sums (dbias may be null).
-int launch_mx4_pair(int tile, const Mx4GemmArgs &ga, bool bf16, const Mx4GemmArgs &gb, const float *parts, uint32_t count, float *dbias, void *stream);
+// Two products, the second one's result in fp32, in one launch, and in it dbias, whose columns are the second one's, from partial sums as for launch_column_sums (dbias may be null).
+int launch_mx4_pair(int tile, const Mx4GemmArgs &ga, bool bf16, const Mx4GemmArgs &gb, const float *parts, uint32_t count, bool fours, float *dbias, void *stream);
 // The same for few rows of a, with scales in the order of omc.h.  Where mx4_few_rounds, these may come as they are (`rows`), and are rounded on the way.
 constexpr uint32_t kMx4FewRows = 32;
 struct Mx4Rows {
@@ -73,8 +73,9 @@ struct Mx4Rows {
 bool mx4_few_rounds(uint32_t M, uint32_t N, uint32_t K);
 int launch_mx4_few(const Mx4GemmArgs &ga, const Mx4Rows *rows, bool bf16, void *stream);
 
-// Of `count` rows of partial sums, `width` floats each: the columns' sums, the first `cols` of them to out0, the others to out1 (either may be null).
-int launch_column_sums(const float *parts, uint32_t count, uint32_t cols, uint32_t width, float *out0, float *out1, void *stream);
+// Of `count` rows of partial sums, `width` floats each: the columns' sums, the first `cols` of them to out0, the others to out1 (either may be null).  fours: each is four rows that lie one after the other,
+// which are added first; 256 of them at most.  The order of all is fixed by count.
+int launch_column_sums(const float *parts, uint32_t count, bool fours, uint32_t cols, uint32_t width, float *out0, float *out1, void *stream);
 
 struct NormArgs {
     const void *x;

@@ -84,7 +84,7 @@ static BackwardLayout backward_layout(uint8_t *ws, uint32_t M, uint32_t N, uint3
     l.x_t = p.take(mx4_code_bytes(K, M));
     l.x_t_scales = p.take(mx4_image_bytes(K, M));
     l.w_image = p.take(mx4_image_bytes(K, N));
-    l.sums = reinterpret_cast<float *>(p.take(4ull * ((M + 255) / 256 * (256 / kSumRows)) * N));
+    l.sums = reinterpret_cast<float *>(p.take(4ull * ((M + 255) / 256 * 4) * N));
     const uint64_t dx = parts_bytes(M, K, N), dw = parts_bytes(K, N, M);
     l.parts = reinterpret_cast<float *>(p.take(dx > dw ? dx : dw));
     l.bytes = p.used;
@@ -204,11 +204,12 @@ omc_status omc_mx4_linear_backward(const void *dY, uint64_t lddy, const void *X,
         rc = launch_mx4_tiles(jobs, count, weights, bf16, stream);
     }
     if (rc != 0) return from_hip(rc);
-    const uint32_t sum_rows = (M + kSumRows - 1) / kSumRows;
+    const uint32_t sum_rows = (M + 255) / 256;
+    const bool fours = mx4_tile_height(jobs, count) == 64;
     const Mx4GemmArgs for_dx{{l.dy, l.dy_scales}, {bytes(w_codes), dx_tiles ? l.w_image : bytes(w_scales)}, nullptr, dX, lddx, M, K, N, l.parts};
     const Mx4GemmArgs for_dw{{l.x_t, l.x_t_scales}, {l.dy_t, l.dy_t_scales}, nullptr, dW, N, K, N, M, l.parts};
-    if (together >= 0) return from_hip(launch_mx4_pair(together, for_dx, dx_type == OMC_BF16, for_dw, l.sums, sum_rows, dbias, stream));
-    if (dbias) rc = launch_column_sums(l.sums, sum_rows, N, N, dbias, nullptr, stream);
+    if (together >= 0) return from_hip(launch_mx4_pair(together, for_dx, dx_type == OMC_BF16, for_dw, l.sums, sum_rows, fours, dbias, stream));
+    if (dbias) rc = launch_column_sums(l.sums, sum_rows, fours, N, N, dbias, nullptr, stream);
     if (rc == 0 && dX) rc = whole ? launch_mx4_gemm(for_dx, true, dx_type == OMC_BF16, stream) : launch_product(for_dx, dx_type == OMC_BF16, stream);
     if (rc == 0 && dW) rc = whole ? launch_mx4_gemm(for_dw, true, false, stream) : launch_product(for_dw, false, stream);
     return from_hip(rc);

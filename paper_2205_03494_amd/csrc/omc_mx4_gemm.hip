@@ -68,6 +68,7 @@ struct Mx4TileArgs {
 struct Mx4PairArgs {
     Mx4TileArgs first, second;
     uint32_t groups;
+    bool fours;
     ColumnSums sums;
 };
 
@@ -103,8 +104,10 @@ void mx4_gemm_kernel(typename std::conditional<PAIR, Mx4PairArgs, Mx4TileArgs>::
         items += ta.second.tiles_m * ta.second.tiles_n;
         if (blockIdx.x >= groups) {
             float(*part)[32] = reinterpret_cast<float(*)[32]>(lds);
-            if (ta.sums.count <= 128) column_sums<NW + LOADERS, 2>(ta.sums, blockIdx.x - groups, part);
-            else column_sums<NW + LOADERS, 8>(ta.sums, blockIdx.x - groups, part);
+            // (with eight chains of fours the tiles' waves spill; fours are 255 at most)
+            auto take = [&](auto chains, auto fours) { column_sums<NW + LOADERS, decltype(chains)::value, decltype(fours)::value>(ta.sums, blockIdx.x - groups, part); };
+            if (ta.fours) ta.sums.count <= 64 ? take(UintTag<1>{}, BoolTag<true>{}) : take(UintTag<4>{}, BoolTag<true>{});
+            else ta.sums.count <= 64 ? take(UintTag<1>{}, BoolTag<false>{}) : take(UintTag<8>{}, BoolTag<false>{});
             return;
         }
     }
@@ -564,10 +567,10 @@ int mx4_pair_tile(uint32_t M, uint32_t N, uint32_t K, bool sums) {
 extern "C" int omc_internal_mx4_pair_tile(uint32_t M, uint32_t N, uint32_t K) { return mx4_backward_whole(M, N, K) ? mx4_pair_tile(M, N, K, true) : -1; }
 
 template <typename T>
-static int launch_pair(int tile, const Mx4GemmArgs &ga, const Mx4GemmArgs &gb, const ColumnSums &sums, hipStream_t st) {
+static int launch_pair(int tile, const Mx4GemmArgs &ga, const Mx4GemmArgs &gb, const ColumnSums &sums, bool fours, hipStream_t st) {
     const uint32_t b = kMx4Tiles[tile].bm, most = 256 * kMx4Tiles[tile].resident;
     auto tiles = [b](const Mx4GemmArgs &g, bool streams) { return Mx4TileArgs{g, (g.M + b - 1) / b, (g.N + b - 1) / b, 1, (g.K + 255) / 256, streams}; };
-    Mx4PairArgs pa{tiles(ga, past_caches<T>(ga)), tiles(gb, past_caches<F32>(gb)), 0, sums};
+    Mx4PairArgs pa{tiles(ga, past_caches<T>(ga)), tiles(gb, past_caches<F32>(gb)), 0, fours, sums};
     const uint32_t items = pa.first.tiles_m * pa.first.tiles_n + pa.second.tiles_m * pa.second.tiles_n;
     pa.groups = items < most ? items : most;
     const dim3 grid(pa.groups + (sums.width + 31) / 32);
@@ -575,10 +578,10 @@ static int launch_pair(int tile, const Mx4GemmArgs &ga, const Mx4GemmArgs &gb, c
     else mx4_gemm_kernel<2, 2, 1, 1, 4, 4, 4, T, false, true><<<grid, dim3(512), 0, st>>>(pa);
     return static_cast<int>(hipGetLastError());
 }
-int launch_mx4_pair(int tile, const Mx4GemmArgs &ga, bool bf16, const Mx4GemmArgs &gb, const float *parts, uint32_t count, float *dbias, void *stream) {
+int launch_mx4_pair(int tile, const Mx4GemmArgs &ga, bool bf16, const Mx4GemmArgs &gb, const float *parts, uint32_t count, bool fours, float *dbias, void *stream) {
     hipStream_t st = static_cast<hipStream_t>(stream);
     const ColumnSums sums{parts, count, dbias ? gb.N : 0, dbias ? gb.N : 0, dbias, nullptr};
-    return bf16 ? launch_pair<BF16>(tile, ga, gb, sums, st) : launch_pair<F32>(tile, ga, gb, sums, st);
+    return bf16 ? launch_pair<BF16>(tile, ga, gb, sums, fours, st) : launch_pair<F32>(tile, ga, gb, sums, fours, st);
 }
 
 int launch_mx4_gemm(const Mx4GemmArgs &ga, bool whole, bool bf16, void *stream) {

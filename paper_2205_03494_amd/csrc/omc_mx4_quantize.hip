@@ -373,15 +373,20 @@ __global__ __launch_bounds__(2 * HIGH) void mx4_tiles_kernel(TileJobs jobs) {
         }
     }
     if (qa.colsum) {
-        static_assert(2 * HIGH == kWide * (HIGH / kSumRows) && kSumRows == 64, "a thread has a column of two waves");
-        const uint32_t c = threadIdx.x % kWide, part = threadIdx.x / kWide;
-        if (c0 + c < qa.cols) qa.colsum[(static_cast<uint64_t>(tr) * (HIGH / kSumRows) + part) * qa.cols + c0 + c] = sums_lds[2 * part][c] + sums_lds[2 * part + 1][c];
+        // of two waves, then of such pairs in order: here all of a tile's 256 rows, or a row of the four that column_sums adds the same way
+        const uint32_t c = threadIdx.x;
+        if (c < kWide && c0 + c < qa.cols) {
+            float s = sums_lds[0][c] + sums_lds[1][c];
+#pragma unroll
+            for (uint32_t w = 2; w < kWaves; w += 2) s += sums_lds[w][c] + sums_lds[w + 1][c];
+            qa.colsum[static_cast<uint64_t>(tr) * qa.cols + c0 + c] = s;
+        }
     }
 }
 
 // Fewer tiles of 256 rows than compute units: tiles of 64 (1000 x 777, both directions: 6.9 -> 5.5 us; 2048 x 2048 in fp32: 7.0 -> 6.4).  Of many these would store quarters of cache lines along the
 // columns (512 x 16384: 8.7 us, 10.1 with them).
-static uint32_t tile_height(const QuantArgs *args, uint32_t count) {
+uint32_t mx4_tile_height(const QuantArgs *args, uint32_t count) {
     uint64_t tiles = 0;
     for (uint32_t j = 0; j < count; ++j) tiles += static_cast<uint64_t>((args[j].rows + 255) / 256) * ((args[j].cols + kWide - 1) / kWide);
     return tiles < 256 ? 64 : 256;
@@ -405,7 +410,7 @@ static int launch_tiles_of(const QuantArgs *args, uint32_t count, const Mx4Reord
 }
 template <typename T>
 static int launch_tiles(const QuantArgs *args, uint32_t count, const Mx4Reorder &also, hipStream_t st) {
-    return tile_height(args, count) == 64 ? launch_tiles_of<T, 64>(args, count, also, st) : launch_tiles_of<T, 256>(args, count, also, st);
+    return mx4_tile_height(args, count) == 64 ? launch_tiles_of<T, 64>(args, count, also, st) : launch_tiles_of<T, 256>(args, count, also, st);
 }
 int launch_mx4_tiles(const QuantArgs *args, uint32_t count, const Mx4Reorder &also, bool bf16, void *stream) {
     hipStream_t st = static_cast<hipStream_t>(stream);

@@ -487,7 +487,7 @@ static int launch_grad(const NormGradArgs &given, hipStream_t st) {
     }
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || !na.parts) return static_cast<int>(e);
-    return launch_column_sums(na.parts, groups, na.cols, 2 * na.cols, na.dgamma, na.dbeta, st);
+    return launch_column_sums(na.parts, groups, false, na.cols, 2 * na.cols, na.dgamma, na.dbeta, st);
 }
 int launch_layer_norm_backward(const NormGradArgs &na, bool x_bf16, bool dy_bf16, void *stream) {
     hipStream_t st = static_cast<hipStream_t>(stream);
