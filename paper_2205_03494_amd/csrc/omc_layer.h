@@ -63,14 +63,14 @@ bool mx4_backward_whole(uint32_t M, uint32_t N, uint32_t K);
 int mx4_pair_tile(uint32_t M, uint32_t N, uint32_t K, bool sums);
 // Two products, the second one's result in fp32, in one launch, and in it dbias, whose columns are the second one's, from partial sums as for launch_column_sums (dbias may be null).
 int launch_mx4_pair(int tile, const Mx4GemmArgs &ga, bool bf16, const Mx4GemmArgs &gb, const float *parts, uint32_t count, bool fours, float *dbias, void *stream);
-// The same for few rows of a, with scales in the order of omc.h.  Where mx4_few_rounds, these may come as they are (`rows`), and are rounded on the way.
-constexpr uint32_t kMx4FewRows = 32;
+// The same for few rows of a (mx4_few, 32 at most), with scales in the order of omc.h.  Where mx4_few_rounds, these may come as they are (`rows`), and are rounded on the way.
 struct Mx4Rows {
     const void *x;
     uint64_t ldx;
     bool bf16;
 };
-bool mx4_few_rounds(uint32_t M, uint32_t N, uint32_t K);
+bool mx4_few(uint32_t M, uint32_t N, uint32_t K);
+bool mx4_few_rounds(uint32_t M, uint32_t K);
 int launch_mx4_few(const Mx4GemmArgs &ga, const Mx4Rows *rows, bool bf16, void *stream);
 
 // Of `count` rows of partial sums, `width` floats each: the columns' sums, the first `cols` of them to out0, the others to out1 (either may be null).  fours: each is four rows that lie one after the other,

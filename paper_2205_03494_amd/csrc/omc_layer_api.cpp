@@ -28,11 +28,9 @@ struct Parts {
 static const uint8_t *bytes(const void *p) { return static_cast<const uint8_t *>(p); }
 
 // A product's way: few rows of the first operand, or tiles, whose scales are reordered first.
-static bool few(uint32_t M) { return M <= kMx4FewRows; }
-static uint64_t scale_bytes(uint32_t M, uint32_t rows, uint32_t K) { return few(M) ? mx4_scale_bytes(rows, K) : mx4_image_bytes(rows, K); }
-static uint64_t parts_bytes(uint32_t M, uint32_t N, uint32_t K) { return few(M) ? 0 : mx4_gemm_workspace(M, N, K); }
+static uint64_t parts_bytes(uint32_t M, uint32_t N, uint32_t K) { return mx4_few(M, N, K) ? 0 : mx4_gemm_workspace(M, N, K); }
 static int launch_product(const Mx4GemmArgs &ga, bool bf16, void *stream) {
-    return few(ga.M) ? launch_mx4_few(ga, nullptr, bf16, stream) : launch_mx4_gemm(ga, false, bf16, stream);
+    return mx4_few(ga.M, ga.N, ga.K) ? launch_mx4_few(ga, nullptr, bf16, stream) : launch_mx4_gemm(ga, false, bf16, stream);
 }
 
 struct GemmLayout {
@@ -42,7 +40,7 @@ struct GemmLayout {
 };
 static GemmLayout gemm_layout(uint8_t *ws, uint32_t M, uint32_t N, uint32_t K) {
     GemmLayout l{};
-    if (few(M)) return l;
+    if (mx4_few(M, N, K)) return l;
     Parts p{ws};
     l.a_image = p.take(mx4_image_bytes(M, K));
     l.b_image = p.take(mx4_image_bytes(N, K));
@@ -58,11 +56,12 @@ struct LinearLayout {
 };
 static LinearLayout linear_layout(uint8_t *ws, uint32_t M, uint32_t N, uint32_t K) {
     LinearLayout l{};
-    if (few(M) && mx4_few_rounds(M, N, K)) return l;
+    const bool few = mx4_few(M, N, K);
+    if (few && mx4_few_rounds(M, K)) return l;
     Parts p{ws};
     l.codes = p.take(mx4_code_bytes(M, K));
-    l.scales = p.take(scale_bytes(M, M, K));
-    if (!few(M)) l.w_image = p.take(mx4_image_bytes(N, K));
+    l.scales = p.take(few ? mx4_scale_bytes(M, K) : mx4_image_bytes(M, K));
+    if (!few) l.w_image = p.take(mx4_image_bytes(N, K));
     l.parts = reinterpret_cast<float *>(p.take(parts_bytes(M, N, K)));
     l.bytes = p.used;
     return l;
@@ -126,7 +125,7 @@ omc_status omc_mx4_gemm(const void *a_codes, const void *a_scales, const void *b
     if (l.bytes > 0 && !aligned(ws, 16)) return OMC_ERR_ALIGN;
     Mx4GemmArgs ga{{bytes(a_codes), bytes(a_scales)}, {bytes(b_codes), bytes(b_scales)}, bias, C, ldc, M, N, K, l.parts};
     int rc = 0;
-    if (!few(M)) {
+    if (!mx4_few(M, N, K)) {
         rc = launch_mx4_reorder({ga.a.scales, l.a_image, M, K}, {ga.b.scales, l.b_image, N, K}, stream);
         ga.a.scales = l.a_image;
         ga.b.scales = l.b_image;
@@ -147,14 +146,14 @@ omc_status omc_mx4_linear(const void *X, omc_type x_type, uint64_t ldx, const vo
     const LinearLayout l = linear_layout(static_cast<uint8_t *>(ws), M, N, K);
     if (l.bytes > 0 && (!ws || ws_bytes < l.bytes)) return OMC_ERR_WORKSPACE;
     if (l.bytes > 0 && !aligned(ws, 16)) return OMC_ERR_ALIGN;
-    const bool x_bf16 = x_type == OMC_BF16, y_bf16 = y_type == OMC_BF16;
-    const Mx4 w{bytes(w_codes), few(M) ? bytes(w_scales) : l.w_image};
+    const bool x_bf16 = x_type == OMC_BF16, y_bf16 = y_type == OMC_BF16, few = mx4_few(M, N, K);
+    const Mx4 w{bytes(w_codes), few ? bytes(w_scales) : l.w_image};
     const Mx4GemmArgs ga{{l.codes, l.scales}, w, bias, Y, ldy, M, N, K, l.parts};
     if (!l.codes) {
         const Mx4Rows rows{X, ldx, x_bf16};
         return from_hip(launch_mx4_few(ga, &rows, y_bf16, stream));
     }
-    const QuantArgs qa{X, ldx, M, K, l.codes, l.scales, nullptr, nullptr, nullptr, 0, nullptr, !few(M), {bytes(w_scales), l.w_image, N, K}};
+    const QuantArgs qa{X, ldx, M, K, l.codes, l.scales, nullptr, nullptr, nullptr, 0, nullptr, !few, {bytes(w_scales), l.w_image, N, K}};
     const int rc = launch_mx4_quantize(qa, x_bf16, stream);
     return from_hip(rc != 0 ? rc : launch_product(ga, y_bf16, stream));
 }
@@ -178,7 +177,7 @@ omc_status omc_mx4_linear_backward(const void *dY, uint64_t lddy, const void *X,
     const bool bf16 = type == OMC_BF16;
 
     // all roundings in one launch; dY's in one pass, unless its two products want their scales in different orders
-    const bool whole = mx4_backward_whole(M, N, K), dx_tiles = whole || !few(M), dw_tiles = whole || !few(K);
+    const bool whole = mx4_backward_whole(M, N, K), dx_tiles = whole || !mx4_few(M, K, N), dw_tiles = whole || !mx4_few(K, N, M);
     const int together = whole && dX && dW ? mx4_pair_tile(M, N, K, dbias != nullptr) : -1;
     const Mx4Reorder weights = dX && dx_tiles ? Mx4Reorder{bytes(w_scales), l.w_image, K, N} : Mx4Reorder{};
     QuantArgs jobs[kMostJobs];

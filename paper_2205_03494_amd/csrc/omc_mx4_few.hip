@@ -161,7 +161,17 @@ __global__ __launch_bounds__(512) void mx4_few_kernel(Mx4GemmArgs g, Mx4Rows row
 constexpr uint32_t kFusedRows = 16;
 constexpr uint64_t kFusedBytes = 8192;
 static uint64_t rounded_bytes(uint32_t M, uint32_t K) { return static_cast<uint64_t>(M) * (mx4_padded(K) / 32) * 17; }
-bool mx4_few_rounds(uint32_t M, uint32_t, uint32_t K) { return M <= kFusedRows && rounded_bytes(M, K) <= kFusedBytes; }
+bool mx4_few_rounds(uint32_t M, uint32_t K) { return M <= kFusedRows && rounded_bytes(M, K) <= kFusedBytes; }
+
+// Up to 32 rows, unless the contraction is long and B narrow: it is cut into four waves' shares here, whose units of 256 take 0.24 us each one after the other (0.44 with more than 16 rows, since the ring
+// has two stages then), while tiles cut it over the whole chip.  Linear layers in bf16, us, here and in tiles, 16 rows: 16 x 32768 13.1 and 14.5, 16 x 49152 19.8 and 15.7, 33 x 1048576 518 and 93, 2048 x 20480
+// 18.3 and 17.7, 2048 x 49152 34.0 and 26.5; wider ones are bound by the weights' way through memory, 4096 x 49152 39.5 and 40.8, 8192 x 49152 70 and 69 (one row 50).  32 rows: 512 x 16384 12.8 and 14.8, 16 x 24576
+// 16.2 and 14.2, 512 x 32768 22.9 and 16.8, 33 x 1048576 749 and 93, 4096 x 24576 27.5 and 25.2, 8192 x 16384 31.3 and 30.3, 8192 x 28672 53.6 and 43.5.
+constexpr uint32_t kLongOf16 = 40960, kLongOf32 = 20480, kWide = 2048;
+bool mx4_few(uint32_t M, uint32_t N, uint32_t K) {
+    if (M <= 16) return K <= kLongOf16 || N > kWide;
+    return M <= 32 && K <= kLongOf32;
+}
 
 template <int MT, int S, bool FUSED, typename T, typename X>
 static int launch_rows(const Mx4GemmArgs &ga, const Mx4Rows &rows, hipStream_t st) {
