@@ -552,16 +552,25 @@ static int best_pair(uint32_t M, uint32_t N, uint32_t K, uint32_t M2, uint32_t N
 // Asked of the sizes alone: tiles add up the contraction in the same order, whichever they are, so that a gradient's bits do not depend on what is asked for beside it.  Backward of a linear layer with its bias,
 // 64 x 64 x 64: 13.4 us in four launches, 8.9 in two; 1003 x 971 x 243 in fp32: 16.9 and 11.1; 4057 x 832 x 562 in bf16: 24.4 and 19.2;
 // 8192 x 1024 x 4096: 78.7 and 75.3; 4096 x 2048 x 2048: 46.2 and 41.3.
+// A product of few rows would go another way by itself (mx4_few), which the estimate does not know.  Where its contraction is short both ways take the same within 1 or 2 us, and together pays; where
+// it is long it loses by itself more than both gain: all three gradients apart and together, and the product's alone in its own way and in tiles, 1 x 64 x 64 12.6 and 10.2,
+// dX 5.4 and 6.3 us; 32 x 1024 x 4096 17.9 and 16.2, 6.7 and 7.4; 16 x 4096 x 4096 29.0 and 25.7, 8.1 and 11.0; 1 x 8192 x 2048 30.5 and 29.5, 8.1 and 14.3; 8 x 8192 x 8192 68.9 and 71.3; dW of 1000 x 1000 x 32 15.2
+// and 11.9, 8.5 and 9.6; 8192 x 300 x 20 20.5 and 19.6, 12.5 and 17.0; 16000 x 300 x 32 27.8 and 28.4, 18.9 and 26.0.  Apart, dW of few rows has a rounding of dY to itself: 8192 x 4096 x 32 50.4 and 37.7, 28.6 and 31.4.
 constexpr double kSumsLaunch = 2.5;
+constexpr uint32_t kLongAlone = 4096;
+constexpr uint64_t kRoundedTwice = 1u << 23;
 bool mx4_backward_whole(uint32_t M, uint32_t N, uint32_t K) {
+    if (mx4_few(M, K, N) && N > kLongAlone) return false;
+    if (mx4_few(K, N, M) && M > kLongAlone && static_cast<uint64_t>(M) * N <= kRoundedTwice) return false;
     double together;
     best_pair(M, K, N, K, N, M, together);
     return together <= choose(M, K, N, false).cost + choose(K, N, M, false).cost + kSumsLaunch;
 }
+// (Of few rows, uncut tiles in a launch of their own take longer than the estimate says: 16 x 4096 x 4096 without dbias 30.3 us, 25.5 together.)
 int mx4_pair_tile(uint32_t M, uint32_t N, uint32_t K, bool sums) {
     double together;
     const int tile = best_pair(M, K, N, K, N, M, together);
-    return together <= choose(M, K, N, true).cost + choose(K, N, M, true).cost + (sums ? kSumsLaunch : 0.0) ? tile : -1;
+    return mx4_few(M, K, N) || mx4_few(K, N, M) || together <= choose(M, K, N, true).cost + choose(K, N, M, true).cost + (sums ? kSumsLaunch : 0.0) ? tile : -1;
 }
 // Host only, not part of the interface: the tile in which both products of a backward pass with its bias go together; -1: each in a launch of its own.
 extern "C" int omc_internal_mx4_pair_tile(uint32_t M, uint32_t N, uint32_t K) { return mx4_backward_whole(M, N, K) ? mx4_pair_tile(M, N, K, true) : -1; }
