@@ -9,6 +9,7 @@ a fixed batch and then answers single frames:
 """
 from __future__ import annotations
 
+import functools
 import math
 
 import torch
@@ -18,8 +19,19 @@ from . import omc
 EPS = 1e-5
 
 
+@functools.lru_cache(maxsize=1024)
+def _workspace_bytes(rows: int, width: int, inner: int, back: bool) -> int:
+    if not back:
+        return max(omc.omc_mx4_linear_workspace_bytes(rows, inner, width), omc.omc_mx4_linear_workspace_bytes(rows, width, inner))
+    return max(omc.omc_mx4_linear_backward_workspace_bytes(rows, inner, width), omc.omc_mx4_linear_backward_workspace_bytes(rows, width, inner),
+               omc.omc_layer_norm_backward_workspace_bytes(rows, width))
+
+
 class FeedForward:
-    """width -> inner -> width; `fmt` is the storage format of the matrices."""
+    """width -> inner -> width; `fmt` is the storage format of the matrices.
+
+    Work goes to the current stream.  A pass' workspace is its own (of the caching allocator, which keeps streams apart), so that frames may be answered on several
+    streams at once; step and refresh rewrite the variables that every pass reads, and backward the one gradient buffer, and a caller with several streams orders these."""
 
     def __init__(self, width: int, inner: int, fmt=None, seed: int = 0):
         self.width, self.inner = width, inner
@@ -48,7 +60,6 @@ class FeedForward:
             r, c = self.shapes[name]
             self.mx4[name] = [torch.empty(size(*s), dtype=torch.uint8, device="cuda") for s in ((r, c), (c, r))
                               for size in (omc.omc_mx4_code_bytes, omc.omc_mx4_scale_bytes)]
-        self.ws = torch.empty(0, dtype=torch.uint8, device="cuda")
         self.refresh()
 
     def _view(self, flat: torch.Tensor, name: str) -> torch.Tensor:
@@ -68,21 +79,15 @@ class FeedForward:
         for name, buffers in self.mx4.items():
             omc.omc_mx4_quantize(self.value(name), *buffers)
 
-    def _workspace(self, rows: int) -> torch.Tensor:
-        d, f = self.width, self.inner
-        need = max(omc.omc_mx4_linear_workspace_bytes(rows, f, d), omc.omc_mx4_linear_workspace_bytes(rows, d, f),
-                   omc.omc_mx4_linear_backward_workspace_bytes(rows, f, d), omc.omc_mx4_linear_backward_workspace_bytes(rows, d, f),
-                   omc.omc_layer_norm_backward_workspace_bytes(rows, d))
-        if self.ws.numel() < need:
-            self.ws = torch.empty(need, dtype=torch.uint8, device="cuda")
-        return self.ws
+    def _workspace(self, rows: int, back: bool) -> torch.Tensor:
+        return torch.empty(_workspace_bytes(rows, self.width, self.inner, back), dtype=torch.uint8, device="cuda")
 
     def forward(self, x: torch.Tensor, keep: bool = False) -> torch.Tensor:
         """x [frames, width] in fp32 -> the module's output in fp32; keep: what backward needs."""
         rows, half = x.shape[0], torch.bfloat16
-        ws = self._workspace(rows)
         y, h = torch.empty(rows, self.width, device="cuda", dtype=half), torch.empty(rows, self.inner, device="cuda", dtype=half)
         z = torch.empty(rows, self.width, device="cuda")
+        ws = self._workspace(rows, False)
         mean, rstd = (torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")) if keep else (None, None)
         omc.omc_layer_norm(x, self.value("gamma"), self.value("beta"), EPS, y, mean, rstd)
         omc.omc_mx4_linear(y, *self.mx4["w1"][2:], self.value("b1"), h, ws)
@@ -95,7 +100,7 @@ class FeedForward:
     def backward(self, dout: torch.Tensor) -> torch.Tensor:
         """The gradients of all variables into the flat gradient buffer; returns the input's."""
         x, mean, rstd, y, h, a = self.kept
-        ws = self._workspace(x.shape[0])
+        ws = self._workspace(x.shape[0], True)
         da, dy, dx = torch.empty_like(h), torch.empty_like(y), torch.empty_like(x)
         omc.omc_mx4_linear_backward((0.5 * dout).to(a.dtype), a, *self.mx4["w2"][:2], da, self.grad("w2"), self.grad("b2"), ws)
         s = torch.sigmoid(h.float())
