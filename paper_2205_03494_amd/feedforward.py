@@ -11,6 +11,7 @@ from __future__ import annotations
 
 import functools
 import math
+from typing import NamedTuple, Optional
 
 import torch
 
@@ -25,6 +26,22 @@ def _workspace_bytes(rows: int, width: int, inner: int, back: bool) -> int:
         return max(omc.omc_mx4_linear_workspace_bytes(rows, inner, width), omc.omc_mx4_linear_workspace_bytes(rows, width, inner))
     return max(omc.omc_mx4_linear_backward_workspace_bytes(rows, inner, width), omc.omc_mx4_linear_backward_workspace_bytes(rows, width, inner),
                omc.omc_layer_norm_backward_workspace_bytes(rows, width))
+
+
+class Kept(NamedTuple):
+    """What a forward pass leaves for its backward pass."""
+    x: torch.Tensor
+    x_version: Optional[int]               # torch's count of its changes in place
+    variables: int                         # which ones it was computed with
+    mean: torch.Tensor
+    rstd: torch.Tensor
+    y: torch.Tensor
+    h: torch.Tensor
+    a: torch.Tensor
+
+
+def _version(x: torch.Tensor) -> Optional[int]:
+    return None if x.is_inference() else x._version    # (inference tensors have none)
 
 
 class FeedForward:
@@ -49,6 +66,8 @@ class FeedForward:
         self.sb = torch.zeros((len(table), 2), device="cuda")
         self.values, self.grads = torch.zeros(aux, device="cuda"), torch.zeros(aux, device="cuda")
         self.states = []
+        self.kept: Optional[Kept] = None
+        self.variables = 0
         self.step_ws = torch.empty(self.plan.workspace_bytes, dtype=torch.uint8, device="cuda")
         g = torch.Generator(device="cuda").manual_seed(seed)
         for name, fan_in in (("w1", width), ("w2", inner)):
@@ -75,6 +94,7 @@ class FeedForward:
 
     def refresh(self) -> None:
         """The set in fp32 and its matrices in MX4, K x N blocked along N (input gradient) and N x K blocked along K (forward)."""
+        self.variables += 1
         omc.omc_decompress_set(self.arena, self.plan, self.sb, self.values)
         for name, buffers in self.mx4.items():
             omc.omc_mx4_quantize(self.value(name), *buffers)
@@ -83,7 +103,8 @@ class FeedForward:
         return torch.empty(_workspace_bytes(rows, self.width, self.inner, back), dtype=torch.uint8, device="cuda")
 
     def forward(self, x: torch.Tensor, keep: bool = False) -> torch.Tensor:
-        """x [frames, width] in fp32 -> the module's output in fp32; keep: what backward needs."""
+        """x [frames, width] in fp32 -> the module's output in fp32; keep: `kept` becomes what backward needs, x itself among it, which must
+        stay as it is until then."""
         rows, half = x.shape[0], torch.bfloat16
         y, h = torch.empty(rows, self.width, device="cuda", dtype=half), torch.empty(rows, self.inner, device="cuda", dtype=half)
         z = torch.empty(rows, self.width, device="cuda")
@@ -94,12 +115,21 @@ class FeedForward:
         a = h * torch.sigmoid(h)
         omc.omc_mx4_linear(a, *self.mx4["w2"][2:], self.value("b2"), z, ws)
         if keep:
-            self.kept = (x, mean, rstd, y, h, a)
+            self.kept = Kept(x, _version(x), self.variables, mean, rstd, y, h, a)
         return x + 0.5 * z
 
-    def backward(self, dout: torch.Tensor) -> torch.Tensor:
-        """The gradients of all variables into the flat gradient buffer; returns the input's."""
-        x, mean, rstd, y, h, a = self.kept
+    def backward(self, dout: torch.Tensor, kept: Optional[Kept] = None) -> torch.Tensor:
+        """The gradients of all variables into the flat gradient buffer; returns the input's.  Of the last forward pass with keep, or of the one that left `kept`."""
+        kept = self.kept if kept is None else kept
+        if kept is None:
+            raise RuntimeError("no forward pass with keep=True to go back through")
+        x, x_version, variables, mean, rstd, y, h, a = kept
+        if variables != self.variables:
+            raise RuntimeError("the forward pass was computed with other variables than the module now has")
+        if _version(x) != x_version:
+            raise RuntimeError("the forward pass' input was changed in place since")
+        if dout.shape != x.shape:
+            raise ValueError(f"the gradient of {tuple(x.shape)} outputs is expected, not {tuple(dout.shape)}")
         ws = self._workspace(x.shape[0], True)
         da, dy, dx = torch.empty_like(h), torch.empty_like(y), torch.empty_like(x)
         omc.omc_mx4_linear_backward((0.5 * dout).to(a.dtype), a, *self.mx4["w2"][:2], da, self.grad("w2"), self.grad("b2"), ws)

@@ -1,4 +1,4 @@
-"""The feed-forward module as callers use it: several streams."""
+"""The feed-forward module as callers use it: several streams, several passes under way, mistakes that are told."""
 import pytest
 import torch
 
@@ -29,3 +29,42 @@ def test_passes_on_two_streams_share_no_workspace(monkeypatch):
     spans = [[(w.data_ptr(), w.data_ptr() + w.numel()) for i, w in used if i == k and w.numel()] for k in (0, 1)]
     assert spans[0] and spans[1]
     assert all(a1 <= b0 or b1 <= a0 for a0, a1 in spans[0] for b0, b1 in spans[1])
+
+
+def test_two_passes_forward_then_both_back():
+    m = FeedForward(96, 260)
+    x, dout = [frames(40, i) for i in (1, 2)], [frames(40, i) for i in (3, 4)]
+    want = []
+    for i in (0, 1):
+        m.forward(x[i], keep=True)
+        want.append((m.backward(dout[i]), m.grads.clone()))
+    kept = []
+    for i in (0, 1):
+        m.forward(x[i], keep=True)
+        kept.append(m.kept)
+    for i in (0, 1):
+        dx = m.backward(dout[i], kept[i])
+        assert torch.equal(dx, want[i][0]) and torch.equal(m.grads, want[i][1])
+    assert torch.equal(m.backward(dout[1]), want[1][0])    # of the last pass, if none is named
+
+
+def test_backward_refuses_what_it_would_answer_wrongly():
+    m, x, dout = FeedForward(96, 260), frames(10, 1), frames(10, 2)
+    with pytest.raises(RuntimeError, match="no forward pass"):
+        m.backward(dout)
+    m.forward(x)
+    with pytest.raises(RuntimeError, match="no forward pass"):
+        m.backward(dout)
+    m.forward(x, keep=True)
+    x.mul_(2.0)
+    with pytest.raises(RuntimeError, match="changed"):
+        m.backward(dout)
+    m.forward(x, keep=True)
+    with pytest.raises(ValueError):
+        m.backward(frames(11, 2))
+    m.backward(dout)
+    m.step(omc.opt(omc.OMC_SGD, 0.1, t=1))
+    with pytest.raises(RuntimeError, match="other variables"):
+        m.backward(dout)
+    m.forward(x, keep=True)
+    m.backward(dout)
