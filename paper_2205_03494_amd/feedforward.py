@@ -166,8 +166,9 @@ def main() -> None:
         module.backward(diff * (2.0 / diff.numel()))
         module.step(omc.opt(omc.OMC_ADAM, a.lr, t=t))
         print(f"step {t}: mean square error {diff.square().mean().item():.6f}", flush=True)
-    frame = torch.cat([module.forward(x[i:i + 1]) for i in range(4)])
-    print(f"four frames one by one, largest difference from the batch: {(frame - module.forward(x)[:4]).abs().max().item():.3g}")
+    few = min(4, a.frames)
+    single = torch.cat([module.forward(x[i:i + 1]) for i in range(few)])
+    print(f"{few} frames one by one, largest difference from the batch: {(single - module.forward(x)[:few]).abs().max().item():.3g}")
 
 
 if __name__ == "__main__":

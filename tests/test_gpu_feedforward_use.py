@@ -1,8 +1,10 @@
 """The feed-forward module as callers use it: several streams, several passes under way, mistakes that are told."""
+import sys
+
 import pytest
 import torch
 
-from paper_2205_03494_amd import omc
+from paper_2205_03494_amd import feedforward, omc
 from paper_2205_03494_amd.feedforward import FeedForward
 
 pytestmark = pytest.mark.gpu
@@ -68,3 +70,10 @@ def test_backward_refuses_what_it_would_answer_wrongly():
         m.backward(dout)
     m.forward(x, keep=True)
     m.backward(dout)
+
+
+@pytest.mark.parametrize("count", [1, 3, 5])
+def test_program_with_few_frames(count, monkeypatch, capsys):
+    monkeypatch.setattr(sys, "argv", ["feedforward", "--width", "64", "--inner", "128", "--frames", str(count), "--steps", "2"])
+    feedforward.main()
+    assert "step 2: mean square error" in capsys.readouterr().out
