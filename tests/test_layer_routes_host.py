@@ -26,3 +26,8 @@ def test_a_product_of_few_rows_and_a_long_contraction_goes_its_own_way(M, N, K):
 def test_short_ones_go_together(M, N, K):
     """All three gradients of 16 x 4096 x 4096 take 25.7 us together, 29.0 apart; 8192 x 4096 x 32 37.7 and 50.4."""
     assert ref.pair_tile(M, N, K) > 0
+
+
+def test_gradients_larger_than_the_caches_in_either_tile():
+    from test_gpu_layer_paths import LARGE_GRADIENTS
+    assert {ref.pair_tile(*shape) for shape in LARGE_GRADIENTS} == {1, 2} and all(2 * M * K >= 1 << 25 and K % 64 == 0 for M, _, K in LARGE_GRADIENTS)
