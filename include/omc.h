@@ -455,10 +455,11 @@ omc_status omc_dw_update_recompress(const uint16_t *X, const uint16_t *dY, void 
  *     scales   omc_mx4_scale_bytes: row r begins at byte r * 4 * ceil(cols / 128), a byte e + 127 for every block; 255: its values are NaN
  * Rows are padded to whole multiples of 128 values with codes 0 and scales 0.  codes must be 16-byte aligned, scales 4-byte aligned; other
  * tensors here need only the alignment of their elements, and rows of theirs may lie apart (ld = elements from one row to the next, at least
- * a row's length).  A dimension must lie in 1 .. 2^24 (OMC_ERR_SIZE). */
+ * a row's length).  A dimension must lie in 1 .. 2^24, and of those of one matrix (for products M x N, M x K and N x K) the product in 1 .. 2^37
+ * (OMC_ERR_SIZE).  The size queries answer 0 for others; of a workspace 0 also means that none is needed, and not that the sizes are accepted. */
 typedef enum { OMC_F32 = 0, OMC_BF16 = 1 } omc_type; /* fp32, bfloat16 bit patterns; others are OMC_ERR_FORMAT */
 
-/* Bytes of the two buffers; 0 if a dimension is out of range. */
+/* Bytes of the two buffers; 0 if the sizes are out of range. */
 size_t omc_mx4_code_bytes(uint32_t rows, uint32_t cols);
 size_t omc_mx4_scale_bytes(uint32_t rows, uint32_t cols);
 
@@ -501,7 +502,7 @@ omc_status omc_mx4_linear(const void *X, omc_type x_type, uint64_t ldx, const vo
  *   dW                  device, K*N floats, or NULL: the gradient as omc_step_update_recompress takes it for a K x N variable.  X is not needed without it
  *   dbias               device, N floats, or NULL
  *   ws                  device workspace of omc_mx4_linear_backward_workspace_bytes(M, N, K) bytes, 16-byte aligned
- * At least one output (OMC_ERR_NULL).  Every sum's order is fixed by the sizes. */
+ * At least one output (OMC_ERR_NULL).  Every sum's order is fixed by the sizes: a gradient has the same bits whichever others are asked for. */
 size_t omc_mx4_linear_backward_workspace_bytes(uint32_t M, uint32_t N, uint32_t K);
 omc_status omc_mx4_linear_backward(const void *dY, uint64_t lddy, const void *X, uint64_t ldx, omc_type type, const void *w_codes,
                                    const void *w_scales, void *dX, omc_type dx_type, uint64_t lddx, float *dW, float *dbias, uint32_t M,
@@ -510,7 +511,7 @@ omc_status omc_mx4_linear_backward(const void *dY, uint64_t lddy, const void *X,
 /* ---- layer norm ---------------------------------------------------------------------------------
  * Its weights are the vectors that stay fp32 in a variable set (Sec. 2.4).  For every row x of `cols` values
  *     mean = sum x / cols,   rstd = 1 / sqrt(sum (x - mean)^2 / cols + eps),   y = (x - mean) * rstd * gamma + beta
- * in fp32, rounded once to y's type.  Rows and cols in 1 .. 2^24 (OMC_ERR_SIZE), eps finite and not negative (OMC_ERR_OPT).
+ * in fp32, rounded once to y's type.  Rows and cols in 1 .. 2^24, their product in 1 .. 2^37 (OMC_ERR_SIZE), eps finite and not negative (OMC_ERR_OPT).
  *   x, y          device, of x_type and y_type, row strides ldx and ldy
  *   gamma, beta   device, cols floats each; NULL: 1 and 0
  *   mean, rstd    device, a float for every row, for the backward pass; NULL: not kept */

@@ -5,7 +5,8 @@
 // instruction's operands takes half a line of a row at a time, which costs the load path as much as a whole one), and waits for nobody.  Lane l multiplies blocks 2 (l / 16) and
 // 2 (l / 16) + 1 of a unit of row l % 16, whose scales are two neighbouring bytes.
 // FUSED: A comes as it is and is rounded by every workgroup for itself into LDS, while B is on its way, which saves a launch and costs M K roundings in each.
-// 1 x 8192 x 8192: 8.6 us, 4.1 TB/s of weights; 1 x 4096 x 1024: 3.4 us; 29 x 8200 x 8192: 12.1 us and 2.5 for the rounding before, bound by the loads into LDS, of which half are A's.
+// 1 x 8192 x 8192: 8.6 us, 4.1 TB/s of weights; 1 x 4096 x 1024: 3.4 us; 29 x 8200 x 8192: 12.1 us and 2.5 for the rounding before.  There, with more than 16 rows, the ring has two stages:
+// a wave has one unit on its way while it multiplies another, eight round trips in a row.  What is loaded, B once and A for every 16 columns, 109 MB, would take a third of that time at the rate of the tiles' loads.
 #include "omc_mma.h"
 #include "omc_mx4.h"
 

@@ -14,7 +14,8 @@
 // loads 60.  8192 x 4096 x 1024: 27 - 30 us; stores alone 13, products 10, loads 7, which all but add up.
 //
 // The fragments of a step are read while the step before is multiplied; a stage's last step is multiplied behind the barrier of the next one, under that one's first reads and loads.  A
-// workgroup goes on to its next tile without a break: the loads run ahead of the products by S - 1 stages, whosever they are, and a tile's stores pass under the next one's products.
+// workgroup goes on to its next tile without a break: the loads run ahead of the products by S - 1 stages, whosever they are, and nothing waits for a tile's stores.  These overlap little all the same
+// where tiles have few stages: all waves of a unit convert and store at the same time, and its matrix cores idle meanwhile.
 #include <type_traits>
 
 #include "omc_mma.h"
@@ -440,7 +441,7 @@ __global__ __launch_bounds__(256) void mx4_join_kernel(Mx4GemmArgs g, uint32_t s
 // Which tile a product takes, and into how many parts its contraction is cut, by an estimate of the time in us: `base` is a launch; `alone` a stage of workgroups that nothing else slows down,
 // `resident` of them on a compute unit; `busy` what a stage costs per workgroup of a unit where all units have some (of the last workgroups' unevenness over the units `uneven` counts); `store` the
 // stores of 256 tiles, `store_lines` where a row of C is whole cache lines.  Fitted to 408 sizes (301 for the largest tile) of 33 .. 16384 x 64 .. 8192 x 64 .. 8192, half of them with whole lines,
-// bf16 results: 6 - 9 % (standard deviation).  On these the chosen tile takes 0.7 % longer than the best one, at worst 17 % (13450 x 3516 x 1101), but for some of a few us.
+// bf16 results: 6 - 9 % (standard deviation).  (The result's type is not asked for: fp32 results, dW's among them, are chosen for by the same figures.)  On these the chosen tile takes 0.7 % longer than the best one, at worst 17 % (13450 x 3516 x 1101), but for some of a few us.
 // 16384 x 8192 x 8192: 256 x 256 480 - 500 us, 128 x 128 628, 64 x 64 940; 8192 x 4096 x 1024: 27 - 30, 28 - 33, 42; 4096 x 1024 x 8192: 49, 22, 32; 1003 x 971 x 243: 10.4, 5.1, 4.1.
 // The largest tile's eight waves load for themselves; beside the others are four that only load (64 x 8192 x 8192 in tiles of 64 x 64: 12.8 us without them, 10 with).  128 x 128 has three stages
 // and the unit for itself: a stage more on its way counts for more than a second workgroup with two stages where each unit has one tile (4096 x 1024 x 8192: 26 us), and for less in a

@@ -6,8 +6,8 @@
 // Along columns a wave takes 32 rows x 128 columns, a lane two columns of them, so that a lane holds two whole blocks and no lane needs another's
 // values; the codes of a workgroup's 256 rows go through LDS, so that 128 bytes of a column are written together.  Where both directions are asked for, 16 lanes compare
 // their largest magnitudes of a row, from the same registers.
-// 8192 x 4096 from memory: along rows 28 us in fp32 (5.4 TB/s), 18.5 in bf16 (4.6); along columns 32 and 21; both 37 and 30 (3.4 TB/s: codes of 64 and scales of 2 bytes a row and tile are parts
-// of cache lines; tiles of 128 x 256 take as long).  16384 x 8192 in bf16 along rows, with the rounded values: 100 us, 6.1 TB/s.
+// 8192 x 4096 from memory: along rows 28 us in fp32 (5.4 TB/s), 18.5 in bf16 (4.6); along columns 32 and 21; both 37 and 30 (3.4 TB/s; memory sees every byte once, although codes of 64
+// and scales of 2 bytes a row and tile are parts of cache lines; waves wait 42 % of their time, and an LDS instruction has four clocks of bank conflicts; tiles of 128 x 256 take as long).  16384 x 8192 in bf16 along rows, with the rounded values: 100 us, 6.1 TB/s.
 #include <type_traits>
 
 #include "omc_mx4.h"
