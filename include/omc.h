@@ -508,6 +508,90 @@ omc_status omc_mx4_linear_backward(const void *dY, uint64_t lddy, const void *X,
                                    const void *w_scales, void *dX, omc_type dx_type, uint64_t lddx, float *dW, float *dbias, uint32_t M,
                                    uint32_t N, uint32_t K, void *ws, size_t ws_bytes, void *stream);
 
+/* ---- products on 8-bit integers ------------------------------------------------------------------
+ * I8: a row of values shares a scale.  With a the largest magnitude of the row,
+ *     s = a / 127 in fp32,   code_i = the whole number nearest to x_i / s, ties to even (saturating at 127 where s is subnormal),   value_i = s * code_i.
+ * A row of zeros has s = 0 and codes 0; a row with a value that is not finite has s = NaN and codes 0, and its values are NaN.
+ *
+ * A matrix of `rows` rows of `cols` values is held in two buffers.
+ *     codes    omc_i8_code_bytes: row r begins at byte r * 128 * ceil(cols / 128), a signed byte for every value, zeros behind them
+ *     scales   a float for every row
+ * codes must be 16-byte aligned; other tensors here and of the gated layer need only the alignment of their elements, and rows of theirs may lie apart (ld).  Dimensions as for MX4;
+ * K, along which two codes' products are added up in 32-bit integers, is at most 131071 (OMC_ERR_SIZE). */
+size_t omc_i8_code_bytes(uint32_t rows, uint32_t cols);   /* 0 if the sizes are out of range */
+
+/* A matrix to I8.
+ *   x              device, rows x cols values of `type`, row stride ldx
+ *   by_columns     0: a scale for every row (a token, a frame); codes of rows x cols, `rows` scales.  Otherwise a scale for every column (a channel of K x N weights):
+ *                  codes and scales are those of the transpose, cols x rows, `cols` scales
+ *   codes, scales  device, written whole, paddings too; must not overlap x
+ *   values         device or NULL, rows x cols of `type`, row stride ldv: what codes and scales stand for, rounded once to `type` */
+omc_status omc_i8_quantize(const void *x, omc_type type, uint32_t rows, uint32_t cols, uint64_t ldx, int by_columns, void *codes, float *scales, void *values, uint64_t ldv, void *stream);
+
+/* C[M x N] = A[M x K] * B[N x K]^T + bias on operands in I8: sums of whole numbers, exact, times A's row's scale, times B's row's, in fp32, rounded once to c_type.
+ *   bias     device, N floats, or NULL
+ *   C        device, row stride ldc
+ *   ws       device workspace of omc_i8_gemm_workspace_bytes(M, N, K) bytes, 16-byte aligned (may be 0: then ws may be NULL) */
+size_t omc_i8_gemm_workspace_bytes(uint32_t M, uint32_t N, uint32_t K);
+omc_status omc_i8_gemm(const void *a_codes, const float *a_scales, const void *b_codes, const float *b_scales, const float *bias, void *C, omc_type c_type, uint64_t ldc, uint32_t M, uint32_t N,
+                       uint32_t K, void *ws, size_t ws_bytes, void *stream);
+
+/* A layer's forward pass: Y[M x N] = Q(X) * W^T + bias, X[M x K] rounded to I8 along its rows on the way; from one row (a frame of a stream) to whole batches.  The same bits as omc_i8_quantize and
+ * omc_i8_gemm one after the other.
+ *   X                   device, of x_type, row stride ldx
+ *   w_codes, w_scales   device, the weights in I8, N rows of K
+ *   bias                device, N floats, or NULL
+ *   Y                   device, of y_type, row stride ldy
+ *   ws                  device workspace of omc_i8_linear_workspace_bytes(M, N, K) bytes, 16-byte aligned */
+size_t omc_i8_linear_workspace_bytes(uint32_t M, uint32_t N, uint32_t K);
+omc_status omc_i8_linear(const void *X, omc_type x_type, uint64_t ldx, const void *w_codes, const float *w_scales, const float *bias, void *Y, omc_type y_type, uint64_t ldy, uint32_t M, uint32_t N,
+                         uint32_t K, void *ws, size_t ws_bytes, void *stream);
+
+/* ---- a gated linear layer ------------------------------------------------------------------------
+ *     g = X Wg^T + bg,   u = X Wu^T + bu,   H = act(g) * u
+ * with act one of
+ *     OMC_GATE_SIGMOID   1 / (1 + exp(-g))        (the gated linear unit of a Conformer's convolution module)
+ *     OMC_GATE_SWISH     g / (1 + exp(-g))
+ *     OMC_GATE_GELU      g * erfc(-g / sqrt 2) / 2
+ * Other values are OMC_ERR_OPT.  M, N and K in 1 .. 2^22 (in 8 bits as above). */
+typedef enum { OMC_GATE_SIGMOID = 0, OMC_GATE_SWISH = 1, OMC_GATE_GELU = 2 } omc_gate;
+
+/* Its forward pass on operands in bf16, sums in fp32; X and the weights may come in fp32 and are rounded to bf16 on the way.
+ *   X                  device, M x K of x_type, row stride ldx
+ *   Wg, Wu             device, N x K each, of w_type, row stride ldw
+ *   bg, bu             device, N floats each, or NULL
+ *   H                  device, M x N of h_type, row stride ldh; rounded once
+ *   slope_g, slope_u   device, M x N bf16 each, row stride ld_slope, or both NULL: dH/dg = u act'(g) and dH/du = act(g), each rounded once, for the backward pass
+ *   ws                 device workspace of omc_gated_linear_workspace_bytes(M, N, K) bytes, 16-byte aligned (may be 0: then ws may be NULL)
+ * The order of the sums is fixed by the sizes. */
+size_t omc_gated_linear_workspace_bytes(uint32_t M, uint32_t N, uint32_t K);
+omc_status omc_gated_linear(const void *X, omc_type x_type, uint64_t ldx, const void *Wg, const void *Wu, omc_type w_type, uint64_t ldw, const float *bg, const float *bu, omc_gate gate, void *H,
+                            omc_type h_type, uint64_t ldh, void *slope_g, void *slope_u, uint64_t ld_slope, uint32_t M, uint32_t N, uint32_t K, void *ws, size_t ws_bytes, void *stream);
+
+/* Its backward pass.  With dg = dH * slope_g and du = dH * slope_u in fp32,
+ *     dX[M x K] = dg Wg + du Wu,   dWg[N x K] = dg^T X,   dWu = du^T X     dg and du rounded to bf16, X and the weights as above, sums in fp32
+ *     dbg[N] = sum over the rows of dg,   dbu likewise                      not rounded
+ *   dH                 device, M x N of dh_type, row stride lddh
+ *   slope_g, slope_u   device, as the forward pass left them
+ *   X                  device, M x K of x_type, row stride ldx; not needed without dWg and dWu
+ *   Wg, Wu             device, as the forward pass took them; not needed without dX
+ *   dX                 device, of dx_type, row stride lddx, or NULL
+ *   dWg, dWu           device, N*K floats each, or both NULL: the gradients as omc_step_update_recompress takes them for N x K variables
+ *   dbg, dbu           device, N floats each, either may be NULL
+ *   ws                 device workspace of omc_gated_linear_backward_workspace_bytes(M, N, K) bytes, 16-byte aligned
+ * At least one output (OMC_ERR_NULL).  Every sum's order is fixed by the sizes: a gradient has the same bits whichever others are asked for. */
+size_t omc_gated_linear_backward_workspace_bytes(uint32_t M, uint32_t N, uint32_t K);
+omc_status omc_gated_linear_backward(const void *dH, omc_type dh_type, uint64_t lddh, const void *slope_g, const void *slope_u, uint64_t ld_slope, const void *X, omc_type x_type, uint64_t ldx,
+                                     const void *Wg, const void *Wu, omc_type w_type, uint64_t ldw, void *dX, omc_type dx_type, uint64_t lddx, float *dWg, float *dWu, float *dbg, float *dbu,
+                                     uint32_t M, uint32_t N, uint32_t K, void *ws, size_t ws_bytes, void *stream);
+
+/* Its forward pass on operands in I8, for serving: X rounded along its rows on the way, as omc_i8_linear does.
+ *   wg_codes, wg_scales, wu_codes, wu_scales   device, the weights in I8, N rows of K each
+ *   others as above */
+size_t omc_i8_gated_linear_workspace_bytes(uint32_t M, uint32_t N, uint32_t K);
+omc_status omc_i8_gated_linear(const void *X, omc_type x_type, uint64_t ldx, const void *wg_codes, const float *wg_scales, const void *wu_codes, const float *wu_scales, const float *bg, const float *bu,
+                               omc_gate gate, void *H, omc_type h_type, uint64_t ldh, uint32_t M, uint32_t N, uint32_t K, void *ws, size_t ws_bytes, void *stream);
+
 /* ---- layer norm ---------------------------------------------------------------------------------
  * Its weights are the vectors that stay fp32 in a variable set (Sec. 2.4).  For every row x of `cols` values
  *     mean = sum x / cols,   rstd = 1 / sqrt(sum (x - mean)^2 / cols + eps),   y = (x - mean) * rstd * gamma + beta

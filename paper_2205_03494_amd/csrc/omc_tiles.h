@@ -1,0 +1,391 @@
+// C[M x N] = A B^T in tiles, on 8-bit integers or bf16: the kernel's body, instantiated by omc_i8_gemm.hip, omc_gated.hip and omc_gated_grad.hip.
+//
+// Both types' matrix instructions take 16 bytes of a row in a lane (16 x 16 results over 64 values of 8 bits or 32 of bf16), so that one kernel serves both.  Operands go from global memory straight into a
+// ring of S LDS stages of 128 bytes of K (8 bits) or 64 k (bf16).
+//   Along K: a row's stage is 128 bytes, eight pieces of 16, XOR-swizzled by half the row on their way in: the sixteen rows of a read lie on different banks.
+//   Across K (a row of the operand for every k, bf16): the stage's 64 rows as they are, fragments by the transposing read (of 16 lanes that point at four rows x 16 columns, lane c receives column
+//   c's four rows).  The 64-byte groups of a row are exchanged by the lowest bits of the row and the 16-byte pieces in them by its bit 3.
+// A stage has two steps.  B's rows are the instruction's first operand: a lane then holds four neighbours of a row of C.  A gated product's tile holds rows of both its matrices, every
+// wave the same columns of the two, and the gate needs no other wave's sums.
+//
+// The order of reads and products is written down: a column of tiles at a time, A's fragments of the next step beside the first products, B's each as soon as its predecessor has been multiplied for the last time; a
+// stage's second step is multiplied behind the barrier of the next stage, under that one's first reads and the loads of the one that is asked for.  A workgroup's tiles follow each other without a gap: the loads
+// of the next tile are under way while the last stages of this one are multiplied.
+#pragma once
+#include "omc_finish.h"
+#include "omc_pieces.h"
+
+namespace omc {
+
+template <bool I8>
+struct SumOf {
+    typedef f32x4 type;
+    typedef float scalar;
+};
+template <>
+struct SumOf<true> {
+    typedef i32x4 type;
+    typedef int scalar;
+};
+__device__ __forceinline__ f32x4 multiply_16(i32x4 a, i32x4 b, f32x4 acc) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), acc, 0, 0, 0);
+}
+__device__ __forceinline__ i32x4 multiply_16(i32x4 a, i32x4 b, i32x4 acc) { return __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, acc, 0, 0, 0); }
+
+struct TileGrid {
+    TiledArgs g;
+    uint32_t tiles_m, tiles_n, splits, stages_per_split;
+};
+
+// Two tiles side by side in bf16, so that a lane has eight neighbours: of tile 0 (even) or 1 (odd lane / 16), columns 8 (lane / 32) ..
+__device__ __forceinline__ u32x4 side_by_side_bf16(const float (&x)[4], const float (&y)[4]) {
+    const auto lo = __builtin_amdgcn_permlane16_swap(to_bf16_pair(x[0], x[1]), to_bf16_pair(y[0], y[1]), false, false);
+    const auto hi = __builtin_amdgcn_permlane16_swap(to_bf16_pair(x[2], x[3]), to_bf16_pair(y[2], y[3]), false, false);
+    return u32x4{static_cast<uint32_t>(lo[0]), static_cast<uint32_t>(hi[0]), static_cast<uint32_t>(lo[1]), static_cast<uint32_t>(hi[1])};
+}
+
+// WM x WN waves of TM x TN matrix tiles, S stages, OCC waves per SIMD.  GATED: the tile's columns are TN / 2 tiles of a wave of either matrix.  SPLIT: the contraction is cut, sums go to parts as they are.
+template <bool I8, bool GATED, bool ACROSS_A, bool ACROSS_B, int WM, int WN, int TM, int TN, int S, int OCC, bool SPLIT, typename T>
+__global__ __attribute__((amdgpu_flat_work_group_size(64 * WM * WN, 64 * WM * WN))) __attribute__((amdgpu_waves_per_eu(OCC, OCC)))
+void tiles_kernel(TileGrid tg) {
+    constexpr int NW = WM * WN, BM = 16 * TM * WM, BN = 16 * TN * WN, kColsOut = GATED ? BN / 2 : BN, TH = GATED ? TN / 2 : TN;
+    constexpr int kALoads = BM / 8 / NW, kBLoads = BN / 8 / NW, kLoads = kALoads + kBLoads;
+    constexpr uint32_t kB = BM * 128, kStage = kB + BN * 128;
+    static_assert(BM % (8 * NW) == 0 && BN % (8 * NW) == 0 && (!GATED || TN % 2 == 0) && !(I8 && (ACROSS_A || ACROSS_B)) && !(GATED && ACROSS_B), "whole loads");
+    typedef typename SumOf<I8>::type Sum;
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[S * kStage];
+    const TiledArgs &g = tg.g;
+    const uint32_t lds0 = lds_offset(lds);
+    const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave / WN, wn = wave % WN;
+    const uint32_t groups = gridDim.x, tiles = tg.tiles_m * tg.tiles_n, items = SPLIT ? tiles * tg.splits : tiles;
+
+    struct Place {
+        uint32_t m0, n0, part, first, stages;
+    };
+    auto locate = [&](uint32_t item) {
+        Place p;
+        p.part = SPLIT ? __builtin_amdgcn_readfirstlane(item / tiles) : 0u;
+        tile_of(item - p.part * tiles, BM == 256 ? 4 : 8, tg.tiles_m, tg.tiles_n, p.m0, p.n0);
+        p.m0 = __builtin_amdgcn_readfirstlane(p.m0) * BM;
+        p.n0 = __builtin_amdgcn_readfirstlane(p.n0) * kColsOut;
+        p.first = SPLIT ? p.part * tg.stages_per_split : 0u;
+        p.stages = SPLIT ? min(tg.stages_per_split, g.stages - p.first) : g.stages;
+        return p;
+    };
+
+    // ---- global -> LDS, 1 KB a load.  Rows, or columns' pieces, past the end: the last ones again.
+    auto across_row = [&](auto width, uint32_t i) { return (wave + NW * i) * (512 / decltype(width)::value) + lane / (decltype(width)::value / 8); };
+    auto across_piece = [&](auto width, uint32_t i) {
+        constexpr uint32_t W = decltype(width)::value;
+        const uint32_t row = across_row(width, i), slot = lane % (W / 8), swz = W >= 128 ? row & 3u : (row >> 1) & 1u;
+        return (((slot >> 2) ^ swz) << 2) | ((slot & 3u) ^ ((row >> 2) & 2u));
+    };
+    auto load_row = [&](uint32_t i) { return 8 * (wave + NW * i) + (lane >> 3); };
+    auto load_piece = [&](uint32_t i) { return 16 * ((lane & 7u) ^ (load_row(i) >> 1 & 7u)); };
+    const uint8_t *a_from, *b_from, *b2_from = nullptr;
+    uint32_t off[kLoads];
+    uint32_t ask_item = blockIdx.x, ask_stage, ask_end;
+    uint64_t lanes = ~0ull;                    // none once everything has been asked for
+    const uint64_t a_step = ACROSS_A ? 64 * g.a_pitch : 128, b_step = ACROSS_B ? 64 * g.b_pitch : 128;
+    auto ask_for = [&](uint32_t item) {
+        const Place p = locate(item);
+        if constexpr (ACROSS_A) {
+            a_from = static_cast<const uint8_t *>(g.a) + p.first * a_step;
+            for_constants<kALoads>([&](auto i) { off[i.value] = across_row(UintTag<BM>{}, i.value) * static_cast<uint32_t>(g.a_pitch) + 2 * min(p.m0 + 8 * across_piece(UintTag<BM>{}, i.value), g.M - 8); });
+        } else {
+            a_from = static_cast<const uint8_t *>(g.a) + p.m0 * g.a_pitch + p.first * 128;
+            for_constants<kALoads>([&](auto i) { off[i.value] = min(load_row(i.value), g.M - 1 - p.m0) * static_cast<uint32_t>(g.a_pitch) + load_piece(i.value); });
+        }
+        if constexpr (ACROSS_B) {
+            b_from = p.first < g.turn ? static_cast<const uint8_t *>(g.b) + p.first * b_step : static_cast<const uint8_t *>(g.b2) + (p.first - g.turn) * b_step;
+            for_constants<kBLoads>([&](auto i) { off[kALoads + i.value] = across_row(UintTag<BN>{}, i.value) * static_cast<uint32_t>(g.b_pitch) + 2 * min(p.n0 + 8 * across_piece(UintTag<BN>{}, i.value), g.b_cols - 8); });
+        } else {
+            const uint64_t at = p.n0 * g.b_pitch + p.first * 128;
+            b_from = static_cast<const uint8_t *>(g.b) + at;
+            if constexpr (GATED) b2_from = static_cast<const uint8_t *>(g.b2) + at;
+            for_constants<kBLoads>([&](auto i) {
+                const uint32_t row = load_row(i.value), col = GATED ? 16 * (TH * (row / (16 * TN)) + row / 16 % TH) + row % 16 : row;
+                off[kALoads + i.value] = min(col, g.N - 1 - p.n0) * static_cast<uint32_t>(g.b_pitch) + load_piece(i.value);
+            });
+        }
+        ask_stage = p.first;
+        ask_end = p.first + p.stages;
+    };
+    const uint32_t to = lds0 + 1024 * wave;
+    struct From {
+        const uint8_t *a, *b, *b2;
+    };
+    auto from_now = [&]() { return From{in_scalars(a_from), in_scalars(b_from), GATED ? in_scalars(b2_from) : nullptr}; };
+    auto load_one = [&](const From &from, uint32_t at, auto index) {
+        constexpr uint32_t I = decltype(index)::value;
+        if constexpr (I < kALoads) {
+            load_pieces<1024 * NW * I>(from.a, off[I], to + at, lanes);
+        } else {
+            constexpr uint32_t J = I - kALoads;
+            const bool second = GATED && 8 * (wave + NW * J) / 16 % TN >= TH;
+            load_pieces<kB + 1024 * NW * J>(second ? from.b2 : from.b, off[I], to + at, lanes);
+        }
+    };
+    auto load_stage = [&](uint32_t at) {
+        const From from = from_now();
+        for_constants<kLoads>([&](auto i) { load_one(from, at, i); });
+    };
+    auto next_stage = [&]() {
+        if (lanes == 0) return;
+        if (++ask_stage == ask_end) {
+            ask_item += groups;
+            if (ask_item < items) ask_for(ask_item);
+            else lanes = 0;
+        } else {
+            a_from += a_step;
+            b_from += b_step;
+            if constexpr (GATED) b2_from += 128;
+            if (ACROSS_B && ask_stage == g.turn) b_from = static_cast<const uint8_t *>(g.b2);
+        }
+    };
+
+    // ---- LDS -> fragments
+    const uint32_t r = lane & 15u, q = lane >> 4;
+    auto along_place = [&](uint32_t row, uint32_t step) { return row * 128 + (((q + 4 * step) ^ ((r >> 1) & 7u)) << 4); };   // (row % 16 is r)
+    const uint32_t t_row = 8 * q + (r >> 2);
+    auto across_place = [&](auto width, uint32_t tile) {
+        constexpr uint32_t W = decltype(width)::value;
+        const uint32_t piece = 2 * (tile & 1u) + ((lane >> 1) & 1u), swz = W >= 128 ? t_row & 3u : (t_row >> 1) & 1u;
+        return t_row * (2 * W) + (((tile >> 1) ^ swz) * 4 + (piece ^ ((t_row >> 2) & 2u))) * 16 + 8 * (lane & 1u);
+    };
+    uint32_t a_at[ACROSS_A ? TM : 2], b_at[ACROSS_B ? TN : 2];
+#pragma unroll
+    for (uint32_t i = 0; i < (ACROSS_A ? TM : 2); ++i) a_at[i] = ACROSS_A ? across_place(UintTag<BM>{}, TM * wm + i) : along_place(16 * TM * wm + r, i);
+#pragma unroll
+    for (uint32_t i = 0; i < (ACROSS_B ? TN : 2); ++i) b_at[i] = kB + (ACROSS_B ? across_place(UintTag<BN>{}, TN * wn + i) : along_place(16 * TN * wn + r, i));
+    uint32_t cur = 0, far = (S - 1) * kStage;
+    auto transposed = [&](uint32_t at, uint32_t four_rows) {
+        uint8_t *p = lds + at;
+        const i32x2 lo = __builtin_bit_cast(i32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((OMC_LDS s16x4 *)(p)));
+        const i32x2 hi = __builtin_bit_cast(i32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((OMC_LDS s16x4 *)(p + four_rows)));
+        return i32x4{lo[0], lo[1], hi[0], hi[1]};
+    };
+    Sum acc[TM][TN];
+    i32x4 a[2][TM], b[TN];
+    auto read_a = [&](auto step, auto index) {
+        constexpr uint32_t s = decltype(step)::value, I = decltype(index)::value;
+        if constexpr (ACROSS_A) a[s][I] = transposed(cur + a_at[I] + 32 * 2 * BM * s, 4 * 2 * BM);
+        else a[s][I] = *reinterpret_cast<const i32x4 *>(lds + cur + a_at[s] + 2048 * I);
+    };
+    auto read_b = [&](auto step, auto index) {
+        constexpr uint32_t s = decltype(step)::value, I = decltype(index)::value;
+        if constexpr (ACROSS_B) b[I] = transposed(cur + b_at[I] + 32 * 2 * BN * s, 4 * 2 * BN);
+        else b[I] = *reinterpret_cast<const i32x4 *>(lds + cur + b_at[s] + 2048 * I);
+    };
+    // The products of step s and the reads of the next one; beside the second step's the loads of the stage that is asked for.
+    auto multiply = [&](auto step) {
+        constexpr uint32_t s = decltype(step)::value, NEXT = 1 - s;
+        constexpr int kL = s == 1 ? kLoads : 0;
+        const From from = kL > 0 ? from_now() : From{};
+        for_constants<TN>([&](auto column) {
+            constexpr int J = decltype(column)::value, R0 = J * TM / TN, R1 = (J + 1) * TM / TN, L0 = J * kL / TN, L1 = (J + 1) * kL / TN;
+            for_constants<R1 - R0>([&](auto i) { read_a(UintTag<NEXT>{}, UintTag<R0 + decltype(i)::value>{}); });
+            for_constants<L1 - L0>([&](auto i) { load_one(from, far, UintTag<L0 + decltype(i)::value>{}); });
+#pragma unroll
+            for (int i = 0; i < TM; ++i) acc[i][J] = multiply_16(b[J], a[s][i], acc[i][J]);
+            read_b(UintTag<NEXT>{}, column);
+            __builtin_amdgcn_sched_barrier(0);
+        });
+    };
+    // Waits for the next stage: it is there when at most the loads of the S - 2 after it are on their way.  (At the end it is nothing that is waited for, read and asked for.  Loads without lanes are not relied on to count.)
+    auto wait_for_next = [&]() {
+        if (lanes == 0) wait_loads_and_sync<0>();
+        else wait_loads_and_sync<(S - 2) * kLoads>();
+        cur = cur == (S - 1) * kStage ? 0 : cur + kStage;
+        far = far == (S - 1) * kStage ? 0 : far + kStage;
+    };
+
+    ask_for(ask_item);
+#pragma unroll
+    for (uint32_t i = 0; i < S - 1; ++i) {
+        load_stage(i * kStage);
+        next_stage();
+    }
+    if (lanes != 0) wait_loads_and_sync<(S - 2) * kLoads>();
+    else wait_loads_and_sync<0>();
+    load_stage(far);
+    next_stage();
+    for_constants<TM>([&](auto i) { read_a(UintTag<0>{}, i); });
+    for_constants<TN>([&](auto i) { read_b(UintTag<0>{}, i); });
+    for (uint32_t item = blockIdx.x; item < items; item += groups) {
+        const Place p = locate(item);
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int j = 0; j < TN; ++j) acc[i][j] = Sum{0, 0, 0, 0};
+        for (uint32_t left = p.stages; left > 0; --left) {
+            multiply(UintTag<0>{});
+            wait_for_next();
+            multiply(UintTag<1>{});
+            next_stage();
+        }
+
+        // ---- results: tile (i, j)'s lane holds row r, columns 4 q .. of it
+        const uint32_t m_wave = p.m0 + 16 * TM * wm + r, n_wave = p.n0 + 16 * TH * wn;
+        if constexpr (SPLIT) {
+            const uint64_t width = GATED ? 2ull * g.N : g.N;
+            typedef typename SumOf<I8>::scalar Scalar;
+#pragma unroll
+            for (uint32_t i = 0; i < TM; ++i) {
+                const uint32_t m = m_wave + 16 * i;
+#pragma unroll
+                for (uint32_t j = 0; j < TN; ++j) {
+                    const uint32_t n = n_wave + 16 * (j % TH) + 4 * q;
+                    if (m >= g.M || n >= g.N) continue;
+                    Scalar *out = static_cast<Scalar *>(g.parts) + (static_cast<uint64_t>(p.part) * g.M + m) * width + (j / TH) * static_cast<uint64_t>(g.N) + n;
+                    if (n + 4 <= g.N) {
+                        __builtin_memcpy(out, &acc[i][j], 16);
+                    } else {
+#pragma unroll
+                        for (uint32_t e = 0; e < 4; ++e)
+                            if (n + e < g.N) out[e] = acc[i][j][e];
+                    }
+                }
+            }
+        } else {
+            const Finish &f = g.f;
+#pragma unroll
+            for (uint32_t i = 0; i < TM; ++i) {
+                const uint32_t m = m_wave + 16 * i;
+                const float row_scale = I8 ? f.row_scale[min(m, g.M - 1)] : 1.0f;
+                typename T::type *row = m < g.M ? row_of<T>(f, m) : nullptr;
+                auto finished = [&](uint32_t j, Four &sg, Four &su) {
+                    const uint32_t n = n_wave + 16 * j + 4 * q, at = min(n, g.N - 1), left = g.N - at;
+                    if constexpr (GATED) return finish_gated(f, acc[i][j], acc[i][j + TH], row_scale, at, left, sg, su);
+                    else return finish_plain(f, acc[i][j], row_scale, at, left);
+                };
+                // (all lanes take part in the exchange)
+                auto store_two = [&](uint16_t *to_row, const float (&x)[4], const float (&y)[4], uint32_t j) {
+                    const u32x4 w = side_by_side_bf16(x, y);
+                    const uint32_t n = n_wave + 16 * (j + (q & 1u)) + 8 * (q >> 1);
+                    if (!to_row || n >= g.N) return;
+                    if (n + 8 <= g.N) {
+                        __builtin_memcpy(to_row + n, &w, 16);
+                    } else {
+#pragma unroll
+                        for (uint32_t e = 0; e < 8; ++e)
+                            if (n + e < g.N) to_row[n + e] = static_cast<uint16_t>(w[e / 2] >> (16 * (e & 1)));
+                    }
+                };
+                auto store_four = [&](auto type, auto *to_row, const float (&x)[4], uint32_t j) {
+                    const uint32_t n = n_wave + 16 * j + 4 * q;
+                    if (to_row && n < g.N) store_run<decltype(type), 4>(to_row + n, x, g.N - n);
+                };
+                const bool keep = GATED && f.slope_g;
+                uint16_t *row_g = keep && m < g.M ? f.slope_g + m * f.ld_slope : nullptr, *row_u = keep && m < g.M ? f.slope_u + m * f.ld_slope : nullptr;
+                if constexpr (TH % 2 == 0) {
+#pragma unroll
+                    for (uint32_t j = 0; j < TH; j += 2) {
+                        Four sg[2], su[2];
+                        const Four x = finished(j, sg[0], su[0]), y = finished(j + 1, sg[1], su[1]);
+                        if constexpr (T::kBytes == 2) {
+                            store_two(row, x.v, y.v, j);
+                        } else {
+                            store_four(T{}, row, x.v, j);
+                            store_four(T{}, row, y.v, j + 1);
+                        }
+                        if (keep) {
+                            store_two(row_g, sg[0].v, sg[1].v, j);
+                            store_two(row_u, su[0].v, su[1].v, j);
+                        }
+                    }
+                } else {
+#pragma unroll
+                    for (uint32_t j = 0; j < TH; ++j) {
+                        Four sg, su;
+                        const Four x = finished(j, sg, su);
+                        store_four(T{}, row, x.v, j);
+                        if (keep) {
+                            store_four(BF16{}, row_g, sg.v, j);
+                            store_four(BF16{}, row_u, su.v, j);
+                        }
+                    }
+                }
+            }
+        }
+    }
+}
+
+// The parts of a split contraction, added in order, and what becomes of the sums.
+template <bool I8, bool GATED, typename T>
+__global__ __launch_bounds__(256) void join_kernel(TiledArgs g, uint32_t splits) {
+    typedef typename SumOf<I8>::type Sum;
+    typedef typename SumOf<I8>::scalar Scalar;
+    const uint32_t n = 4 * (blockIdx.x * 64 + (threadIdx.x & 63u)), m = blockIdx.y * 4 + (threadIdx.x >> 6);
+    if (m >= g.M || n >= g.N) return;
+    const uint32_t left = g.N - n;
+    const uint64_t width = GATED ? 2ull * g.N : g.N;
+    auto sum_from = [&](uint64_t column) {
+        Sum t = {0, 0, 0, 0};
+        for (uint32_t s = 0; s < splits; ++s) {
+            const Scalar *from = static_cast<const Scalar *>(g.parts) + (static_cast<uint64_t>(s) * g.M + m) * width + column;
+            Sum w = {0, 0, 0, 0};
+            if (left >= 4) {
+                __builtin_memcpy(&w, from, 16);
+            } else {
+#pragma unroll
+                for (uint32_t e = 0; e < 4; ++e)
+                    if (e < left) w[e] = from[e];
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) t[e] += w[e];
+        }
+        return t;
+    };
+    const float row_scale = I8 ? g.f.row_scale[m] : 1.0f;
+    typename T::type *row = row_of<T>(g.f, m);
+    if constexpr (GATED) {
+        Four sg, su;
+        const Four x = finish_gated(g.f, sum_from(n), sum_from(static_cast<uint64_t>(g.N) + n), row_scale, n, left, sg, su);
+        store_run<T, 4>(row + n, x.v, left);
+        if (g.f.slope_g) {
+            store_run<BF16, 4>(g.f.slope_g + m * g.f.ld_slope + n, sg.v, left);
+            store_run<BF16, 4>(g.f.slope_u + m * g.f.ld_slope + n, su.v, left);
+        }
+    } else {
+        const Four x = finish_plain(g.f, sum_from(n), row_scale, n, left);
+        if (row) store_run<T, 4>(row + n, x.v, left);
+    }
+}
+
+// The tile that a product takes and into how many parts its contraction is cut.
+struct TileChoice {
+    int tile;
+    uint32_t splits;
+};
+constexpr uint32_t kTileRows[] = {256, 256, 128, 64}, kTileCols[] = {256, 128, 128, 64};
+TileChoice choose_tile(uint32_t M, uint32_t cols, uint32_t stages);   // cols: of both matrices where gated
+
+template <bool I8, bool GATED, bool ACROSS_A, bool ACROSS_B, int WM, int WN, int TM, int TN, int S, int OCC, int RESIDENT, typename T>
+static void launch_one(const TileGrid &tg, hipStream_t st) {
+    const uint32_t items = tg.tiles_m * tg.tiles_n * tg.splits, most = 256 * RESIDENT;
+    const dim3 grid(items < most ? items : most), block(64 * WM * WN);
+    if (tg.splits > 1) tiles_kernel<I8, GATED, ACROSS_A, ACROSS_B, WM, WN, TM, TN, S, OCC, true, T><<<grid, block, 0, st>>>(tg);
+    else tiles_kernel<I8, GATED, ACROSS_A, ACROSS_B, WM, WN, TM, TN, S, OCC, false, T><<<grid, block, 0, st>>>(tg);
+}
+template <bool I8, bool GATED, bool ACROSS_A, bool ACROSS_B, typename T>
+static int launch_tiles(const TiledArgs &pa, hipStream_t st) {
+    const uint32_t cols = GATED ? 2 * pa.N : pa.N;
+    const TileChoice c = choose_tile(pa.M, cols, pa.stages);
+    const uint32_t bm = kTileRows[c.tile], bn = kTileCols[c.tile] / (GATED ? 2 : 1);
+    const TileGrid tg{pa, (pa.M + bm - 1) / bm, (pa.N + bn - 1) / bn, c.splits, (pa.stages + c.splits - 1) / c.splits};
+    switch (c.tile) {
+        case 0: launch_one<I8, GATED, ACROSS_A, ACROSS_B, 4, 2, 4, 8, 2, 2, 1, T>(tg, st); break;
+        case 1: launch_one<I8, GATED, ACROSS_A, ACROSS_B, 4, 2, 4, 4, 3, 2, 1, T>(tg, st); break;
+        case 2: launch_one<I8, GATED, ACROSS_A, ACROSS_B, 4, 2, 2, 4, 4, 2, 1, T>(tg, st); break;
+        default: launch_one<I8, GATED, ACROSS_A, ACROSS_B, 2, 2, 2, 2, 4, 2, 2, T>(tg, st); break;
+    }
+    if (c.splits > 1) {
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return static_cast<int>(e);
+        join_kernel<I8, GATED, T><<<dim3((pa.N + 255) / 256, (pa.M + 3) / 4), dim3(256), 0, st>>>(pa, c.splits);
+    }
+    return static_cast<int>(hipGetLastError());
+}
+
+}  // namespace omc

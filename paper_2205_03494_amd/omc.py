@@ -119,6 +119,20 @@ _norm_backward_ws = _sig("omc_layer_norm_backward_workspace_bytes", _sz, _u32, _
 _norm_backward = _sig("omc_layer_norm_backward", _i, _vp, _i, _u64, _vp, _i, _u64, _vp, _vp, _vp, _vp, _u64, _vp, _vp, _u32, _u32, _vp,
                       _sz, _vp)
 
+_i8_codes = _sig("omc_i8_code_bytes", _sz, _u32, _u32)
+_i8_quantize = _sig("omc_i8_quantize", _i, _vp, _i, _u32, _u32, _u64, _i, _vp, _vp, _vp, _u64, _vp)
+_i8_gemm_ws = _sig("omc_i8_gemm_workspace_bytes", _sz, _u32, _u32, _u32)
+_i8_gemm = _sig("omc_i8_gemm", _i, _vp, _vp, _vp, _vp, _vp, _vp, _i, _u64, _u32, _u32, _u32, _vp, _sz, _vp)
+_i8_linear_ws = _sig("omc_i8_linear_workspace_bytes", _sz, _u32, _u32, _u32)
+_i8_linear = _sig("omc_i8_linear", _i, _vp, _i, _u64, _vp, _vp, _vp, _vp, _i, _u64, _u32, _u32, _u32, _vp, _sz, _vp)
+_i8_gated_ws = _sig("omc_i8_gated_linear_workspace_bytes", _sz, _u32, _u32, _u32)
+_i8_gated = _sig("omc_i8_gated_linear", _i, _vp, _i, _u64, _vp, _vp, _vp, _vp, _vp, _vp, _i, _vp, _i, _u64, _u32, _u32, _u32, _vp, _sz, _vp)
+_gated_ws = _sig("omc_gated_linear_workspace_bytes", _sz, _u32, _u32, _u32)
+_gated = _sig("omc_gated_linear", _i, _vp, _i, _u64, _vp, _vp, _i, _u64, _vp, _vp, _i, _vp, _i, _u64, _vp, _vp, _u64, _u32, _u32, _u32, _vp, _sz, _vp)
+_gated_backward_ws = _sig("omc_gated_linear_backward_workspace_bytes", _sz, _u32, _u32, _u32)
+_gated_backward = _sig("omc_gated_linear_backward", _i, _vp, _i, _u64, _vp, _vp, _u64, _vp, _i, _u64, _vp, _vp, _i, _u64, _vp, _i, _u64, _vp, _vp,
+                       _vp, _vp, _u32, _u32, _u32, _vp, _sz, _vp)
+
 EXPORTED = ["omc_status_string", "omc_format_validate", "omc_format_bits", "omc_format_max",
             "omc_packed_bytes", "omc_compress_workspace_bytes", "omc_compress", "omc_decompress",
             "omc_compress_noalloc", "omc_compress_noalloc_max_elems",
@@ -135,7 +149,10 @@ EXPORTED = ["omc_status_string", "omc_format_validate", "omc_format_bits", "omc_
             "omc_mx4_code_bytes", "omc_mx4_scale_bytes", "omc_mx4_quantize", "omc_mx4_gemm_workspace_bytes", "omc_mx4_gemm",
             "omc_mx4_linear_workspace_bytes", "omc_mx4_linear", "omc_mx4_linear_backward_workspace_bytes",
             "omc_mx4_linear_backward", "omc_layer_norm", "omc_layer_norm_backward_workspace_bytes",
-            "omc_layer_norm_backward"]
+            "omc_layer_norm_backward",
+            "omc_i8_code_bytes", "omc_i8_quantize", "omc_i8_gemm_workspace_bytes", "omc_i8_gemm", "omc_i8_linear_workspace_bytes", "omc_i8_linear",
+            "omc_i8_gated_linear_workspace_bytes", "omc_i8_gated_linear", "omc_gated_linear_workspace_bytes", "omc_gated_linear",
+            "omc_gated_linear_backward_workspace_bytes", "omc_gated_linear_backward"]
 
 
 class OmcError(RuntimeError):
@@ -604,3 +621,133 @@ def omc_layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, gamma: Optional[t
     _check(_norm_backward(pdy, ykind, lddy, px, xkind, ldx, _floats(gamma, cols), _floats(mean, rows), _floats(rstd, rows), pdx, lddx,
                           _floats(dgamma, cols), _floats(dbeta, cols), rows, cols, *_space(ws), _stream(stream)),
            "omc_layer_norm_backward")
+
+
+# --------------------------------------------------------------------------- products on 8-bit integers, and a gated linear layer
+OMC_GATE_SIGMOID, OMC_GATE_SWISH, OMC_GATE_GELU = 0, 1, 2
+
+
+def _i8(t: Optional[torch.Tensor], rows: int, cols: int):
+    return None if t is None else _array(t, rows * ((cols + 127) // 128) * 128, _uint8)
+
+
+def omc_i8_code_bytes(rows: int, cols: int) -> int:
+    return _i8_codes(rows, cols)
+
+
+def omc_i8_gemm_workspace_bytes(M: int, N: int, K: int) -> int:
+    return _i8_gemm_ws(M, N, K)
+
+
+def omc_i8_linear_workspace_bytes(M: int, N: int, K: int) -> int:
+    return _i8_linear_ws(M, N, K)
+
+
+def omc_i8_gated_linear_workspace_bytes(M: int, N: int, K: int) -> int:
+    return _i8_gated_ws(M, N, K)
+
+
+def omc_gated_linear_workspace_bytes(M: int, N: int, K: int) -> int:
+    return _gated_ws(M, N, K)
+
+
+def omc_gated_linear_backward_workspace_bytes(M: int, N: int, K: int) -> int:
+    return _gated_backward_ws(M, N, K)
+
+
+def omc_i8_quantize(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, by_columns: bool = False,
+                    values: Optional[torch.Tensor] = None, stream=None) -> None:
+    """x [rows, cols] in fp32 or bf16.  codes: uint8 buffer of omc_i8_code_bytes(rows, cols), scales [rows]; by_columns: of
+    omc_i8_code_bytes(cols, rows), the transpose's, and scales [cols].  values: like x, what the codes stand for."""
+    rows, cols = x.shape
+    px, kind, ldx = _matrix(x)
+    pv, vkind, ldv = (None, kind, 0) if values is None else _rows_like(values, rows, cols)
+    if vkind != kind:
+        raise ValueError("values have x's type")
+    lines, length = (cols, rows) if by_columns else (rows, cols)
+    _check(_i8_quantize(px, kind, rows, cols, ldx, bool(by_columns), _i8(codes, lines, length), _floats(scales, lines), pv, ldv,
+                        _stream(stream)), "omc_i8_quantize")
+
+
+def omc_i8_gemm(a_codes: torch.Tensor, a_scales: torch.Tensor, b_codes: torch.Tensor, b_scales: torch.Tensor,
+                bias: Optional[torch.Tensor], Cout: torch.Tensor, K: int, ws: Optional[torch.Tensor], stream=None) -> None:
+    """Cout [M, N] in fp32 or bf16 = A [M x K] B [N x K]^T + bias."""
+    M, N = Cout.shape
+    pc, kind, ldc = _matrix(Cout)
+    _check(_i8_gemm(_i8(a_codes, M, K), _floats(a_scales, M), _i8(b_codes, N, K), _floats(b_scales, N), _floats(bias, N), pc, kind,
+                    ldc, M, N, K, *_space(ws), _stream(stream)), "omc_i8_gemm")
+
+
+def omc_i8_linear(X: torch.Tensor, w_codes: torch.Tensor, w_scales: torch.Tensor, bias: Optional[torch.Tensor], Y: torch.Tensor,
+                  ws: Optional[torch.Tensor], stream=None) -> None:
+    """Y [M, N] = Q(X [M, K]) W^T + bias; w_codes, w_scales: the weights, N rows of K."""
+    M, K = X.shape
+    N = Y.shape[1]
+    px, xkind, ldx = _matrix(X)
+    py, ykind, ldy = _rows_like(Y, M, N)
+    _check(_i8_linear(px, xkind, ldx, _i8(w_codes, N, K), _floats(w_scales, N), _floats(bias, N), py, ykind, ldy, M, N, K,
+                      *_space(ws), _stream(stream)), "omc_i8_linear")
+
+
+def omc_i8_gated_linear(X: torch.Tensor, wg_codes: torch.Tensor, wg_scales: torch.Tensor, wu_codes: torch.Tensor, wu_scales: torch.Tensor,
+                        bg: Optional[torch.Tensor], bu: Optional[torch.Tensor], gate: int, H: torch.Tensor, ws: Optional[torch.Tensor],
+                        stream=None) -> None:
+    """H [M, N] = act(Q(X) Wg^T + bg) * (Q(X) Wu^T + bu); the weights N rows of K each."""
+    M, K = X.shape
+    N = H.shape[1]
+    px, xkind, ldx = _matrix(X)
+    ph, hkind, ldh = _rows_like(H, M, N)
+    _check(_i8_gated(px, xkind, ldx, _i8(wg_codes, N, K), _floats(wg_scales, N), _i8(wu_codes, N, K), _floats(wu_scales, N), _floats(bg, N),
+                     _floats(bu, N), gate, ph, hkind, ldh, M, N, K, *_space(ws), _stream(stream)), "omc_i8_gated_linear")
+
+
+def _alike(a: Optional[torch.Tensor], b: Optional[torch.Tensor], rows: int, cols: int, what: str):
+    """(pointers, type, row stride) of two matrices that lie alike; None for both: (None, None, fp32, 0)."""
+    if a is None and b is None:
+        return None, None, OMC_F32, 0
+    if a is None or b is None:
+        raise ValueError(f"{what}: both or neither")
+    pa, kind, ld = _rows_like(a, rows, cols)
+    pb, bkind, bld = _rows_like(b, rows, cols)
+    if bkind != kind or bld != ld:
+        raise ValueError(f"{what} are of one type and row stride")
+    return pa, pb, kind, ld
+
+
+def _slopes(a: Optional[torch.Tensor], b: Optional[torch.Tensor], M: int, N: int):
+    pa, pb, kind, ld = _alike(a, b, M, N, "slope_g and slope_u")
+    if pa is not None and kind != OMC_BF16:
+        raise ValueError("slopes are bfloat16")
+    return pa, pb, ld
+
+
+def omc_gated_linear(X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, bg: Optional[torch.Tensor], bu: Optional[torch.Tensor], gate: int,
+                     H: torch.Tensor, slope_g: Optional[torch.Tensor], slope_u: Optional[torch.Tensor], ws: Optional[torch.Tensor],
+                     stream=None) -> None:
+    """H [M, N] = act(X [M, K] Wg^T + bg) * (X Wu^T + bu), weights [N, K]; slope_g, slope_u [M, N] bf16, or None: what the backward pass takes."""
+    M, K = X.shape
+    N = H.shape[1]
+    px, xkind, ldx = _matrix(X)
+    pg, pu, wkind, ldw = _alike(Wg, Wu, N, K, "Wg and Wu")
+    ph, hkind, ldh = _rows_like(H, M, N)
+    sg, su, lds = _slopes(slope_g, slope_u, M, N)
+    _check(_gated(px, xkind, ldx, pg, pu, wkind, ldw, _floats(bg, N), _floats(bu, N), gate, ph, hkind, ldh, sg, su, lds, M, N, K,
+                  *_space(ws), _stream(stream)), "omc_gated_linear")
+
+
+def omc_gated_linear_backward(dH: torch.Tensor, slope_g: torch.Tensor, slope_u: torch.Tensor, X: Optional[torch.Tensor],
+                              Wg: Optional[torch.Tensor], Wu: Optional[torch.Tensor], dX: Optional[torch.Tensor], dWg: Optional[torch.Tensor],
+                              dWu: Optional[torch.Tensor], dbg: Optional[torch.Tensor], dbu: Optional[torch.Tensor], ws: torch.Tensor,
+                              stream=None) -> None:
+    """dH, slopes [M, N]; X, dX [M, K]; weights, dWg and dWu [N, K] (gradients fp32); dbg, dbu [N] fp32.  Without dX the weights, without
+    dWg and dWu X may be None (K is taken from whichever is there)."""
+    M, N = dH.shape
+    K = next((t.shape[1] for t in (X, dX, dWg) if t is not None), 1)
+    pdh, hkind, lddh = _matrix(dH)
+    sg, su, lds = _slopes(slope_g, slope_u, M, N)
+    px, xkind, ldx = (None, OMC_F32, 0) if X is None else _rows_like(X, M, K)
+    pg, pu, wkind, ldw = _alike(Wg, Wu, N, K, "Wg and Wu")
+    pdx, dxkind, lddx = (None, OMC_F32, 0) if dX is None else _rows_like(dX, M, K)
+    _check(_gated_backward(pdh, hkind, lddh, sg, su, lds, px, xkind, ldx, pg, pu, wkind, ldw, pdx, dxkind, lddx, _floats(dWg, N * K),
+                           _floats(dWu, N * K), _floats(dbg, N), _floats(dbu, N), M, N, K, *_space(ws), _stream(stream)),
+           "omc_gated_linear_backward")
