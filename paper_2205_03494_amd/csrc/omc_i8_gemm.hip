@@ -4,10 +4,10 @@
 namespace omc {
 
 int launch_i8_plain(const TiledArgs &pa, bool c_bf16, hipStream_t st) {
-    return c_bf16 ? launch_tiles<true, false, false, false, BF16>(pa, st) : launch_tiles<true, false, false, false, F32>(pa, st);
+    return c_bf16 ? launch_tiles<true, false, false, false, BF16>(pa, false, st) : launch_tiles<true, false, false, false, F32>(pa, false, st);
 }
 int launch_i8_gated(const TiledArgs &pa, bool c_bf16, hipStream_t st) {
-    return c_bf16 ? launch_tiles<true, true, false, false, BF16>(pa, st) : launch_tiles<true, true, false, false, F32>(pa, st);
+    return c_bf16 ? launch_tiles<true, true, false, false, BF16>(pa, false, st) : launch_tiles<true, true, false, false, F32>(pa, false, st);
 }
 
 }  // namespace omc

@@ -16,6 +16,11 @@ __device__ __forceinline__ void load_pieces(const uint8_t *lanes_own, uint32_t t
                  : "memory", "m0", "scc");
 }
 
+// The same with 4 bytes of a lane, to `to` + 4 l.
+__device__ __forceinline__ void load_dwords(const float *lanes_own, uint32_t to, uint64_t lanes) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_mov_b64 exec, %2\n\tglobal_load_lds_dword %1, off\n\ts_mov_b64 exec, -1" ::"s"(to), "v"(lanes_own), "s"(lanes) : "memory", "m0");
+}
+
 // Between a wave's writes to LDS and reads by its other lanes, and back.  The hardware takes a wave's LDS accesses in order; the compiler must not carry a value over.
 __device__ __forceinline__ void lanes_exchange() { asm volatile("" ::: "memory"); }
 

@@ -27,7 +27,10 @@ struct TiledArgs {
     void *parts;                         // of a split contraction
 };
 size_t product_workspace(ProductKind kind, uint32_t M, uint32_t N, uint32_t stages);   // bytes of parts
-int launch_product_tiles(ProductKind kind, const TiledArgs &pa, bool c_bf16, void *stream);
+int launch_product_tiles(ProductKind kind, const TiledArgs &pa, bool whole, bool c_bf16, void *stream);   // whole: the contraction is not cut
+// Of a gated layer's backward products, M x N as kBF16AcrossB and M2 x N2 as kBF16AcrossBoth (its result in fp32): the tile in which both go together, uncut, in one launch; -1: each goes its own way.
+int product_pair_tile(uint32_t M, uint32_t N, uint32_t stages, uint32_t M2, uint32_t N2, uint32_t stages2);
+int launch_product_pair(int tile, const TiledArgs &dx, bool dx_bf16, const TiledArgs &dw, void *stream);
 
 // The same for few rows of A (product_few).  x_type and w_type: 8-bit codes in padded rows (then K is whole 128s), or fp32 or bf16 as they lie, which are rounded to bf16 on the way; pitches in bytes.
 // rounds: A comes in fp32 or bf16 and becomes 8-bit codes on the way (product_few_rounds).

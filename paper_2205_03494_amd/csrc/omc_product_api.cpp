@@ -65,7 +65,7 @@ static int i8_product(const void *codes, const float *scales, const I8Operands &
     f.gate = o.gate;
     if (product_few(M, N, K)) return launch_product_few(kE8, kE8, gated, FewArgs{codes, pitch, o.w, o.w2, pitch, M, N, static_cast<uint32_t>(pitch), f}, c_bf16, stream);
     const uint32_t stages = static_cast<uint32_t>(pitch / 128);
-    return launch_product_tiles(gated ? kI8Gated : kI8Plain, TiledArgs{codes, o.w, o.w2, pitch, pitch, M, N, stages, stages, N, f, parts}, c_bf16, stream);
+    return launch_product_tiles(gated ? kI8Gated : kI8Plain, TiledArgs{codes, o.w, o.w2, pitch, pitch, M, N, stages, stages, N, f, parts}, false, c_bf16, stream);
 }
 struct I8Layout {
     uint8_t *codes;
@@ -121,6 +121,8 @@ static GatedLayout gated_layout(uint8_t *ws, uint32_t M, uint32_t N, uint32_t K)
     l.bytes = p.used;
     return l;
 }
+// Asked of the sizes alone, so that a gradient's bits do not depend on what is asked for beside it: tiles add up the contraction in the same order, whichever they are, but for where it is cut.
+static int backward_pair(uint32_t M, uint32_t N, uint32_t K) { return product_pair_tile(M, K, to_64(N) / 64 * 2, 2 * to_64(N), K, to_64(M) / 64); }
 struct GatedBackwardLayout {
     uint16_t *dgu, *x, *wg, *wu;
     float *sums;
@@ -136,7 +138,8 @@ static GatedBackwardLayout gated_backward_layout(uint8_t *ws, uint32_t M, uint32
     l.wg = reinterpret_cast<uint16_t *>(p.take(2 * n * k));
     l.wu = reinterpret_cast<uint16_t *>(p.take(2 * n * k));
     l.sums = reinterpret_cast<float *>(p.take(8ull * ((M + kSlopeRows - 1) / kSlopeRows) * N));
-    const uint64_t dx = product_workspace(kBF16AcrossB, M, K, to_64(N) / 64 * 2), dw = product_workspace(kBF16AcrossBoth, 2 * to_64(N), K, to_64(M) / 64);
+    const bool whole = backward_pair(M, N, K) >= 0;
+    const uint64_t dx = whole ? 0 : product_workspace(kBF16AcrossB, M, K, to_64(N) / 64 * 2), dw = whole ? 0 : product_workspace(kBF16AcrossBoth, 2 * to_64(N), K, to_64(M) / 64);
     l.parts = p.take(dx > dw ? dx : dw);
     l.bytes = p.used;
     return l;
@@ -228,7 +231,7 @@ omc_status omc_gated_linear(const void *X, omc_type x_type, uint64_t ldx, const 
         ta.b_pitch = 2 * pitch;
     }
     const int rc = count > 0 ? launch_pack(packs, count, stream) : 0;
-    return from_hip(rc != 0 ? rc : launch_product_tiles(kBF16Gated, ta, h_type == OMC_BF16, stream));
+    return from_hip(rc != 0 ? rc : launch_product_tiles(kBF16Gated, ta, false, h_type == OMC_BF16, stream));
 }
 
 size_t omc_gated_linear_backward_workspace_bytes(uint32_t M, uint32_t N, uint32_t K) { return gated_dims_ok(M, N, K) ? gated_backward_layout(nullptr, M, N, K).bytes : 0; }
@@ -271,8 +274,10 @@ omc_status omc_gated_linear_backward(const void *dH, omc_type dh_type, uint64_t 
         for_dw.b_cols = k;
     }
     if (rc == 0 && count > 0) rc = launch_pack(packs, count, stream);
-    if (rc == 0 && dX) rc = launch_product_tiles(kBF16AcrossB, for_dx, dx_type == OMC_BF16, stream);
-    if (rc == 0 && dWg) rc = launch_product_tiles(kBF16AcrossBoth, for_dw, false, stream);
+    const int pair = backward_pair(M, N, K);
+    if (rc == 0 && pair >= 0 && dX && dWg) return from_hip(launch_product_pair(pair, for_dx, dx_type == OMC_BF16, for_dw, stream));
+    if (rc == 0 && dX) rc = launch_product_tiles(kBF16AcrossB, for_dx, pair >= 0, dx_type == OMC_BF16, stream);
+    if (rc == 0 && dWg) rc = launch_product_tiles(kBF16AcrossBoth, for_dw, pair >= 0, false, stream);
     return from_hip(rc);
 }
 

@@ -127,17 +127,11 @@ __global__ __launch_bounds__(512) void few_kernel(FewArgs fa) {
         const float row_scale = I8 ? fa.f.row_scale[m] : 1.0f;
         typename T::type *to = static_cast<typename T::type *>(fa.f.c) + m * fa.f.ldc + n;
         const uint32_t left = fa.N - n;
+        const Columns columns = columns_from<I8, GATED>(fa.f, n, fa.N);
         if constexpr (GATED) {
-            Four sg, su;
-            const Four v = finish_gated(fa.f, total[0], total[MATRICES - 1], row_scale, n, left, sg, su);
-            store_run<T, 4>(to, v.v, left);
-            if (fa.f.slope_g) {
-                store_run<BF16, 4>(fa.f.slope_g + m * fa.f.ld_slope + n, sg.v, left);
-                store_run<BF16, 4>(fa.f.slope_u + m * fa.f.ld_slope + n, su.v, left);
-            }
+            store_gated<T>(fa.f, total[0], total[MATRICES - 1], row_scale, columns, to, m, n, left);
         } else {
-            const Four v = finish_plain(fa.f, total[0], row_scale, n, left);
-            store_run<T, 4>(to, v.v, left);
+            store_run<T, 4>(to, finish_plain(total[0], row_scale, columns).v, left);
         }
     }
 }

@@ -44,20 +44,35 @@ __device__ __forceinline__ u32x4 side_by_side_bf16(const float (&x)[4], const fl
     return u32x4{static_cast<uint32_t>(lo[0]), static_cast<uint32_t>(hi[0]), static_cast<uint32_t>(lo[1]), static_cast<uint32_t>(hi[1])};
 }
 
-// WM x WN waves of TM x TN matrix tiles, S stages, OCC waves per SIMD.  GATED: the tile's columns are TN / 2 tiles of a wave of either matrix.  SPLIT: the contraction is cut, sums go to parts as they are.
-template <bool I8, bool GATED, bool ACROSS_A, bool ACROSS_B, int WM, int WN, int TM, int TN, int S, int OCC, bool SPLIT, typename T>
-__global__ __attribute__((amdgpu_flat_work_group_size(64 * WM * WN, 64 * WM * WN))) __attribute__((amdgpu_waves_per_eu(OCC, OCC)))
-void tiles_kernel(TileGrid tg) {
-    constexpr int NW = WM * WN, BM = 16 * TM * WM, BN = 16 * TN * WN, kColsOut = GATED ? BN / 2 : BN, TH = GATED ? TN / 2 : TN;
-    constexpr int kALoads = BM / 8 / NW, kBLoads = BN / 8 / NW, kLoads = kALoads + kBLoads;
-    constexpr uint32_t kB = BM * 128, kStage = kB + BN * 128;
+// WM x WN waves of TM x TN matrix tiles, S stages.  GATED: the tile's columns are TN / 2 tiles of a wave of either matrix.  SPLIT: the contraction is cut, sums go to parts as they are.
+template <bool I8_, bool GATED_, bool ACROSS_A_, bool ACROSS_B_, int WM_, int WN_, int TM_, int TN_, int S_, bool SPLIT_, typename T_>
+struct Tiles {
+    static constexpr bool I8 = I8_, GATED = GATED_, ACROSS_A = ACROSS_A_, ACROSS_B = ACROSS_B_, SPLIT = SPLIT_;
+    static constexpr int WM = WM_, WN = WN_, TM = TM_, TN = TN_, S = S_;
+    typedef T_ T;
+    static constexpr int NW = WM * WN, BM = 16 * TM * WM, BN = 16 * TN * WN, kColsOut = GATED ? BN / 2 : BN, TH = GATED ? TN / 2 : TN;
+    static constexpr uint32_t kB = BM * 128, kStage = kB + BN * 128;
+    // scales and biases of a tile's columns and scales of its rows, in LDS, for every tile that is under way (a tile may have one stage): a slot is kLines lines of kColsOut floats and BM floats
+    static constexpr uint32_t kLines = SPLIT || ACROSS_B ? 0 : (I8 ? 2 : 1) * (GATED ? 2 : 1), kSlot = 4 * (kLines * kColsOut + (I8 && !SPLIT ? BM : 0)), kSlots = S + 2, kParams = S * kStage;
+    static constexpr uint32_t kLds = kParams + kSlots * kSlot;
     static_assert(BM % (8 * NW) == 0 && BN % (8 * NW) == 0 && (!GATED || TN % 2 == 0) && !(I8 && (ACROSS_A || ACROSS_B)) && !(GATED && ACROSS_B), "whole loads");
+};
+
+// The tiles that workgroup `block` of `groups` takes.
+template <typename C>
+__device__ __forceinline__ void tiles_body(const TileGrid &tg, const uint32_t block, const uint32_t groups, uint8_t *lds) {
+    constexpr bool I8 = C::I8, GATED = C::GATED, ACROSS_A = C::ACROSS_A, ACROSS_B = C::ACROSS_B, SPLIT = C::SPLIT;
+    constexpr int WN = C::WN, TM = C::TM, TN = C::TN, S = C::S, NW = C::NW, BM = C::BM, BN = C::BN, kColsOut = C::kColsOut, TH = C::TH;
+    constexpr uint32_t kB = C::kB, kStage = C::kStage, kLines = C::kLines, kSlot = C::kSlot, kSlots = C::kSlots, kParams = C::kParams;
+    typedef typename C::T T;
+    constexpr int kALoads = BM / 8 / NW, kBLoads = BN / 8 / NW, kLoads = kALoads + kBLoads;
+    constexpr int kParamLoads = (kSlot / 4 + 64 * NW - 1) / (64 * NW);
+    constexpr int kStores = TM * (T::kBytes == 2 && TH % 2 == 0 ? TH / 2 : TH);
     typedef typename SumOf<I8>::type Sum;
-    __shared__ __attribute__((aligned(1024))) uint8_t lds[S * kStage];
     const TiledArgs &g = tg.g;
     const uint32_t lds0 = lds_offset(lds);
     const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave / WN, wn = wave % WN;
-    const uint32_t groups = gridDim.x, tiles = tg.tiles_m * tg.tiles_n, items = SPLIT ? tiles * tg.splits : tiles;
+    const uint32_t tiles = tg.tiles_m * tg.tiles_n, items = SPLIT ? tiles * tg.splits : tiles;
 
     struct Place {
         uint32_t m0, n0, part, first, stages;
@@ -84,7 +99,7 @@ void tiles_kernel(TileGrid tg) {
     auto load_piece = [&](uint32_t i) { return 16 * ((lane & 7u) ^ (load_row(i) >> 1 & 7u)); };
     const uint8_t *a_from, *b_from, *b2_from = nullptr;
     uint32_t off[kLoads];
-    uint32_t ask_item = blockIdx.x, ask_stage, ask_end;
+    uint32_t ask_item = block, ask_stage, ask_end, ask_slot = 0, slot = 0;
     uint64_t lanes = ~0ull;                    // none once everything has been asked for
     const uint64_t a_step = ACROSS_A ? 64 * g.a_pitch : 128, b_step = ACROSS_B ? 64 * g.b_pitch : 128;
     auto ask_for = [&](uint32_t item) {
@@ -110,6 +125,19 @@ void tiles_kernel(TileGrid tg) {
         }
         ask_stage = p.first;
         ask_end = p.first + p.stages;
+        // (more loads on their way than the waits count make these stricter)
+        for_constants<kParamLoads>([&](auto i) {
+            const uint32_t x = 64 * (wave + NW * i.value) + lane, line = x / kColsOut, rows_from = kLines * kColsOut;
+            const float *array = line % 4 == 0 ? (I8 ? g.f.scale : g.f.bias) : line % 4 == 1 ? (I8 ? g.f.bias : g.f.bias2) : line % 4 == 2 ? g.f.scale2 : g.f.bias2;
+            const float *own = array + min(p.n0 + x % kColsOut, g.N - 1);
+            if (I8 && x >= rows_from) {
+                array = g.f.row_scale;
+                own = array + min(p.m0 + x - rows_from, g.M - 1);
+            }
+            const uint64_t mine = __ballot(x < kSlot / 4 && array);
+            load_dwords(own, __builtin_amdgcn_readfirstlane(lds0 + kParams + ask_slot * kSlot + 256 * (wave + NW * i.value)), mine);
+        });
+        ask_slot = ask_slot + 1 == kSlots ? 0 : ask_slot + 1;
     };
     const uint32_t to = lds0 + 1024 * wave;
     struct From {
@@ -192,14 +220,23 @@ void tiles_kernel(TileGrid tg) {
             __builtin_amdgcn_sched_barrier(0);
         });
     };
-    // Waits for the next stage: it is there when at most the loads of the S - 2 after it are on their way.  (At the end it is nothing that is waited for, read and asked for.  Loads without lanes are not relied on to count.)
+    // Waits for the next stage: it is there when at most the loads of the S - 2 after it, and the stores behind loads of its own age, are on their way.  (At the end it is nothing that is waited for, read and asked for.
+    // Loads without lanes are not relied on to count.)
+    uint32_t behind = 0;                       // so many stages yet that were asked for before the last stores
     auto wait_for_next = [&]() {
+        constexpr int kLater = (S - 2) * kLoads;
         if (lanes == 0) wait_loads_and_sync<0>();
-        else wait_loads_and_sync<(S - 2) * kLoads>();
+        else if (behind > 0) wait_loads_and_sync<(kLater + kStores < 63 ? kLater + kStores : 63)>();
+        else wait_loads_and_sync<kLater>();
+        behind -= behind > 0 ? 1 : 0;
         cur = cur == (S - 1) * kStage ? 0 : cur + kStage;
         far = far == (S - 1) * kStage ? 0 : far + kStage;
     };
 
+    if constexpr (kLines > 0) {                // absent biases are zeros
+        for (uint32_t x = threadIdx.x; x < kSlots * kSlot / 4; x += 64 * NW) *reinterpret_cast<float *>(lds + kParams + 4 * x) = 0.0f;
+        sync_lds();
+    }
     ask_for(ask_item);
 #pragma unroll
     for (uint32_t i = 0; i < S - 1; ++i) {
@@ -210,9 +247,14 @@ void tiles_kernel(TileGrid tg) {
     else wait_loads_and_sync<0>();
     load_stage(far);
     next_stage();
-    for_constants<TM>([&](auto i) { read_a(UintTag<0>{}, i); });
-    for_constants<TN>([&](auto i) { read_b(UintTag<0>{}, i); });
-    for (uint32_t item = blockIdx.x; item < items; item += groups) {
+    // (read again behind the largest tile's results, which need the registers)
+    constexpr bool kReadAgain = !SPLIT && TM * TN == 32;
+    auto first_reads = [&]() {
+        for_constants<TM>([&](auto i) { read_a(UintTag<0>{}, i); });
+        for_constants<TN>([&](auto i) { read_b(UintTag<0>{}, i); });
+    };
+    first_reads();
+    for (uint32_t item = block; item < items; item += groups) {
         const Place p = locate(item);
 #pragma unroll
         for (int i = 0; i < TM; ++i)
@@ -249,66 +291,115 @@ void tiles_kernel(TileGrid tg) {
             }
         } else {
             const Finish &f = g.f;
-#pragma unroll
-            for (uint32_t i = 0; i < TM; ++i) {
-                const uint32_t m = m_wave + 16 * i;
-                const float row_scale = I8 ? f.row_scale[min(m, g.M - 1)] : 1.0f;
-                typename T::type *row = m < g.M ? row_of<T>(f, m) : nullptr;
-                auto finished = [&](uint32_t j, Four &sg, Four &su) {
-                    const uint32_t n = n_wave + 16 * j + 4 * q, at = min(n, g.N - 1), left = g.N - at;
-                    if constexpr (GATED) return finish_gated(f, acc[i][j], acc[i][j + TH], row_scale, at, left, sg, su);
-                    else return finish_plain(f, acc[i][j], row_scale, at, left);
-                };
-                // (all lanes take part in the exchange)
-                auto store_two = [&](uint16_t *to_row, const float (&x)[4], const float (&y)[4], uint32_t j) {
-                    const u32x4 w = side_by_side_bf16(x, y);
-                    const uint32_t n = n_wave + 16 * (j + (q & 1u)) + 8 * (q >> 1);
-                    if (!to_row || n >= g.N) return;
-                    if (n + 8 <= g.N) {
-                        __builtin_memcpy(to_row + n, &w, 16);
+            const uint8_t *params = lds + kParams + slot * kSlot;
+            slot = slot + 1 == kSlots ? 0 : slot + 1;
+            const bool upper = p.m0 + BM <= f.rows, lower = f.c2 && p.m0 >= f.second && p.m0 - f.second + BM <= f.rows;
+            const bool stored = (upper || lower) && p.n0 + kColsOut <= g.N;   // a whole tile
+            typename T::type *const c_tile = upper ? static_cast<typename T::type *>(f.c) + p.m0 * f.ldc : static_cast<typename T::type *>(f.c2) + (p.m0 - f.second) * f.ldc;   // (of a whole tile)
+            auto line = [&](uint32_t index, uint32_t j) { return *reinterpret_cast<const f32x4 *>(params + 4 * (index * kColsOut + 16 * (TH * wn + j) + 4 * q)); };
+            auto columns = [&](uint32_t j) {
+                const f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
+                if constexpr (kLines == 0) return Columns{zero, zero, zero, zero};
+                else if constexpr (I8 && GATED) return Columns{line(0, j), line(2, j), line(1, j), line(3, j)};
+                else if constexpr (I8) return Columns{line(0, j), zero, line(1, j), zero};
+                else return Columns{zero, zero, line(0, j), line(1, j)};
+            };
+            constexpr uint32_t kTogether = TH % 2 == 0 ? 2 : 1;
+            // Large results in bf16 go past the caches: gated 8192 x 4096 x 1024 with slopes 168 -> 150 us, in 8 bits 102 -> 96 us; plain 8192 x 4096 x 1024 in 8 bits 42 us, 44 so.
+            const bool streams = static_cast<uint64_t>(g.M) * g.N >= (GATED ? 16u << 20 : 64u << 20) && (f.ldc | f.ld_slope) % 64 == 0 &&
+                                 ((reinterpret_cast<uintptr_t>(f.c) | reinterpret_cast<uintptr_t>(f.slope_g) | reinterpret_cast<uintptr_t>(f.slope_u)) & 15u) == 0;
+            auto rows = [&](auto kind, auto keep, auto whole) {
+                constexpr bool KEEP = decltype(keep)::value, WHOLE = decltype(whole)::value;
+                const uint32_t two_from = n_wave + 16 * (q & 1u) + 8 * (q >> 1), four_from = n_wave + 4 * q;
+                auto store_eight = [&](uint16_t *to_row, const u32x4 &w, uint32_t j) {
+                    uint16_t *const at = to_row + 16 * j;
+                    if constexpr (WHOLE) {
+                        if (streams) __builtin_nontemporal_store(w, reinterpret_cast<u32x4 *>(at));
+                        else __builtin_memcpy(at, &w, 16);
                     } else {
+                        const uint32_t n = two_from + 16 * j;
+                        if (!to_row || n >= g.N) return;
+                        if (n + 8 <= g.N) {
+                            __builtin_memcpy(at, &w, 16);
+                        } else {
 #pragma unroll
-                        for (uint32_t e = 0; e < 8; ++e)
-                            if (n + e < g.N) to_row[n + e] = static_cast<uint16_t>(w[e / 2] >> (16 * (e & 1)));
+                            for (uint32_t e = 0; e < 8; ++e)
+                                if (n + e < g.N) at[e] = static_cast<uint16_t>(w[e / 2] >> (16 * (e & 1)));
+                        }
                     }
                 };
                 auto store_four = [&](auto type, auto *to_row, const float (&x)[4], uint32_t j) {
                     const uint32_t n = n_wave + 16 * j + 4 * q;
-                    if (to_row && n < g.N) store_run<decltype(type), 4>(to_row + n, x, g.N - n);
+                    if (WHOLE || (to_row && n < g.N)) store_run<decltype(type), 4>(to_row + 16 * j, x, WHOLE ? 4 : g.N - n);
                 };
-                const bool keep = GATED && f.slope_g;
-                uint16_t *row_g = keep && m < g.M ? f.slope_g + m * f.ld_slope : nullptr, *row_u = keep && m < g.M ? f.slope_u + m * f.ld_slope : nullptr;
-                if constexpr (TH % 2 == 0) {
+                constexpr bool kTwo = T::kBytes == 2 && kTogether >= 2;
 #pragma unroll
-                    for (uint32_t j = 0; j < TH; j += 2) {
-                        Four sg[2], su[2];
-                        const Four x = finished(j, sg[0], su[0]), y = finished(j + 1, sg[1], su[1]);
-                        if constexpr (T::kBytes == 2) {
-                            store_two(row, x.v, y.v, j);
-                        } else {
-                            store_four(T{}, row, x.v, j);
-                            store_four(T{}, row, y.v, j + 1);
-                        }
-                        if (keep) {
-                            store_two(row_g, sg[0].v, sg[1].v, j);
-                            store_two(row_u, su[0].v, su[1].v, j);
-                        }
+                for (uint32_t i = 0; i < TM; ++i) {
+                    const uint32_t m = m_wave + 16 * i;
+                    const float row_scale = I8 ? *reinterpret_cast<const float *>(params + 4 * (kLines * kColsOut + 16 * (TM * wm + i) + r)) : 1.0f;
+                    typename T::type *row = WHOLE ? c_tile + (m - p.m0) * f.ldc : m < g.M ? row_of<T>(f, m) : nullptr;
+                    if (WHOLE || row) row += kTwo ? two_from : four_from;
+                    uint16_t *row_g = nullptr, *row_u = nullptr;
+                    if (KEEP && (WHOLE || m < g.M)) {
+                        row_g = f.slope_g + m * f.ld_slope + (kTogether >= 2 ? two_from : four_from);
+                        row_u = f.slope_u + m * f.ld_slope + (kTogether >= 2 ? two_from : four_from);
                     }
-                } else {
 #pragma unroll
-                    for (uint32_t j = 0; j < TH; ++j) {
-                        Four sg, su;
-                        const Four x = finished(j, sg, su);
-                        store_four(T{}, row, x.v, j);
-                        if (keep) {
-                            store_four(BF16{}, row_g, sg.v, j);
-                            store_four(BF16{}, row_u, su.v, j);
+                    for (uint32_t j = 0; j < TH; j += kTogether) {
+                        Four x[kTogether], sg[kTogether], su[kTogether];
+#pragma unroll
+                        for (uint32_t k = 0; k < kTogether; ++k) {
+                            const Columns c = columns(j + k);
+                            if constexpr (GATED) x[k] = finish_gated<decltype(kind)::value, KEEP>(acc[i][j + k], acc[i][j + k + TH], row_scale, c, sg[k], su[k]);
+                            else x[k] = finish_plain(acc[i][j + k], row_scale, c);
+                        }
+                        // (all lanes take part in the exchange)
+                        auto store_pairs = [&](uint16_t *to_row, const Four(&v)[kTogether]) {
+#pragma unroll
+                            for (uint32_t k = 0; k < kTogether; k += 2) store_eight(to_row, side_by_side_bf16(v[k].v, v[(k + 1) % kTogether].v), j + k);
+                        };
+                        if constexpr (kTwo) {
+                            store_pairs(row, x);
+                        } else {
+#pragma unroll
+                            for (uint32_t k = 0; k < kTogether; ++k) store_four(T{}, row, x[k].v, j + k);
+                        }
+                        if constexpr (KEEP && kTogether >= 2) {
+                            store_pairs(row_g, sg);
+                            store_pairs(row_u, su);
+                        } else if constexpr (KEEP) {
+                            store_four(BF16{}, row_g, sg[0].v, j);
+                            store_four(BF16{}, row_u, su[0].v, j);
                         }
                     }
                 }
-            }
+            };
+            auto all = [&](auto kind, auto keep) { stored ? rows(kind, keep, BoolTag<true>{}) : rows(kind, keep, BoolTag<false>{}); };
+            if constexpr (!GATED) all(IntTag<0>{}, BoolTag<false>{});
+            else for_gate(f.gate, [&](auto kind) { !I8 && f.slope_g ? all(kind, BoolTag<true>{}) : all(kind, BoolTag<false>{}); });
+            behind = stored ? S - 1 : 0;
+            if constexpr (kReadAgain) first_reads();
         }
     }
+}
+
+template <typename C, int OCC>
+__global__ __attribute__((amdgpu_flat_work_group_size(64 * C::NW, 64 * C::NW))) __attribute__((amdgpu_waves_per_eu(OCC, OCC))) void tiles_kernel(TileGrid tg) {
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[C::kLds];
+    tiles_body<C>(tg, blockIdx.x, gridDim.x, lds);
+}
+
+// Two products in one launch, a workgroup for every tile; the second one's begin at a multiple of 8, so that both keep their order over the dies.
+struct PairGrid {
+    TileGrid first, second;
+};
+template <typename C, typename D, int OCC>
+__global__ __attribute__((amdgpu_flat_work_group_size(64 * C::NW, 64 * C::NW))) __attribute__((amdgpu_waves_per_eu(OCC, OCC))) void tiles_pair_kernel(PairGrid pg) {
+    static_assert(C::NW == D::NW, "one workgroup size");
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[C::kLds > D::kLds ? C::kLds : D::kLds];
+    const uint32_t first = pg.first.tiles_m * pg.first.tiles_n, second = (first + 7) / 8 * 8;
+    if (blockIdx.x >= second) tiles_body<D>(pg.second, blockIdx.x - second, pg.second.tiles_m * pg.second.tiles_n, lds);
+    else if (blockIdx.x < first) tiles_body<C>(pg.first, blockIdx.x, first, lds);
 }
 
 // The parts of a split contraction, added in order, and what becomes of the sums.
@@ -338,48 +429,49 @@ __global__ __launch_bounds__(256) void join_kernel(TiledArgs g, uint32_t splits)
         return t;
     };
     const float row_scale = I8 ? g.f.row_scale[m] : 1.0f;
+    const Columns columns = columns_from<I8, GATED>(g.f, n, g.N);
     typename T::type *row = row_of<T>(g.f, m);
     if constexpr (GATED) {
-        Four sg, su;
-        const Four x = finish_gated(g.f, sum_from(n), sum_from(static_cast<uint64_t>(g.N) + n), row_scale, n, left, sg, su);
-        store_run<T, 4>(row + n, x.v, left);
-        if (g.f.slope_g) {
-            store_run<BF16, 4>(g.f.slope_g + m * g.f.ld_slope + n, sg.v, left);
-            store_run<BF16, 4>(g.f.slope_u + m * g.f.ld_slope + n, su.v, left);
-        }
-    } else {
-        const Four x = finish_plain(g.f, sum_from(n), row_scale, n, left);
-        if (row) store_run<T, 4>(row + n, x.v, left);
+        store_gated<T>(g.f, sum_from(n), sum_from(static_cast<uint64_t>(g.N) + n), row_scale, columns, row + n, m, n, left);
+    } else if (row) {
+        store_run<T, 4>(row + n, finish_plain(sum_from(n), row_scale, columns).v, left);
     }
 }
 
-// The tile that a product takes and into how many parts its contraction is cut.
+// Which tile a product takes, and into how many parts its contraction is cut (omc_gated.hip).
 struct TileChoice {
     int tile;
     uint32_t splits;
+    double cost;
 };
 constexpr uint32_t kTileRows[] = {256, 256, 128, 64}, kTileCols[] = {256, 128, 128, 64};
-TileChoice choose_tile(uint32_t M, uint32_t cols, uint32_t stages);   // cols: of both matrices where gated
+TileChoice choose_tile(ProductKind kind, uint32_t M, uint32_t N, uint32_t stages, bool whole);   // whole: not cut
 
-template <bool I8, bool GATED, bool ACROSS_A, bool ACROSS_B, int WM, int WN, int TM, int TN, int S, int OCC, int RESIDENT, typename T>
-static void launch_one(const TileGrid &tg, hipStream_t st) {
-    const uint32_t items = tg.tiles_m * tg.tiles_n * tg.splits, most = 256 * RESIDENT;
-    const dim3 grid(items < most ? items : most), block(64 * WM * WN);
-    if (tg.splits > 1) tiles_kernel<I8, GATED, ACROSS_A, ACROSS_B, WM, WN, TM, TN, S, OCC, true, T><<<grid, block, 0, st>>>(tg);
-    else tiles_kernel<I8, GATED, ACROSS_A, ACROSS_B, WM, WN, TM, TN, S, OCC, false, T><<<grid, block, 0, st>>>(tg);
+static inline TileGrid grid_of(const TiledArgs &pa, int tile, bool gated, uint32_t splits) {
+    const uint32_t bm = kTileRows[tile], bn = kTileCols[tile] / (gated ? 2 : 1);
+    return TileGrid{pa, (pa.M + bm - 1) / bm, (pa.N + bn - 1) / bn, splits, (pa.stages + splits - 1) / splits};
+}
+// f(waves in rows, in columns, matrix tiles of a wave in rows, in columns, stages, waves per SIMD, workgroups of a compute unit)
+template <typename F>
+static void for_tile(int tile, F &&f) {
+    switch (tile) {
+        case 0: f(IntTag<4>{}, IntTag<2>{}, IntTag<4>{}, IntTag<8>{}, IntTag<2>{}, IntTag<2>{}, IntTag<1>{}); break;
+        case 1: f(IntTag<4>{}, IntTag<2>{}, IntTag<4>{}, IntTag<4>{}, IntTag<3>{}, IntTag<2>{}, IntTag<1>{}); break;
+        case 2: f(IntTag<2>{}, IntTag<2>{}, IntTag<4>{}, IntTag<4>{}, IntTag<2>{}, IntTag<2>{}, IntTag<2>{}); break;
+        default: f(IntTag<2>{}, IntTag<2>{}, IntTag<2>{}, IntTag<2>{}, IntTag<4>{}, IntTag<2>{}, IntTag<2>{}); break;
+    }
 }
 template <bool I8, bool GATED, bool ACROSS_A, bool ACROSS_B, typename T>
-static int launch_tiles(const TiledArgs &pa, hipStream_t st) {
-    const uint32_t cols = GATED ? 2 * pa.N : pa.N;
-    const TileChoice c = choose_tile(pa.M, cols, pa.stages);
-    const uint32_t bm = kTileRows[c.tile], bn = kTileCols[c.tile] / (GATED ? 2 : 1);
-    const TileGrid tg{pa, (pa.M + bm - 1) / bm, (pa.N + bn - 1) / bn, c.splits, (pa.stages + c.splits - 1) / c.splits};
-    switch (c.tile) {
-        case 0: launch_one<I8, GATED, ACROSS_A, ACROSS_B, 4, 2, 4, 8, 2, 2, 1, T>(tg, st); break;
-        case 1: launch_one<I8, GATED, ACROSS_A, ACROSS_B, 4, 2, 4, 4, 3, 2, 1, T>(tg, st); break;
-        case 2: launch_one<I8, GATED, ACROSS_A, ACROSS_B, 4, 2, 2, 4, 4, 2, 1, T>(tg, st); break;
-        default: launch_one<I8, GATED, ACROSS_A, ACROSS_B, 2, 2, 2, 2, 4, 2, 2, T>(tg, st); break;
-    }
+static int launch_tiles(const TiledArgs &pa, bool whole, hipStream_t st) {
+    const TileChoice c = choose_tile(ACROSS_A ? kBF16AcrossBoth : ACROSS_B ? kBF16AcrossB : I8 ? (GATED ? kI8Gated : kI8Plain) : kBF16Gated, pa.M, pa.N, pa.stages, whole);
+    const TileGrid tg = grid_of(pa, c.tile, GATED, c.splits);
+    for_tile(c.tile, [&](auto wm, auto wn, auto tm, auto tn, auto s, auto occ, auto resident) {
+        constexpr int WM = decltype(wm)::value, WN = decltype(wn)::value, TM = decltype(tm)::value, TN = decltype(tn)::value, S = decltype(s)::value, OCC = decltype(occ)::value;
+        const uint32_t items = tg.tiles_m * tg.tiles_n * tg.splits, most = 256 * decltype(resident)::value;
+        const dim3 grid(items < most ? items : most), block(64 * WM * WN);
+        if (tg.splits > 1) tiles_kernel<Tiles<I8, GATED, ACROSS_A, ACROSS_B, WM, WN, TM, TN, S, true, T>, OCC><<<grid, block, 0, st>>>(tg);
+        else tiles_kernel<Tiles<I8, GATED, ACROSS_A, ACROSS_B, WM, WN, TM, TN, S, false, T>, OCC><<<grid, block, 0, st>>>(tg);
+    });
     if (c.splits > 1) {
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return static_cast<int>(e);
