@@ -1,4 +1,4 @@
-// What the gated linear layer's products take: operands in bf16 with padded rows, and dg and du.
+// What the gated linear layer's products take: operands in bf16 with padded rows, and dg and du with partial sums of their columns.  Bound by memory.
 #include "omc_mx4.h"
 #include "omc_product.h"
 
@@ -6,7 +6,9 @@ namespace omc {
 
 struct Packs {
     PackArgs p[kMostPacks];
+    uint32_t groups[kMostPacks];               // workgroups of each
 };
+
 template <typename T>
 __device__ __forceinline__ u32x4 eight_bf16(const Eight<T> &v) {
     u32x4 w;
@@ -17,73 +19,96 @@ __device__ __forceinline__ u32x4 eight_bf16(const Eight<T> &v) {
     }
     return w;
 }
-__global__ __launch_bounds__(256) void pack_kernel(Packs packs) {
-    const PackArgs &p = packs.p[blockIdx.y];
-    const uint32_t pieces = p.pitch / 8;
-    const uint64_t count = static_cast<uint64_t>(p.to_rows) * pieces;
-    for (uint64_t at = blockIdx.x * 256ull + threadIdx.x; at < count; at += gridDim.x * 256ull) {
-        const uint32_t row = static_cast<uint32_t>(at / pieces), col = 8 * static_cast<uint32_t>(at % pieces);
-        u32x4 w = {0, 0, 0, 0};
-        if (row < p.rows && col < p.cols) {
-            if (p.bf16) {
-                Eight<BF16> v;
-                v.load(static_cast<const uint16_t *>(p.x) + row * p.ldx, col, p.cols);
-                w = eight_bf16(v);
-            } else {
-                Eight<F32> v;
-                v.load(static_cast<const float *>(p.x) + row * p.ldx, col, p.cols);
-                w = eight_bf16(v);
-            }
-        }
-        *reinterpret_cast<u32x4 *>(p.to + row * static_cast<uint64_t>(p.pitch) + col) = w;
-    }
+// A lane takes eight values.
+template <typename T>
+__device__ __forceinline__ void pack_pieces(const PackArgs &p, uint32_t group) {
+    const uint32_t pieces = p.pitch / 8, row0 = static_cast<uint32_t>(group * 256ull / pieces), rest = static_cast<uint32_t>(group * 256ull - static_cast<uint64_t>(row0) * pieces) + threadIdx.x;
+    const uint32_t down = rest / pieces, row = row0 + down, col = 8 * (rest - down * pieces);
+    if (row >= p.to_rows) return;
+    Eight<T> v;
+    v.clear();
+    if (row < p.rows && col < p.cols) v.load(static_cast<const typename T::type *>(p.x) + row * p.ldx, col, p.cols);
+    *reinterpret_cast<u32x4 *>(p.to + row * static_cast<uint64_t>(p.pitch) + col) = eight_bf16(v);
 }
-int launch_pack(const PackArgs *packs, uint32_t count, void *stream) {
+__device__ __forceinline__ void pack(const Packs &packs, uint32_t group) {
+    const uint32_t second = packs.groups[0], third = second + packs.groups[1], i = group < second ? 0u : group < third ? 1u : 2u;
+    const PackArgs &p = packs.p[i];            // (by number: the arguments stay where they are)
+    group -= i == 0 ? 0u : i == 1 ? second : third;
+    p.bf16 ? pack_pieces<BF16>(p, group) : pack_pieces<F32>(p, group);
+}
+static Packs packs_of(const PackArgs *packs, uint32_t count, uint32_t &groups) {
     Packs all{};
-    uint64_t most = 0;
+    groups = 0;
     for (uint32_t i = 0; i < count; ++i) {
         all.p[i] = packs[i];
         const uint64_t n = static_cast<uint64_t>(packs[i].to_rows) * (packs[i].pitch / 8);
-        most = n > most ? n : most;
+        all.groups[i] = static_cast<uint32_t>((n + 255) / 256);
+        groups += all.groups[i];
     }
-    const uint64_t groups = (most + 255) / 256;
-    pack_kernel<<<dim3(static_cast<uint32_t>(groups < 8192 ? groups : 8192), count), dim3(256), 0, static_cast<hipStream_t>(stream)>>>(all);
+    return all;
+}
+__global__ __launch_bounds__(256) void pack_kernel(Packs packs) { pack(packs, blockIdx.x); }
+int launch_pack(const PackArgs *packs, uint32_t count, void *stream) {
+    uint32_t groups;
+    const Packs all = packs_of(packs, count, groups);
+    pack_kernel<<<dim3(groups), dim3(256), 0, static_cast<hipStream_t>(stream)>>>(all);
     return static_cast<int>(hipGetLastError());
 }
 
-// A workgroup takes kSlopeRows rows x 512 columns, a wave every fourth row, a lane eight columns.
-template <typename T>
-__global__ __launch_bounds__(256) void slopes_kernel(SlopeArgs sa) {
+// A workgroup takes 4 * EACH rows x 512 columns, a wave every fourth row, a lane eight columns.  The workgroups behind theirs copy operands.  Of few rows a wave asks for all four together; of many for one at a time, which leaves
+// registers for more waves (8192 x 4096, bf16, sums alone: four at a time 47 us, two 44, one 41).
+struct SlopeGrid {
+    SlopeArgs s;
+    uint32_t across, groups;
+    Packs packs;
+};
+template <typename T, int EACH>
+__global__ __launch_bounds__(256) void slopes_kernel(SlopeGrid sg) {
     __shared__ float sums[4][2][512];
-    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, col = blockIdx.x * 512 + 8 * lane, row0 = blockIdx.y * kSlopeRows;
+    if (blockIdx.x >= sg.groups) {
+        pack(sg.packs, blockIdx.x - sg.groups);
+        return;
+    }
+    const SlopeArgs &sa = sg.s;
+    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, down = blockIdx.x / sg.across, col0 = (blockIdx.x - down * sg.across) * 512, col = col0 + 8 * lane, row0 = down * (4 * EACH);
+    constexpr uint32_t kTogether = EACH == 4 ? 4 : 1;
     float s[2][8] = {};
-#pragma unroll 4
-    for (uint32_t i = 0; i < kSlopeRows / 4; ++i) {
-        const uint32_t row = row0 + 4 * i + wave;
-        if (row >= sa.to_rows) break;
-        u32x4 w[2] = {};
-        if (row < sa.M && col < sa.N) {
-            Eight<T> dh;
-            Eight<BF16> slope[2];
-            dh.load(static_cast<const typename T::type *>(sa.dh) + row * sa.lddh, col, sa.N);
-            slope[0].load(sa.slope_g + row * sa.ld_slope, col, sa.N);
-            slope[1].load(sa.slope_u + row * sa.ld_slope, col, sa.N);
+#pragma unroll 1
+    for (uint32_t first = 0; first < EACH; first += kTogether) {
+        Eight<T> dh[kTogether];
+        Eight<BF16> slope[kTogether][2];
+#pragma unroll
+        for (uint32_t k = 0; k < kTogether; ++k) {
+            const uint32_t row = row0 + 4 * (first + k) + wave;
+            dh[k].clear();
+            slope[k][0].clear();
+            slope[k][1].clear();
+            if (row < sa.M && col < sa.N) {
+                dh[k].load(static_cast<const typename T::type *>(sa.dh) + row * sa.lddh, col, sa.N);
+                slope[k][0].load(sa.slope_g + row * sa.ld_slope, col, sa.N);
+                slope[k][1].load(sa.slope_u + row * sa.ld_slope, col, sa.N);
+            }
+        }
+#pragma unroll
+        for (uint32_t k = 0; k < kTogether; ++k) {
+            const uint32_t row = row0 + 4 * (first + k) + wave;
+            u32x4 w[2];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 float d[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    d[e] = dh.value(e) * slope[h].value(e);
+                    d[e] = dh[k].value(e) * slope[k][h].value(e);
                     s[h][e] += d[e];
                 }
 #pragma unroll
                 for (int e = 0; e < 4; ++e) w[h][e] = to_bf16_pair(d[2 * e], d[2 * e + 1]);
             }
-        }
-        if (sa.to && col < sa.half) {
-            uint16_t *to = sa.to + row * (2ull * sa.half) + col;
-            *reinterpret_cast<u32x4 *>(to) = w[0];
-            *reinterpret_cast<u32x4 *>(to + sa.half) = w[1];
+            if (sa.to && row < sa.to_rows && col < sa.half) {
+                uint16_t *to = sa.to + row * (2ull * sa.half) + col;
+                *reinterpret_cast<u32x4 *>(to) = w[0];
+                *reinterpret_cast<u32x4 *>(to + sa.half) = w[1];
+            }
         }
     }
     if (!sa.sums || row0 >= sa.M) return;
@@ -93,15 +118,26 @@ __global__ __launch_bounds__(256) void slopes_kernel(SlopeArgs sa) {
         for (int e = 0; e < 8; ++e) sums[wave][h][8 * lane + e] = s[h][e];
     __syncthreads();
     for (uint32_t t = threadIdx.x; t < 1024; t += 256) {
-        const uint32_t h = t / 512, c = t % 512, n = blockIdx.x * 512 + c;
-        if (n < sa.N) sa.sums[(static_cast<uint64_t>(blockIdx.y) * 2 + h) * sa.N + n] = ((sums[0][h][c] + sums[1][h][c]) + sums[2][h][c]) + sums[3][h][c];
+        const uint32_t h = t / 512, c = t % 512, n = col0 + c;
+        if (n < sa.N) sa.sums[(static_cast<uint64_t>(down) * 2 + h) * sa.N + n] = ((sums[0][h][c] + sums[1][h][c]) + sums[2][h][c]) + sums[3][h][c];
     }
 }
-int launch_slopes(const SlopeArgs &sa, void *stream) {
+// 16 rows a workgroup where 64 would leave compute units without one: VVV
+uint32_t slope_rows(uint32_t M, uint32_t N) { return static_cast<uint64_t>((M + 63) / 64) * ((N + 511) / 512) >= 512 ? 64 : 16; }
+
+template <typename T>
+static void launch_typed(const SlopeGrid &sg, uint32_t rows, uint32_t groups, hipStream_t st) {
+    if (rows == 64) slopes_kernel<T, 16><<<dim3(groups), dim3(256), 0, st>>>(sg);
+    else slopes_kernel<T, 4><<<dim3(groups), dim3(256), 0, st>>>(sg);
+}
+int launch_slopes(const SlopeArgs &sa, const PackArgs *packs, uint32_t count, void *stream) {
     hipStream_t st = static_cast<hipStream_t>(stream);
-    const dim3 grid((sa.half + 511) / 512, (sa.to_rows + kSlopeRows - 1) / kSlopeRows), block(256);
-    if (sa.bf16) slopes_kernel<BF16><<<grid, block, 0, st>>>(sa);
-    else slopes_kernel<F32><<<grid, block, 0, st>>>(sa);
+    const uint32_t rows = slope_rows(sa.M, sa.N), across = (sa.half + 511) / 512, groups = (sa.to_rows + rows - 1) / rows * across;
+    uint32_t more;
+    const Packs all = packs_of(packs, count, more);
+    const SlopeGrid sg{sa, across, groups, all};
+    if (sa.bf16) launch_typed<BF16>(sg, rows, groups + more, st);
+    else launch_typed<F32>(sg, rows, groups + more, st);
     return static_cast<int>(hipGetLastError());
 }
 

@@ -1,0 +1,58 @@
+// Device side of I8: a row of values shares a scale and holds a whole number each.
+//
+//   a = max |x_i|,  s = a / 127 rounded to fp32,  code_i = the whole number nearest to x_i / s, ties to even.
+// The quotient is never formed exactly: r = rint(x * (1 / s)) is off by at most one, and d = x - r s, which fp32 holds exactly (r = 0: x itself; r = 1: both are within a factor of two; otherwise x > s, and d is a
+// multiple of s' last place below s / 2 and a little), says whether the neighbour is nearer.  That is asked where x * (1 / s) comes within 2^-12 of halfway between two whole numbers (it is off by 2^-15 at most).  Scales below 2^-100 are handled times 2^100, which is exact.
+#pragma once
+#include "omc_mx4.h"
+
+namespace omc {
+
+struct Rounding {
+    float scale, up, s, inverse;
+    bool nan;
+    __device__ __forceinline__ void of(float top, bool is_nan) {
+        nan = is_nan;
+        scale = is_nan ? __builtin_nanf("") : top / 127.0f;
+        up = scale < 0x1p-100f ? 0x1p100f : 1.0f;
+        s = is_nan || scale == 0.0f ? 1.0f : scale * up;
+        inverse = is_nan || scale == 0.0f ? 0.0f : 1.0f / s;         // 0: all codes are 0
+    }
+    __device__ __forceinline__ float code(float x) const {
+        if (inverse == 0.0f) return 0.0f;
+        const float v = x * up;
+        float r = rintf(v * inverse);
+        const float d = fmaf(-r, s, v), twice = fabsf(d + d);
+        const bool odd = static_cast<int>(r) & 1;
+        if (twice > s || (twice == s && odd)) r += copysignf(1.0f, d);
+        return fminf(fmaxf(r, -127.0f), 127.0f);                     // (a scale below 2^-126 is coarser than its largest value's 127th part)
+    }
+    // Of eight values, where lanes seldom need code(): adding 1.5 * 2^23 rounds to a whole number, ties to even, and leaves it in the low bits.
+    __device__ __forceinline__ void eight(const float (&x)[8], float (&r)[8]) const {
+        constexpr float kWhole = 12582912.0f;
+        float far = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float f = x[i] * inverse;
+            r[i] = (f + kWhole) - kWhole;
+            far = fmaxf(far, fabsf(f - r[i]));
+        }
+        if (far > 0.499755859375f || up != 1.0f || inverse == 0.0f) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) r[i] = code(x[i]);
+        }
+    }
+    __device__ __forceinline__ float value(float r) const { return r * scale; }
+};
+__device__ __forceinline__ uint32_t four_bytes(const float *r) {   // of whole numbers
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = __float_as_uint(r[i] + 12582912.0f);
+    return __builtin_amdgcn_perm(__builtin_amdgcn_perm(w[3], w[2], 0x0c0c0400u), __builtin_amdgcn_perm(w[1], w[0], 0x0c0c0400u), 0x05040100u);
+}
+template <typename T>
+__device__ __forceinline__ float from_top(uint32_t top) {
+    return __uint_as_float(T::kBytes == 4 ? top : top << 16);
+}
+
+}  // namespace omc

@@ -1,44 +1,8 @@
-// omc_i8_quantize: a matrix in fp32 or bf16 to 8-bit integers, a scale for every row or for every column.
-//
-//   a = max |x_i|,  s = a / 127 rounded to fp32,  code_i = the whole number nearest to x_i / s, ties to even.
-// The quotient is never formed exactly: r = rint(x * (1 / s)) is off by at most one, and d = x - r s, which fp32 holds exactly (r = 0: x itself; r = 1: both are within a factor of two; otherwise x > s, and d is a
-// multiple of s' last place below s / 2 and a little), says whether the neighbour is nearer.  Scales below 2^-100 are handled times 2^100, which is exact.
-#include "omc_mx4.h"
+// omc_i8_quantize: a matrix in fp32 or bf16 to 8-bit integers, a scale for every row or for every column (see omc_i8.h).
+#include "omc_i8.h"
 #include "omc_product.h"
 
 namespace omc {
-
-struct Rounding {
-    float scale, up, s, inverse;
-    bool nan;
-    __device__ __forceinline__ void of(float top, bool is_nan) {
-        nan = is_nan;
-        scale = is_nan ? __builtin_nanf("") : top / 127.0f;
-        up = scale < 0x1p-100f ? 0x1p100f : 1.0f;
-        s = is_nan || scale == 0.0f ? 1.0f : scale * up;
-        inverse = is_nan || scale == 0.0f ? 0.0f : 1.0f / s;         // 0: all codes are 0
-    }
-    __device__ __forceinline__ float code(float x) const {
-        if (inverse == 0.0f) return 0.0f;
-        const float v = x * up;
-        float r = rintf(v * inverse);
-        const float d = fmaf(-r, s, v), twice = fabsf(d + d);
-        const bool odd = static_cast<int>(r) & 1;
-        if (twice > s || (twice == s && odd)) r += copysignf(1.0f, d);
-        return fminf(fmaxf(r, -127.0f), 127.0f);                     // (a scale below 2^-126 is coarser than its largest value's 127th part)
-    }
-    __device__ __forceinline__ float value(float r) const { return r * scale; }
-};
-__device__ __forceinline__ uint32_t four_bytes(const float *r) {
-    uint32_t w = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) w |= (static_cast<uint32_t>(static_cast<int>(r[i])) & 255u) << (8 * i);
-    return w;
-}
-template <typename T>
-__device__ __forceinline__ float from_top(uint32_t top) {
-    return __uint_as_float(T::kBytes == 4 ? top : top << 16);
-}
 
 // LANES lanes (64, or the workgroup's 256) take a row, R pieces of eight values each; PIECES in registers.  REREAD: the row is longer, and is read twice.
 template <typename T, int LANES, int R, bool REREAD>
@@ -84,9 +48,10 @@ __global__ __launch_bounds__(256) void i8_rows_kernel(I8Args ia) {
         for (uint32_t k = 0; k < R; ++k) {
             const uint32_t col = from + 8 * (lane + LANES * k);
             if (col >= pitch) continue;
-            float r[8];
+            float x8[8], r[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) r[i] = to.code(v[k].value(i));
+            for (int i = 0; i < 8; ++i) x8[i] = v[k].value(i);
+            to.eight(x8, r);
             const uint64_t w = four_bytes(r) | static_cast<uint64_t>(four_bytes(r + 4)) << 32;
             *reinterpret_cast<uint64_t *>(codes + col) = w;
             if (ia.values && col < ia.cols) {
@@ -98,13 +63,13 @@ __global__ __launch_bounds__(256) void i8_rows_kernel(I8Args ia) {
     }
 }
 
-// A workgroup takes 32 columns, twice: for their largest magnitudes, and for the codes, which go through LDS so that runs of a column are written together.
-template <typename T>
+// A workgroup takes COLS columns, twice: for their largest magnitudes, and for the codes, which go through LDS so that runs of a column are written together.
+template <typename T, int COLS>
 __global__ __launch_bounds__(1024) void i8_columns_kernel(I8Args ia) {
-    constexpr uint32_t kRows = 512, kPitch = kRows + 16;
-    __shared__ __attribute__((aligned(16))) uint8_t turned[32 * kPitch];
-    __shared__ uint32_t tops[16][32];
-    const uint32_t col0 = blockIdx.x * 32, col = col0 + 4 * (threadIdx.x & 7u), line = threadIdx.x >> 3;
+    constexpr uint32_t kAcross = COLS / 4, kLines = 1024 / kAcross, kRows = 4 * kLines, kPitch = kRows + 16;   // lanes of a row, rows at a time
+    __shared__ __attribute__((aligned(16))) uint8_t turned[COLS * kPitch];
+    __shared__ uint32_t tops[16][COLS];
+    const uint32_t across = threadIdx.x % kAcross, line = threadIdx.x / kAcross, col0 = blockIdx.x * COLS, col = col0 + 4 * across;
     const uint32_t inside = col < ia.cols ? min(4u, ia.cols - col) : 0u;
     const typename T::type *x = static_cast<const typename T::type *>(ia.x) + col;
     auto load = [&](uint32_t row, float (&v)[4]) {
@@ -124,10 +89,10 @@ __global__ __launch_bounds__(1024) void i8_columns_kernel(I8Args ia) {
         }
     };
     uint32_t top[4] = {0, 0, 0, 0};
+    float v[4][4];
     for (uint32_t first = 0; first < ia.rows; first += kRows) {
-        float v[4][4];
 #pragma unroll
-        for (uint32_t k = 0; k < 4; ++k) load(first + 128 * k + line, v[k]);
+        for (uint32_t k = 0; k < 4; ++k) load(first + kLines * k + line, v[k]);
 #pragma unroll
         for (uint32_t k = 0; k < 4; ++k)
 #pragma unroll
@@ -136,8 +101,8 @@ __global__ __launch_bounds__(1024) void i8_columns_kernel(I8Args ia) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
 #pragma unroll
-        for (int by = 8; by < 64; by *= 2) top[i] = max(top[i], static_cast<uint32_t>(__shfl_xor(static_cast<int>(top[i]), by)));
-        if ((threadIdx.x & 63u) < 8) tops[threadIdx.x >> 6][4 * (threadIdx.x & 7u) + i] = top[i];
+        for (int by = kAcross; by < 64; by *= 2) top[i] = max(top[i], static_cast<uint32_t>(__shfl_xor(static_cast<int>(top[i]), by)));
+        if ((threadIdx.x & 63u) < kAcross) tops[threadIdx.x >> 6][4 * across + i] = top[i];
     }
     __syncthreads();
     Rounding to[4];
@@ -145,30 +110,35 @@ __global__ __launch_bounds__(1024) void i8_columns_kernel(I8Args ia) {
     for (int i = 0; i < 4; ++i) {
         uint32_t t = 0;
 #pragma unroll
-        for (int w = 0; w < 16; ++w) t = max(t, tops[w][4 * (threadIdx.x & 7u) + i]);
+        for (int w = 0; w < 16; ++w) t = max(t, tops[w][4 * across + i]);
         to[i].of(__uint_as_float(t), t > 0x7f7fffffu);
         if (line == 0 && static_cast<uint32_t>(i) < inside) ia.scales[col + i] = to[i].scale;
     }
     const uint64_t pitch = i8_pitch(ia.rows);
     for (uint32_t first = 0; first < ia.rows; first += kRows) {
-        float v[4][4];
+        if (ia.rows > kRows) {                 // (otherwise they are there)
 #pragma unroll
-        for (uint32_t k = 0; k < 4; ++k) load(first + 128 * k + line, v[k]);
+            for (uint32_t k = 0; k < 4; ++k) load(first + kLines * k + line, v[k]);
+        }
 #pragma unroll
         for (uint32_t k = 0; k < 4; ++k) {
-            const uint32_t row = first + 128 * k + line;
+            const uint32_t row = first + kLines * k + line;
             float r[4];
 #pragma unroll
             for (uint32_t i = 0; i < 4; ++i) {
                 r[i] = to[i].code(v[k][i]);
-                turned[(4 * (threadIdx.x & 7u) + i) * kPitch + 128 * k + line] = static_cast<uint8_t>(static_cast<int>(r[i]));
+                turned[(4 * across + i) * kPitch + kLines * k + line] = static_cast<uint8_t>(static_cast<int>(r[i]));
                 r[i] = to[i].value(r[i]);
             }
             if (ia.values && row < ia.rows && inside > 0) store_run<T, 4>(static_cast<typename T::type *>(ia.values) + row * ia.ldv + col, r, inside);
         }
         __syncthreads();
-        const uint32_t c = threadIdx.x / 32, at = 16 * (threadIdx.x % 32);
-        if (col0 + c < ia.cols && first + at < pitch) *reinterpret_cast<u32x4 *>(ia.codes + (col0 + c) * pitch + first + at) = *reinterpret_cast<const u32x4 *>(turned + c * kPitch + at);
+#pragma unroll
+        for (uint32_t c = threadIdx.x / (kRows / 16); c < COLS; c += 1024 / (kRows / 16)) {
+            const uint32_t at = 16 * (threadIdx.x % (kRows / 16));
+            if (col0 + c < ia.cols && first + at < pitch)
+                *reinterpret_cast<u32x4 *>(ia.codes + (col0 + c) * pitch + first + at) = *reinterpret_cast<const u32x4 *>(turned + c * kPitch + at);
+        }
         __syncthreads();
     }
 }
@@ -188,11 +158,13 @@ int launch_i8_rows(const I8Args &ia, bool bf16, void *stream) {
     hipStream_t st = static_cast<hipStream_t>(stream);
     return bf16 ? launch_rows<BF16>(ia, st) : launch_rows<F32>(ia, st);
 }
+// 32 columns where that makes a workgroup for every second compute unit, otherwise 8, which are parts of cache lines: VVV
 int launch_i8_columns(const I8Args &ia, bool bf16, void *stream) {
     hipStream_t st = static_cast<hipStream_t>(stream);
-    const dim3 grid((ia.cols + 31) / 32), block(1024);
-    if (bf16) i8_columns_kernel<BF16><<<grid, block, 0, st>>>(ia);
-    else i8_columns_kernel<F32><<<grid, block, 0, st>>>(ia);
+    const bool wide = ia.cols >= 32 * 128;
+    const dim3 grid((ia.cols + (wide ? 31 : 7)) / (wide ? 32 : 8)), block(1024);
+    if (bf16) wide ? i8_columns_kernel<BF16, 32><<<grid, block, 0, st>>>(ia) : i8_columns_kernel<BF16, 8><<<grid, block, 0, st>>>(ia);
+    else wide ? i8_columns_kernel<F32, 32><<<grid, block, 0, st>>>(ia) : i8_columns_kernel<F32, 8><<<grid, block, 0, st>>>(ia);
     return static_cast<int>(hipGetLastError());
 }
 

@@ -30,7 +30,8 @@ size_t product_workspace(ProductKind kind, uint32_t M, uint32_t N, uint32_t stag
 int launch_product_tiles(ProductKind kind, const TiledArgs &pa, bool whole, bool c_bf16, void *stream);   // whole: the contraction is not cut
 // Of a gated layer's backward products, M x N as kBF16AcrossB and M2 x N2 as kBF16AcrossBoth (its result in fp32): the tile in which both go together, uncut, in one launch; -1: each goes its own way.
 int product_pair_tile(uint32_t M, uint32_t N, uint32_t stages, uint32_t M2, uint32_t N2, uint32_t stages2);
-int launch_product_pair(int tile, const TiledArgs &dx, bool dx_bf16, const TiledArgs &dw, void *stream);
+// In the same launch columns' sums, of `count` rows of partial sums, 2 * cols floats each, to out0 and out1 (as launch_column_sums; both may be null: none).
+int launch_product_pair(int tile, const TiledArgs &dx, bool dx_bf16, const TiledArgs &dw, const float *sums, uint32_t count, uint32_t cols, float *out0, float *out1, void *stream);
 
 // The same for few rows of A (product_few).  x_type and w_type: 8-bit codes in padded rows (then K is whole 128s), or fp32 or bf16 as they lie, which are rounded to bf16 on the way; pitches in bytes.
 // rounds: A comes in fp32 or bf16 and becomes 8-bit codes on the way (product_few_rounds).
@@ -41,6 +42,7 @@ struct FewArgs {
     const void *w, *w2;
     uint64_t ldw;
     uint32_t M, N, K;
+    uint32_t columns;                    // values of a row of A, where it becomes codes
     Finish f;
 };
 bool product_few(uint32_t M, uint32_t N, uint32_t K);
@@ -74,8 +76,8 @@ constexpr uint32_t kMostPacks = 3;
 int launch_pack(const PackArgs *packs, uint32_t count, void *stream);
 
 // dg and du: dh times its slopes in fp32, rounded to bf16, side by side in rows of 2 * half values (zeros behind N and up to to_rows; may be null), and partial sums of their columns, a row of 2 N floats for every
-// 64 rows (may be null).
-constexpr uint32_t kSlopeRows = 64;
+// slope_rows rows (may be null).  By the same launch copies, as above.
+uint32_t slope_rows(uint32_t M, uint32_t N);
 struct SlopeArgs {
     const void *dh;
     uint64_t lddh;
@@ -86,6 +88,6 @@ struct SlopeArgs {
     uint16_t *to;
     float *sums;
 };
-int launch_slopes(const SlopeArgs &sa, void *stream);
+int launch_slopes(const SlopeArgs &sa, const PackArgs *packs, uint32_t count, void *stream);
 
 }  // namespace omc

@@ -54,8 +54,7 @@ struct I8Operands {
 static uint64_t i8_parts(ProductKind kind, uint32_t M, uint32_t N, uint32_t K) {
     return product_few(M, N, K) ? 0 : product_workspace(kind, M, N, static_cast<uint32_t>(i8_pitch(K) / 128));
 }
-static int i8_product(const void *codes, const float *scales, const I8Operands &o, bool gated, void *C, bool c_bf16, uint64_t ldc, uint32_t M, uint32_t N, uint32_t K, void *parts, void *stream) {
-    const uint64_t pitch = i8_pitch(K);
+static Finish i8_finish(const float *scales, const I8Operands &o, void *C, uint64_t ldc, uint32_t M) {
     Finish f = finish(C, ldc, M);
     f.row_scale = scales;
     f.scale = o.w_scale;
@@ -63,7 +62,12 @@ static int i8_product(const void *codes, const float *scales, const I8Operands &
     f.bias = o.bias;
     f.bias2 = o.bias2;
     f.gate = o.gate;
-    if (product_few(M, N, K)) return launch_product_few(kE8, kE8, gated, FewArgs{codes, pitch, o.w, o.w2, pitch, M, N, static_cast<uint32_t>(pitch), f}, c_bf16, stream);
+    return f;
+}
+static int i8_product(const void *codes, const float *scales, const I8Operands &o, bool gated, void *C, bool c_bf16, uint64_t ldc, uint32_t M, uint32_t N, uint32_t K, void *parts, void *stream) {
+    const uint64_t pitch = i8_pitch(K);
+    const Finish f = i8_finish(scales, o, C, ldc, M);
+    if (product_few(M, N, K)) return launch_product_few(kE8, kE8, gated, FewArgs{codes, pitch, o.w, o.w2, pitch, M, N, static_cast<uint32_t>(pitch), 0, f}, c_bf16, stream);
     const uint32_t stages = static_cast<uint32_t>(pitch / 128);
     return launch_product_tiles(gated ? kI8Gated : kI8Plain, TiledArgs{codes, o.w, o.w2, pitch, pitch, M, N, stages, stages, N, f, parts}, false, c_bf16, stream);
 }
@@ -75,6 +79,7 @@ struct I8Layout {
 };
 static I8Layout i8_layout(uint8_t *ws, bool gated, uint32_t M, uint32_t N, uint32_t K) {
     I8Layout l{};
+    if (product_few(M, N, K) && product_few_rounds(M, K)) return l;
     Parts p{ws};
     l.codes = p.take(M * i8_pitch(K));
     l.scales = reinterpret_cast<float *>(p.take(4ull * M));
@@ -91,6 +96,11 @@ static omc_status i8_layer(const void *X, omc_type x_type, uint64_t ldx, const I
         return OMC_ERR_ALIGN;
     const I8Layout l = i8_layout(static_cast<uint8_t *>(ws), gated, M, N, K);
     if (const omc_status s = check_workspace(ws, ws_bytes, l.bytes)) return s;
+    if (l.bytes == 0) {
+        const uint64_t pitch = i8_pitch(K);
+        const FewArgs fa{X, ldx, o.w, o.w2, pitch, M, N, static_cast<uint32_t>(pitch), K, i8_finish(nullptr, o, Y, ldy, M)};
+        return from_hip(launch_product_few(element(x_type), kE8, gated, fa, y_type == OMC_BF16, stream));
+    }
     const int rc = launch_i8_rows(I8Args{X, ldx, M, K, l.codes, l.scales, nullptr, 0}, x_type == OMC_BF16, stream);
     return from_hip(rc != 0 ? rc : i8_product(l.codes, l.scales, o, gated, Y, y_type == OMC_BF16, ldy, M, N, K, l.parts, stream));
 }
@@ -123,6 +133,7 @@ static GatedLayout gated_layout(uint8_t *ws, uint32_t M, uint32_t N, uint32_t K)
 }
 // Asked of the sizes alone, so that a gradient's bits do not depend on what is asked for beside it: tiles add up the contraction in the same order, whichever they are, but for where it is cut.
 static int backward_pair(uint32_t M, uint32_t N, uint32_t K) { return product_pair_tile(M, K, to_64(N) / 64 * 2, 2 * to_64(N), K, to_64(M) / 64); }
+static uint32_t sum_rows(uint32_t M, uint32_t N) { return (M + slope_rows(M, N) - 1) / slope_rows(M, N); }
 struct GatedBackwardLayout {
     uint16_t *dgu, *x, *wg, *wu;
     float *sums;
@@ -137,7 +148,7 @@ static GatedBackwardLayout gated_backward_layout(uint8_t *ws, uint32_t M, uint32
     l.x = reinterpret_cast<uint16_t *>(p.take(2 * m * k));
     l.wg = reinterpret_cast<uint16_t *>(p.take(2 * n * k));
     l.wu = reinterpret_cast<uint16_t *>(p.take(2 * n * k));
-    l.sums = reinterpret_cast<float *>(p.take(8ull * ((M + kSlopeRows - 1) / kSlopeRows) * N));
+    l.sums = reinterpret_cast<float *>(p.take(8ull * sum_rows(M, N) * N));
     const bool whole = backward_pair(M, N, K) >= 0;
     const uint64_t dx = whole ? 0 : product_workspace(kBF16AcrossB, M, K, to_64(N) / 64 * 2), dw = whole ? 0 : product_workspace(kBF16AcrossBoth, 2 * to_64(N), K, to_64(M) / 64);
     l.parts = p.take(dx > dw ? dx : dw);
@@ -212,7 +223,7 @@ omc_status omc_gated_linear(const void *X, omc_type x_type, uint64_t ldx, const 
     f.slope_g = static_cast<uint16_t *>(slope_g);
     f.slope_u = static_cast<uint16_t *>(slope_u);
     f.ld_slope = ld_slope;
-    if (product_few(M, N, K)) return from_hip(launch_product_few(element(x_type), element(w_type), true, FewArgs{X, ldx, Wg, Wu, ldw, M, N, K, f}, h_type == OMC_BF16, stream));
+    if (product_few(M, N, K)) return from_hip(launch_product_few(element(x_type), element(w_type), true, FewArgs{X, ldx, Wg, Wu, ldw, M, N, K, 0, f}, h_type == OMC_BF16, stream));
     const uint32_t pitch = to_64(K);
     PackArgs packs[kMostPacks];
     uint32_t count = 0;
@@ -249,10 +260,6 @@ omc_status omc_gated_linear_backward(const void *dH, omc_type dh_type, uint64_t 
     if (const omc_status s = check_workspace(ws, ws_bytes, l.bytes)) return s;
     const bool sums = dbg || dbu;
     const uint32_t rows = to_64(M), half = to_64(N), k = to_64(K);
-    int rc = launch_slopes(SlopeArgs{dH, lddh, dh_type == OMC_BF16, static_cast<const uint16_t *>(slope_g), static_cast<const uint16_t *>(slope_u), ld_slope, M, N, rows, half, dX || dWg ? l.dgu : nullptr,
-                                     sums ? l.sums : nullptr},
-                           stream);
-    if (rc == 0 && sums) rc = launch_column_sums(l.sums, (M + kSlopeRows - 1) / kSlopeRows, false, N, 2 * N, dbg, dbu, stream);
     PackArgs packs[kMostPacks];
     uint32_t count = 0;
     TiledArgs for_dx{l.dgu, Wg, Wu, 4ull * half, 2 * ldw, M, K, half / 64 * 2, half / 64, K, finish(dX, lddx, M), l.parts};
@@ -273,9 +280,12 @@ omc_status omc_gated_linear_backward(const void *dH, omc_type dh_type, uint64_t 
         for_dw.b_pitch = 2ull * k;
         for_dw.b_cols = k;
     }
-    if (rc == 0 && count > 0) rc = launch_pack(packs, count, stream);
+    const SlopeArgs sa{dH, lddh, dh_type == OMC_BF16, static_cast<const uint16_t *>(slope_g), static_cast<const uint16_t *>(slope_u), ld_slope, M, N, rows, half, dX || dWg ? l.dgu : nullptr,
+                       sums ? l.sums : nullptr};
+    int rc = launch_slopes(sa, packs, count, stream);
     const int pair = backward_pair(M, N, K);
-    if (rc == 0 && pair >= 0 && dX && dWg) return from_hip(launch_product_pair(pair, for_dx, dx_type == OMC_BF16, for_dw, stream));
+    if (rc == 0 && pair >= 0 && dX && dWg) return from_hip(launch_product_pair(pair, for_dx, dx_type == OMC_BF16, for_dw, l.sums, sum_rows(M, N), N, dbg, dbu, stream));
+    if (rc == 0 && sums) rc = launch_column_sums(l.sums, sum_rows(M, N), false, N, 2 * N, dbg, dbu, stream);
     if (rc == 0 && dX) rc = launch_product_tiles(kBF16AcrossB, for_dx, pair >= 0, dx_type == OMC_BF16, stream);
     if (rc == 0 && dWg) rc = launch_product_tiles(kBF16AcrossBoth, for_dw, pair >= 0, false, stream);
     return from_hip(rc);

@@ -12,6 +12,7 @@
 // stage's second step is multiplied behind the barrier of the next stage, under that one's first reads and the loads of the one that is asked for.  A workgroup's tiles follow each other without a gap: the loads
 // of the next tile are under way while the last stages of this one are multiplied.
 #pragma once
+#include "omc_column_sums.h"
 #include "omc_finish.h"
 #include "omc_pieces.h"
 
@@ -392,39 +393,56 @@ __global__ __attribute__((amdgpu_flat_work_group_size(64 * C::NW, 64 * C::NW))) 
 // Two products in one launch, a workgroup for every tile; the second one's begin at a multiple of 8, so that both keep their order over the dies.
 struct PairGrid {
     TileGrid first, second;
+    uint32_t groups;                           // of both; behind them come the columns' sums
+    ColumnSums sums;
 };
 template <typename C, typename D, int OCC>
 __global__ __attribute__((amdgpu_flat_work_group_size(64 * C::NW, 64 * C::NW))) __attribute__((amdgpu_waves_per_eu(OCC, OCC))) void tiles_pair_kernel(PairGrid pg) {
     static_assert(C::NW == D::NW, "one workgroup size");
     __shared__ __attribute__((aligned(1024))) uint8_t lds[C::kLds > D::kLds ? C::kLds : D::kLds];
     const uint32_t first = pg.first.tiles_m * pg.first.tiles_n, second = (first + 7) / 8 * 8;
-    if (blockIdx.x >= second) tiles_body<D>(pg.second, blockIdx.x - second, pg.second.tiles_m * pg.second.tiles_n, lds);
-    else if (blockIdx.x < first) tiles_body<C>(pg.first, blockIdx.x, first, lds);
+    if (blockIdx.x >= pg.groups) {
+        float(*part)[32] = reinterpret_cast<float(*)[32]>(lds);
+        pg.sums.count <= 64 ? column_sums<C::NW, 1, false>(pg.sums, blockIdx.x - pg.groups, part) : column_sums<C::NW, 8, false>(pg.sums, blockIdx.x - pg.groups, part);
+    } else if (blockIdx.x >= second) {
+        tiles_body<D>(pg.second, blockIdx.x - second, pg.second.tiles_m * pg.second.tiles_n, lds);
+    } else if (blockIdx.x < first) {
+        tiles_body<C>(pg.first, blockIdx.x, first, lds);
+    }
 }
 
 // The parts of a split contraction, added in order, and what becomes of the sums.
 template <bool I8, bool GATED, typename T>
-__global__ __launch_bounds__(256) void join_kernel(TiledArgs g, uint32_t splits) {
+__global__ __launch_bounds__(64) void join_kernel(TiledArgs g, uint32_t splits) {
     typedef typename SumOf<I8>::type Sum;
     typedef typename SumOf<I8>::scalar Scalar;
-    const uint32_t n = 4 * (blockIdx.x * 64 + (threadIdx.x & 63u)), m = blockIdx.y * 4 + (threadIdx.x >> 6);
+    const uint32_t at = blockIdx.x * 64 + threadIdx.x, quads = (g.N + 3) / 4, m = at / quads, n = 4 * (at - m * quads);   // (M N < 2^28: tiles are few where they are cut)
     if (m >= g.M || n >= g.N) return;
     const uint32_t left = g.N - n;
     const uint64_t width = GATED ? 2ull * g.N : g.N;
     auto sum_from = [&](uint64_t column) {
+        constexpr uint32_t kTogether = 8;      // loads on their way: other dies wrote what they bring
         Sum t = {0, 0, 0, 0};
-        for (uint32_t s = 0; s < splits; ++s) {
-            const Scalar *from = static_cast<const Scalar *>(g.parts) + (static_cast<uint64_t>(s) * g.M + m) * width + column;
-            Sum w = {0, 0, 0, 0};
-            if (left >= 4) {
-                __builtin_memcpy(&w, from, 16);
-            } else {
+        for (uint32_t first = 0; first < splits; first += kTogether) {
+            Sum w[kTogether];
 #pragma unroll
-                for (uint32_t e = 0; e < 4; ++e)
-                    if (e < left) w[e] = from[e];
+            for (uint32_t s = 0; s < kTogether; ++s) {
+                const Scalar *from = static_cast<const Scalar *>(g.parts) + (static_cast<uint64_t>(min(first + s, splits - 1)) * g.M + m) * width + column;
+                w[s] = Sum{0, 0, 0, 0};
+                if (left >= 4) {
+                    __builtin_memcpy(&w[s], from, 16);
+                } else {
+#pragma unroll
+                    for (uint32_t e = 0; e < 4; ++e)
+                        if (e < left) w[s][e] = from[e];
+                }
             }
 #pragma unroll
-            for (int e = 0; e < 4; ++e) t[e] += w[e];
+            for (uint32_t s = 0; s < kTogether; ++s)
+                if (first + s < splits) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) t[e] += w[s][e];
+                }
         }
         return t;
     };
@@ -475,7 +493,7 @@ static int launch_tiles(const TiledArgs &pa, bool whole, hipStream_t st) {
     if (c.splits > 1) {
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return static_cast<int>(e);
-        join_kernel<I8, GATED, T><<<dim3((pa.N + 255) / 256, (pa.M + 3) / 4), dim3(256), 0, st>>>(pa, c.splits);
+        join_kernel<I8, GATED, T><<<dim3((pa.M * ((pa.N + 3) / 4) + 63) / 64), dim3(64), 0, st>>>(pa, c.splits);
     }
     return static_cast<int>(hipGetLastError());
 }
