@@ -5,8 +5,8 @@ namespace omc {
 
 // By an estimate of the time in us: `base` is a launch; `alone` a stage of workgroups that nothing else slows down, `resident` of them on a compute unit; `busy` what a stage costs per workgroup of a unit where all units have some
 // (of the last workgroups' unevenness over the units `uneven` counts); `store` the end of 256 tiles.  A row for every kind of product, the last one for both backward products in one launch, which takes no less than its longest
-// contraction.  Fitted to 2100 sizes of 33 .. 16384 x 64 .. 8192 x 64 .. 8192 in bf16, 60 % of them with whole cache lines: 4 - 16 % (standard deviation).  On these the chosen way takes 1.0 - 2.7 % longer than the best one (both
-// backward products together or apart: 2.6 %), at worst 60 - 85 %, which is 9 us against 15 where a short contraction is cut in vain.
+// contraction.  Fitted to 2100 sizes of 33 .. 16384 x 64 .. 8192 x 64 .. 8192 in bf16, 60 % of them with whole cache lines: 4 - 16 % (standard deviation).  On these the chosen way takes 0.5 - 1.4 % longer than the best one (both
+// backward products together or apart: 2.6 %), at worst 13 - 50 %, of a few us.
 // 8192 x 4096 x 1024, gated: 256 x 256 150 us, 256 x 128 152, 128 x 128 157, 64 x 64 238; in 8 bits, plain: 42, 46, 43, 60; 8192 x 1024 x 4096: 48, 34, 35, 38.
 // 128 x 128 has two stages and two workgroups on a unit; with four stages, eight waves and the unit for itself 8192 x 4096 x 1024, gated, took 168 us.
 // A cut costs a second launch and the parts' way through memory.
@@ -43,7 +43,7 @@ TileChoice choose_tile(ProductKind kind, uint32_t M, uint32_t N, uint32_t stages
             if (splits > 1 && (whole || tiles * splits > 256 * kResident[i] || 2 * splits > stages)) break;
             const double each = static_cast<double>((stages + splits - 1) / splits);
             double c = cost(kCosts[kind][i], kResident[i], tiles * splits, each, each);
-            if (splits > 1) c += 3.0 + 2e-6 * splits * M * N * (gated_kind(kind) ? 2 : 1);   // (8 bytes of a part at 4 TB/s)
+            if (splits > 1) c += 2.5 + 1.6e-6 * splits * M * N * (gated_kind(kind) ? 2 : 1);   // (8 bytes of a part at 5 TB/s)
             if (best.tile < 0 || c < best.cost) best = TileChoice{i, splits, c};
         }
     }
@@ -66,6 +66,8 @@ int product_pair_tile(uint32_t M, uint32_t N, uint32_t stages, uint32_t M2, uint
     return tile;
 }
 
+double product_tiles_cost(ProductKind kind, uint32_t M, uint32_t N, uint32_t stages) { return choose_tile(kind, M, N, stages, false).cost; }
+
 // Host only, not part of the interface: the tile's index, and 16 times the parts, that a product takes; the tile in which both backward products of a gated layer go together, or -1.
 extern "C" int omc_internal_product_tile(int kind, uint32_t M, uint32_t N, uint32_t stages) {
     const TileChoice c = choose_tile(static_cast<ProductKind>(kind), M, N, stages, false);
@@ -83,7 +85,7 @@ int launch_across_both(const TiledArgs &pa, bool whole, bool c_bf16, hipStream_t
 
 size_t product_workspace(ProductKind kind, uint32_t M, uint32_t N, uint32_t stages) {
     const TileChoice c = choose_tile(kind, M, N, stages, false);
-    return c.splits > 1 ? 4ull * c.splits * M * N * (gated_kind(kind) ? 2 : 1) : 0;
+    return c.splits > 1 ? 4ull * c.splits * M * parts_columns(N) * (gated_kind(kind) ? 2 : 1) : 0;
 }
 
 int launch_product_tiles(ProductKind kind, const TiledArgs &pa, bool whole, bool c_bf16, void *stream) {

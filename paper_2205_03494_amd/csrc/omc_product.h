@@ -27,6 +27,7 @@ struct TiledArgs {
     void *parts;                         // of a split contraction
 };
 size_t product_workspace(ProductKind kind, uint32_t M, uint32_t N, uint32_t stages);   // bytes of parts
+double product_tiles_cost(ProductKind kind, uint32_t M, uint32_t N, uint32_t stages);  // an estimate, us
 int launch_product_tiles(ProductKind kind, const TiledArgs &pa, bool whole, bool c_bf16, void *stream);   // whole: the contraction is not cut
 // Of a gated layer's backward products, M x N as kBF16AcrossB and M2 x N2 as kBF16AcrossBoth (its result in fp32): the tile in which both go together, uncut, in one launch; -1: each goes its own way.
 int product_pair_tile(uint32_t M, uint32_t N, uint32_t stages, uint32_t M2, uint32_t N2, uint32_t stages2);
@@ -45,7 +46,7 @@ struct FewArgs {
     uint32_t columns;                    // values of a row of A, where it becomes codes
     Finish f;
 };
-bool product_few(uint32_t M, uint32_t N, uint32_t K);
+bool product_few(ProductKind kind, uint32_t M, uint32_t N, uint32_t K, bool rounds);   // rounds: A would become codes on the way
 bool product_few_rounds(uint32_t M, uint32_t K);
 int launch_product_few(ElementType x, ElementType w, bool gated, const FewArgs &fa, bool c_bf16, void *stream);
 

@@ -52,7 +52,7 @@ struct I8Operands {
     int gate;
 };
 static uint64_t i8_parts(ProductKind kind, uint32_t M, uint32_t N, uint32_t K) {
-    return product_few(M, N, K) ? 0 : product_workspace(kind, M, N, static_cast<uint32_t>(i8_pitch(K) / 128));
+    return product_few(kind, M, N, K, false) ? 0 : product_workspace(kind, M, N, static_cast<uint32_t>(i8_pitch(K) / 128));
 }
 static Finish i8_finish(const float *scales, const I8Operands &o, void *C, uint64_t ldc, uint32_t M) {
     Finish f = finish(C, ldc, M);
@@ -67,7 +67,7 @@ static Finish i8_finish(const float *scales, const I8Operands &o, void *C, uint6
 static int i8_product(const void *codes, const float *scales, const I8Operands &o, bool gated, void *C, bool c_bf16, uint64_t ldc, uint32_t M, uint32_t N, uint32_t K, void *parts, void *stream) {
     const uint64_t pitch = i8_pitch(K);
     const Finish f = i8_finish(scales, o, C, ldc, M);
-    if (product_few(M, N, K)) return launch_product_few(kE8, kE8, gated, FewArgs{codes, pitch, o.w, o.w2, pitch, M, N, static_cast<uint32_t>(pitch), 0, f}, c_bf16, stream);
+    if (product_few(gated ? kI8Gated : kI8Plain, M, N, K, false)) return launch_product_few(kE8, kE8, gated, FewArgs{codes, pitch, o.w, o.w2, pitch, M, N, static_cast<uint32_t>(pitch), 0, f}, c_bf16, stream);
     const uint32_t stages = static_cast<uint32_t>(pitch / 128);
     return launch_product_tiles(gated ? kI8Gated : kI8Plain, TiledArgs{codes, o.w, o.w2, pitch, pitch, M, N, stages, stages, N, f, parts}, false, c_bf16, stream);
 }
@@ -79,7 +79,7 @@ struct I8Layout {
 };
 static I8Layout i8_layout(uint8_t *ws, bool gated, uint32_t M, uint32_t N, uint32_t K) {
     I8Layout l{};
-    if (product_few(M, N, K) && product_few_rounds(M, K)) return l;
+    if (product_few_rounds(M, K) && product_few(gated ? kI8Gated : kI8Plain, M, N, K, true)) return l;   // codes stay in LDS
     Parts p{ws};
     l.codes = p.take(M * i8_pitch(K));
     l.scales = reinterpret_cast<float *>(p.take(4ull * M));
@@ -121,7 +121,7 @@ struct GatedLayout {
 };
 static GatedLayout gated_layout(uint8_t *ws, uint32_t M, uint32_t N, uint32_t K) {
     GatedLayout l{};
-    if (product_few(M, N, K)) return l;
+    if (product_few(kBF16Gated, M, N, K, false)) return l;
     Parts p{ws};
     const uint64_t pitch = to_64(K);
     l.x = reinterpret_cast<uint16_t *>(p.take(2 * M * pitch));
@@ -223,7 +223,7 @@ omc_status omc_gated_linear(const void *X, omc_type x_type, uint64_t ldx, const 
     f.slope_g = static_cast<uint16_t *>(slope_g);
     f.slope_u = static_cast<uint16_t *>(slope_u);
     f.ld_slope = ld_slope;
-    if (product_few(M, N, K)) return from_hip(launch_product_few(element(x_type), element(w_type), true, FewArgs{X, ldx, Wg, Wu, ldw, M, N, K, 0, f}, h_type == OMC_BF16, stream));
+    if (product_few(kBF16Gated, M, N, K, false)) return from_hip(launch_product_few(element(x_type), element(w_type), true, FewArgs{X, ldx, Wg, Wu, ldw, M, N, K, 0, f}, h_type == OMC_BF16, stream));
     const uint32_t pitch = to_64(K);
     PackArgs packs[kMostPacks];
     uint32_t count = 0;

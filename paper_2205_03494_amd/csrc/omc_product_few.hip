@@ -17,12 +17,20 @@ struct TypeOf<4> {
     typedef F32 type;
 };
 
-// A lane's 16 bytes of an operand for one matrix instruction, as they lie in memory.
-template <ElementType E>
+// A lane's 16 bytes of an operand for one matrix instruction, as they lie in memory.  WHOLE: a row is whole pieces.
+template <ElementType E, bool WHOLE>
 struct Piece {
-    Eight<typename TypeOf<E == kE32 ? 4 : 2>::type> v;
-    __device__ __forceinline__ void load(const void *row, uint32_t k, uint32_t K) { v.load(static_cast<const typename TypeOf<E == kE32 ? 4 : 2>::type::type *>(row), k, K); }
-    __device__ __forceinline__ void clear() { v.clear(); }
+    typedef typename TypeOf<E == kE32 ? 4 : 2>::type Type;
+    Eight<Type> v;
+    __device__ __forceinline__ void load(const uint8_t *row, uint32_t k, uint32_t K) {
+        const typename Type::type *from = reinterpret_cast<const typename Type::type *>(row);
+        if constexpr (WHOLE) {
+            __builtin_memcpy(v.w, from + (k < K ? k : 0), sizeof(v.w));
+        } else {
+            v.clear();
+            if (k < K) v.load(from, k, K);
+        }
+    }
     __device__ __forceinline__ i32x4 operand() const {
         i32x4 w;
 #pragma unroll
@@ -31,10 +39,9 @@ struct Piece {
     }
 };
 template <>
-struct Piece<kE8> {
+struct Piece<kE8, true> {
     i32x4 w;
-    __device__ __forceinline__ void load(const void *row, uint32_t k, uint32_t) { w = *reinterpret_cast<const i32x4 *>(static_cast<const uint8_t *>(row) + k); }
-    __device__ __forceinline__ void clear() { w = i32x4{0, 0, 0, 0}; }
+    __device__ __forceinline__ void load(const uint8_t *row, uint32_t k, uint32_t) { w = *reinterpret_cast<const i32x4 *>(row + k); }
     __device__ __forceinline__ i32x4 operand() const { return w; }
 };
 __device__ __forceinline__ f32x4 multiply_few(i32x4 a, i32x4 b, f32x4 acc) {
@@ -52,12 +59,12 @@ struct FewSum<true> {
 
 // MT row tiles of A.  kPieces: of eight values, of a lane at most, where A becomes codes.
 constexpr uint32_t kPieces = 4, kRoundedValues = 16384;
-template <ElementType X, ElementType W, bool GATED, int PARTS, int MT, typename T>
+template <ElementType X, ElementType W, bool GATED, int PARTS, int MT, bool WHOLE, typename T>
 __global__ __launch_bounds__(512) void few_kernel(FewArgs fa) {
     constexpr bool I8 = W == kE8, ROUNDS = I8 && X != kE8;
     constexpr uint32_t kStep = I8 ? 64 : 32, kUnit = 2 * kStep, kPer = I8 ? 16 : 8, kBytes = W == kE8 ? 1 : W == kE16 ? 2 : 4, kXBytes = X == kE8 ? 1 : X == kE16 ? 2 : 4;
     static_assert(!GATED || PARTS == 2, "both matrices");
-    constexpr int U = MT == 2 && X == kE32 && W == kE32 ? 1 : 2;   // (two units would spill)
+    constexpr int U = MT == 2 && X == kE32 && W == kE32 ? 1 : 2;   // units that are asked for together (two of fp32 would spill)
     typedef typename FewSum<I8>::type Sum;
     extern __shared__ __attribute__((aligned(16))) uint8_t few_lds[];
     const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
@@ -70,36 +77,31 @@ __global__ __launch_bounds__(512) void few_kernel(FewArgs fa) {
 #pragma unroll
     for (uint32_t i = 0; i < MT; ++i) x_row[i] = static_cast<const uint8_t *>(fa.x) + min(16 * i + r, fa.M - 1) * (fa.ldx * kXBytes);
     struct Group {
-        Piece<W> w[U][2][PARTS];
-        Piece<I8 ? kE8 : X> x[U][2][ROUNDS ? 1 : MT];
-    } now, next;
+        Piece<W, WHOLE> w[U][2][PARTS];
+        Piece<I8 ? kE8 : X, WHOLE> x[U][2][ROUNDS ? 1 : MT];
+    } even, odd;
     auto load_group = [&](Group &g, uint32_t unit) {
 #pragma unroll
-        for (uint32_t u = 0; u < U; ++u)
+        for (uint32_t u = 0; u < U; ++u) {
+            if (unit + u >= end) break;
 #pragma unroll
             for (uint32_t s = 0; s < 2; ++s) {
                 const uint32_t k = (unit + u) * kUnit + s * kStep + q * kPer;
-                const bool there = unit + u < end && k < fa.K;
 #pragma unroll
-                for (int i = 0; i < PARTS; ++i) {
-                    g.w[u][s][i].clear();
-                    if (there) g.w[u][s][i].load(w_row[i], k, fa.K);
-                }
+                for (int i = 0; i < PARTS; ++i) g.w[u][s][i].load(w_row[i], k, fa.K);
                 if constexpr (!ROUNDS) {
 #pragma unroll
-                    for (int i = 0; i < MT; ++i) {
-                        g.x[u][s][i].clear();
-                        if (there) g.x[u][s][i].load(x_row[i], k, fa.K);
-                    }
+                    for (int i = 0; i < MT; ++i) g.x[u][s][i].load(x_row[i], k, fa.K);
                 }
             }
+        }
     };
     Sum acc[PARTS][MT];
 #pragma unroll
     for (int i = 0; i < PARTS; ++i)
 #pragma unroll
         for (int j = 0; j < MT; ++j) acc[i][j] = Sum{0, 0, 0, 0};
-    load_group(now, begin);
+    load_group(even, begin);
 
     // ROUNDS: A's codes, rows apart by 16 bytes more than they are long, and scales in LDS, while the weights are on their way.  fa.K is whole 128s.
     const uint32_t pitch = fa.K + 16;
@@ -149,22 +151,37 @@ __global__ __launch_bounds__(512) void few_kernel(FewArgs fa) {
         scale_of_row = to.scale;
         __syncthreads();
     }
-    for (uint32_t unit = begin; unit < end; unit += U) {
-        load_group(next, unit + U);
+    auto multiply_group = [&](const Group &g, uint32_t unit) {
 #pragma unroll
-        for (uint32_t u = 0; u < U; ++u)
+        for (uint32_t u = 0; u < U; ++u) {
+            if (unit + u >= end) break;
+            const bool past = WHOLE && !I8 && (unit + u + 1) * kUnit > fa.K;   // a unit with lanes past the rows' end
 #pragma unroll
-            for (uint32_t s = 0; s < 2; ++s)
+            for (uint32_t s = 0; s < 2; ++s) {
+                const uint32_t k = (unit + u) * kUnit + s * kStep + q * kPer;
+                const i32x4 zero = {0, 0, 0, 0};
+                i32x4 x[MT];
 #pragma unroll
-                for (int i = 0; i < PARTS; ++i)
+                for (int j = 0; j < MT; ++j) {
+                    if constexpr (ROUNDS) x[j] = *reinterpret_cast<const i32x4 *>(row_codes + min(r, fa.M - 1) * pitch + k);
+                    else x[j] = g.x[u][s][j].operand();
+                    if (past && k >= fa.K) x[j] = zero;
+                }
 #pragma unroll
-                    for (int j = 0; j < MT; ++j) {
-                        i32x4 x;
-                        if constexpr (ROUNDS) x = *reinterpret_cast<const i32x4 *>(row_codes + min(r, fa.M - 1) * pitch + min((unit + u) * kUnit + s * kStep + q * kPer, fa.K - 16));   // (past the end: the weights are 0)
-                        else x = now.x[u][s][j].operand();
-                        acc[i][j] = multiply_few(now.w[u][s][i].operand(), x, acc[i][j]);
-                    }
-        now = next;
+                for (int i = 0; i < PARTS; ++i) {
+                    i32x4 w = g.w[u][s][i].operand();
+                    if (past && k >= fa.K) w = zero;
+#pragma unroll
+                    for (int j = 0; j < MT; ++j) acc[i][j] = multiply_few(w, x[j], acc[i][j]);
+                }
+            }
+        }
+    };
+    for (uint32_t unit = begin; unit < end; unit += 2 * U) {
+        load_group(odd, unit + U);
+        multiply_group(even, unit);
+        load_group(even, unit + 2 * U);
+        multiply_group(odd, unit + U);
     }
 
     if constexpr (ROUNDS) __syncthreads();     // nobody reads A any more
@@ -192,12 +209,21 @@ __global__ __launch_bounds__(512) void few_kernel(FewArgs fa) {
     }
 }
 
-bool product_few(uint32_t M, uint32_t N, uint32_t K) {
-    (void)N;
-    (void)K;
-    return M <= 32;
+// Up to 32 rows, where by estimates (us) that takes less than tiles, which cut a long contraction over the chip: a workgroup's eight waves take `rounds` units one after the other, at the rate at which a compute unit's loads bring
+// halves of 16 rows' cache lines; all workgroups together are bound by memory.  Fitted to 490 sizes of 1 .. 32 x 16 .. 16384 x 64 .. 32768 of each kind, 10 - 12 % (standard deviation); the chosen way takes 0.5 - 1.8 % longer
+// than the better one on average.  1 x 4096 x 1024 in 8 bits 5.5 us with its rounding, in tiles 9.3; 1 x 512 x 32768 36 and 26; gated in bf16 1 x 4096 x 1024 6.4 and 8.6, 16 x 8192 x 8192 50 and 45.
+bool product_few(ProductKind kind, uint32_t M, uint32_t N, uint32_t K, bool rounds) {
+    if (M > 32) return false;
+    const bool i8 = kind != kBF16Gated, gated = kind != kI8Plain;
+    const uint32_t unit = i8 ? 128 : 64, stages = (K + unit - 1) / unit, waves = stages < 8 ? stages : 8, parts = gated ? 2 : 1;
+    const double per_unit = static_cast<double>((N + 15) / 16) / 256.0, uneven = 1.0 + (per_unit > 1.0 ? 0.1 * (per_unit - 1.0) : 0.0);
+    const double turns = static_cast<double>((stages + waves - 1) / waves) * (0.43 * parts + (M <= 16 ? 0.13 : 0.26) + 0.3 / 16 * M) * uneven;
+    const double memory = static_cast<double>(N) * K * parts * (i8 ? 1 : 2) / 4.4e6;
+    const double few = 3.2 + (turns > memory ? turns : memory) - (rounds ? 2.0 : 0.0);   // a launch less
+    return few <= product_tiles_cost(kind, M, N, stages);
 }
-// VVV
+// A becomes codes in every workgroup where that is worth less than a launch, of which the host's part counts too.  With it, and with one before, from a graph: 1 x 4096 x 1024 5.5 us and 7.5, 8 x 4096 x 1024 6.8 and 8.2,
+// 16 x 4096 x 1024 8.3 and 8.5, 16 x 512 x 512 7.6 and 6.8; gated 16 x 4096 x 1024, call after call from Python, 9.6 and 13.
 bool product_few_rounds(uint32_t M, uint32_t K) { return M <= 16 && M * i8_pitch(K) <= kRoundedValues; }
 
 // With more than 16 rows of A a plain product's workgroup takes 32 columns where that leaves one for every compute unit, so that A is read half as often: 29 x 8192 x 8192 in 8 bits 29.8 -> 26.8 us with the rounding, 29 x 16384 x 4096
@@ -207,7 +233,11 @@ template <ElementType X, ElementType W, bool GATED, int PARTS, int MT, typename 
 static int launch_parts(const FewArgs &fa, hipStream_t st) {
     const uint32_t unit = W == kE8 ? 128 : 64, units = (fa.K + unit - 1) / unit, waves = units < 8 ? units : 8, joined = waves * MT * PARTS * 1024, columns = GATED ? 16 : 16 * PARTS;
     const uint32_t rounded = W == kE8 && X != kE8 ? 64 + fa.M * (fa.K + 16) : 0;
-    few_kernel<X, W, GATED, PARTS, MT, T><<<dim3((fa.N + columns - 1) / columns), dim3(64 * waves), rounded > joined ? rounded : joined, st>>>(fa);
+    const dim3 grid((fa.N + columns - 1) / columns), block(64 * waves);
+    const uint32_t lds = rounded > joined ? rounded : joined;
+    if constexpr (W == kE8) few_kernel<X, W, GATED, PARTS, MT, true, T><<<grid, block, lds, st>>>(fa);
+    else if (fa.K % 8 == 0) few_kernel<X, W, GATED, PARTS, MT, true, T><<<grid, block, lds, st>>>(fa);
+    else few_kernel<X, W, GATED, PARTS, MT, false, T><<<grid, block, lds, st>>>(fa);
     return static_cast<int>(hipGetLastError());
 }
 template <ElementType X, ElementType W, bool GATED, int MT, typename T>

@@ -38,6 +38,9 @@ struct TileGrid {
     uint32_t tiles_m, tiles_n, splits, stages_per_split;
 };
 
+// Parts of a cut contraction lie in rows of whole fours of columns, so that a lane's four are there for all lanes.
+constexpr uint64_t parts_columns(uint32_t N) { return (static_cast<uint64_t>(N) + 3) / 4 * 4; }
+
 // Two tiles side by side in bf16, so that a lane has eight neighbours: of tile 0 (even) or 1 (odd lane / 16), columns 8 (lane / 32) ..
 __device__ __forceinline__ u32x4 side_by_side_bf16(const float (&x)[4], const float (&y)[4]) {
     const auto lo = __builtin_amdgcn_permlane16_swap(to_bf16_pair(x[0], x[1]), to_bf16_pair(y[0], y[1]), false, false);
@@ -271,7 +274,7 @@ __device__ __forceinline__ void tiles_body(const TileGrid &tg, const uint32_t bl
         // ---- results: tile (i, j)'s lane holds row r, columns 4 q .. of it
         const uint32_t m_wave = p.m0 + 16 * TM * wm + r, n_wave = p.n0 + 16 * TH * wn;
         if constexpr (SPLIT) {
-            const uint64_t width = GATED ? 2ull * g.N : g.N;
+            const uint64_t half = parts_columns(g.N), width = GATED ? 2 * half : half;
             typedef typename SumOf<I8>::scalar Scalar;
 #pragma unroll
             for (uint32_t i = 0; i < TM; ++i) {
@@ -279,15 +282,7 @@ __device__ __forceinline__ void tiles_body(const TileGrid &tg, const uint32_t bl
 #pragma unroll
                 for (uint32_t j = 0; j < TN; ++j) {
                     const uint32_t n = n_wave + 16 * (j % TH) + 4 * q;
-                    if (m >= g.M || n >= g.N) continue;
-                    Scalar *out = static_cast<Scalar *>(g.parts) + (static_cast<uint64_t>(p.part) * g.M + m) * width + (j / TH) * static_cast<uint64_t>(g.N) + n;
-                    if (n + 4 <= g.N) {
-                        __builtin_memcpy(out, &acc[i][j], 16);
-                    } else {
-#pragma unroll
-                        for (uint32_t e = 0; e < 4; ++e)
-                            if (n + e < g.N) out[e] = acc[i][j][e];
-                    }
+                    if (m < g.M && n < g.N) *reinterpret_cast<Sum *>(static_cast<Scalar *>(g.parts) + (static_cast<uint64_t>(p.part) * g.M + m) * width + (j / TH) * half + n) = acc[i][j];
                 }
             }
         } else {
@@ -419,24 +414,15 @@ __global__ __launch_bounds__(64) void join_kernel(TiledArgs g, uint32_t splits) 
     const uint32_t at = blockIdx.x * 64 + threadIdx.x, quads = (g.N + 3) / 4, m = at / quads, n = 4 * (at - m * quads);   // (M N < 2^28: tiles are few where they are cut)
     if (m >= g.M || n >= g.N) return;
     const uint32_t left = g.N - n;
-    const uint64_t width = GATED ? 2ull * g.N : g.N;
+    const uint64_t half = parts_columns(g.N), width = GATED ? 2 * half : half;
     auto sum_from = [&](uint64_t column) {
         constexpr uint32_t kTogether = 8;      // loads on their way: other dies wrote what they bring
         Sum t = {0, 0, 0, 0};
         for (uint32_t first = 0; first < splits; first += kTogether) {
             Sum w[kTogether];
 #pragma unroll
-            for (uint32_t s = 0; s < kTogether; ++s) {
-                const Scalar *from = static_cast<const Scalar *>(g.parts) + (static_cast<uint64_t>(min(first + s, splits - 1)) * g.M + m) * width + column;
-                w[s] = Sum{0, 0, 0, 0};
-                if (left >= 4) {
-                    __builtin_memcpy(&w[s], from, 16);
-                } else {
-#pragma unroll
-                    for (uint32_t e = 0; e < 4; ++e)
-                        if (e < left) w[s][e] = from[e];
-                }
-            }
+            for (uint32_t s = 0; s < kTogether; ++s)
+                w[s] = *reinterpret_cast<const Sum *>(static_cast<const Scalar *>(g.parts) + (static_cast<uint64_t>(min(first + s, splits - 1)) * g.M + m) * width + column);
 #pragma unroll
             for (uint32_t s = 0; s < kTogether; ++s)
                 if (first + s < splits) {
@@ -450,7 +436,7 @@ __global__ __launch_bounds__(64) void join_kernel(TiledArgs g, uint32_t splits) 
     const Columns columns = columns_from<I8, GATED>(g.f, n, g.N);
     typename T::type *row = row_of<T>(g.f, m);
     if constexpr (GATED) {
-        store_gated<T>(g.f, sum_from(n), sum_from(static_cast<uint64_t>(g.N) + n), row_scale, columns, row + n, m, n, left);
+        store_gated<T>(g.f, sum_from(n), sum_from(half + n), row_scale, columns, row + n, m, n, left);
     } else if (row) {
         store_run<T, 4>(row + n, finish_plain(sum_from(n), row_scale, columns).v, left);
     }
