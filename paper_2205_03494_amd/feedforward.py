@@ -6,6 +6,9 @@ iteration decompresses the set, rounds the matrices to MX4 in both directions, r
 a fixed batch and then answers single frames:
 
     python -m paper_2205_03494_amd.feedforward --width 512 --inner 2048 --frames 1024 --steps 20
+
+With --gate it is a gated module, x + 1/2 W2 (act(Wg norm(x)) * Wu norm(x)): the gated layer trains on bf16 operands, W2 on 4 bits, and frames are
+answered in 8-bit integers.
 """
 from __future__ import annotations
 
@@ -50,9 +53,14 @@ class FeedForward:
     Work goes to the current stream.  A pass' workspace is its own (of the caching allocator, which keeps streams apart), so that frames may be answered on several
     streams at once; step and refresh rewrite the variables that every pass reads, and backward the one gradient buffer, and a caller with several streams orders these."""
 
+    IN_MX4 = ("w1", "w2")
+
+    def _shapes(self) -> dict:
+        return {"gamma": (self.width,), "beta": (self.width,), "w1": (self.width, self.inner), "b1": (self.inner,), "w2": (self.inner, self.width), "b2": (self.width,)}
+
     def __init__(self, width: int, inner: int, fmt=None, seed: int = 0):
         self.width, self.inner = width, inner
-        self.shapes = {"gamma": (width,), "beta": (width,), "w1": (width, inner), "b1": (inner,), "w2": (inner, width), "b2": (width,)}
+        self.shapes = self._shapes()
         fmt = fmt or omc.fmt(3, 7)
         table, self.at, data, aux = [], {}, 0, 0
         for name, shape in self.shapes.items():
@@ -70,12 +78,13 @@ class FeedForward:
         self.variables = 0
         self.step_ws = torch.empty(self.plan.workspace_bytes, dtype=torch.uint8, device="cuda")
         g = torch.Generator(device="cuda").manual_seed(seed)
-        for name, fan_in in (("w1", width), ("w2", inner)):
-            self.value(name).normal_(0.0, 1.0 / math.sqrt(fan_in), generator=g)
+        for name, shape in self.shapes.items():
+            if len(shape) == 2:
+                self.value(name).normal_(0.0, 1.0 / math.sqrt(inner if name == "w2" else width), generator=g)
         self.value("gamma").fill_(1.0)
         omc.omc_compress_set(self.values, self.plan, self.arena, self.sb, self.step_ws)
         self.mx4 = {}
-        for name in ("w1", "w2"):
+        for name in self.IN_MX4:
             r, c = self.shapes[name]
             self.mx4[name] = [torch.empty(size(*s), dtype=torch.uint8, device="cuda") for s in ((r, c), (c, r))
                               for size in (omc.omc_mx4_code_bytes, omc.omc_mx4_scale_bytes)]
@@ -123,13 +132,16 @@ class FeedForward:
         kept = self.kept if kept is None else kept
         if kept is None:
             raise RuntimeError("no forward pass with keep=True to go back through")
-        x, x_version, variables, mean, rstd, y, h, a = kept
-        if variables != self.variables:
+        if kept.variables != self.variables:
             raise RuntimeError("the forward pass was computed with other variables than the module now has")
-        if _version(x) != x_version:
+        if _version(kept.x) != kept.x_version:
             raise RuntimeError("the forward pass' input was changed in place since")
-        if dout.shape != x.shape:
-            raise ValueError(f"the gradient of {tuple(x.shape)} outputs is expected, not {tuple(dout.shape)}")
+        if dout.shape != kept.x.shape:
+            raise ValueError(f"the gradient of {tuple(kept.x.shape)} outputs is expected, not {tuple(dout.shape)}")
+        return self._backward(dout, kept)
+
+    def _backward(self, dout: torch.Tensor, kept: Kept) -> torch.Tensor:
+        x, _, _, mean, rstd, y, h, a = kept
         ws = self._workspace(x.shape[0], True)
         da, dy, dx = torch.empty_like(h), torch.empty_like(y), torch.empty_like(x)
         omc.omc_mx4_linear_backward((0.5 * dout).to(a.dtype), a, *self.mx4["w2"][:2], da, self.grad("w2"), self.grad("b2"), ws)
@@ -149,9 +161,108 @@ class FeedForward:
         self.refresh()
 
 
+@functools.lru_cache(maxsize=1024)
+def _gated_workspace_bytes(rows: int, width: int, inner: int, what: str) -> int:
+    if what == "answer":
+        return max(omc.omc_i8_gated_linear_workspace_bytes(rows, inner, width), omc.omc_i8_linear_workspace_bytes(rows, width, inner))
+    if what == "forward":
+        return max(omc.omc_gated_linear_workspace_bytes(rows, inner, width), omc.omc_mx4_linear_workspace_bytes(rows, width, inner))
+    return max(omc.omc_gated_linear_backward_workspace_bytes(rows, inner, width), omc.omc_mx4_linear_backward_workspace_bytes(rows, width, inner),
+               omc.omc_layer_norm_backward_workspace_bytes(rows, width))
+
+
+class KeptGated(NamedTuple):
+    """What a gated module's forward pass leaves for its backward pass."""
+    x: torch.Tensor
+    x_version: Optional[int]
+    variables: int
+    mean: torch.Tensor
+    rstd: torch.Tensor
+    y: torch.Tensor
+    slope_g: torch.Tensor
+    slope_u: torch.Tensor
+    h: torch.Tensor
+
+
+class GatedFeedForward(FeedForward):
+    """x + 1/2 W2 (act(Wg norm(x)) * Wu norm(x)); `gate` is one of omc.OMC_GATE_*.  Wg and Wu are inner x width, a row for every channel.
+
+    forward and backward are a training step's, on bf16 and 4-bit operands.  answer() serves frames in 8-bit integers, on the images that prepare_answers() made of the
+    variables as they are; after a step it has to be called again.  Streams as for FeedForward: refresh, step and prepare_answers rewrite what passes and answers read."""
+
+    IN_MX4 = ("w2",)
+
+    def _shapes(self) -> dict:
+        w, i = self.width, self.inner
+        return {"gamma": (w,), "beta": (w,), "wg": (i, w), "bg": (i,), "wu": (i, w), "bu": (i,), "w2": (i, w), "b2": (w,)}
+
+    def __init__(self, width: int, inner: int, gate: int = omc.OMC_GATE_SWISH, fmt=None, seed: int = 0):
+        if gate not in (omc.OMC_GATE_SIGMOID, omc.OMC_GATE_SWISH, omc.OMC_GATE_GELU):
+            raise ValueError(f"not a gate: {gate}")
+        self.gate = gate
+        self.half = {name: torch.empty(inner, width, device="cuda", dtype=torch.bfloat16) for name in ("wg", "wu")}
+        self.i8, self.answers = {}, 0
+        super().__init__(width, inner, fmt, seed)
+
+    def refresh(self) -> None:
+        super().refresh()
+        for name, half in self.half.items():
+            half.copy_(self.value(name))
+
+    def prepare_answers(self) -> None:
+        """The variables in 8 bits, a scale for every channel."""
+        for name in ("wg", "wu", "w2"):
+            rows, cols = (self.width, self.inner) if name == "w2" else (self.inner, self.width)
+            if name not in self.i8:
+                self.i8[name] = (torch.empty(omc.omc_i8_code_bytes(rows, cols), dtype=torch.uint8, device="cuda"), torch.empty(rows, device="cuda"))
+            omc.omc_i8_quantize(self.value(name), *self.i8[name], by_columns=name == "w2")
+        self.answers = self.variables
+
+    def _space(self, rows: int, what: str) -> torch.Tensor:
+        return torch.empty(_gated_workspace_bytes(rows, self.width, self.inner, what), dtype=torch.uint8, device="cuda")
+
+    def answer(self, x: torch.Tensor) -> torch.Tensor:
+        """x [frames, width] in fp32 -> the module's output in fp32, from one frame on, in 8 bits."""
+        if self.answers != self.variables:
+            raise RuntimeError("the variables have changed since prepare_answers, or it was not called")
+        rows = x.shape[0]
+        y, h = torch.empty_like(x), torch.empty(rows, self.inner, device="cuda")
+        z, ws = torch.empty_like(x), self._space(rows, "answer")
+        omc.omc_layer_norm(x, self.value("gamma"), self.value("beta"), EPS, y)
+        omc.omc_i8_gated_linear(y, *self.i8["wg"], *self.i8["wu"], self.value("bg"), self.value("bu"), self.gate, h, ws)
+        omc.omc_i8_linear(h, *self.i8["w2"], self.value("b2"), z, ws)
+        return x + 0.5 * z
+
+    def forward(self, x: torch.Tensor, keep: bool = False) -> torch.Tensor:
+        rows, half = x.shape[0], torch.bfloat16
+        y, h = torch.empty(rows, self.width, device="cuda", dtype=half), torch.empty(rows, self.inner, device="cuda", dtype=half)
+        z, ws = torch.empty(rows, self.width, device="cuda"), self._space(rows, "forward")
+        mean, rstd = (torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")) if keep else (None, None)
+        slope_g, slope_u = (torch.empty_like(h), torch.empty_like(h)) if keep else (None, None)
+        omc.omc_layer_norm(x, self.value("gamma"), self.value("beta"), EPS, y, mean, rstd)
+        omc.omc_gated_linear(y, self.half["wg"], self.half["wu"], self.value("bg"), self.value("bu"), self.gate, h, slope_g, slope_u, ws)
+        omc.omc_mx4_linear(h, *self.mx4["w2"][2:], self.value("b2"), z, ws)
+        if keep:
+            self.kept = KeptGated(x, _version(x), self.variables, mean, rstd, y, slope_g, slope_u, h)
+        return x + 0.5 * z
+
+    def _backward(self, dout: torch.Tensor, kept: KeptGated) -> torch.Tensor:
+        x, _, _, mean, rstd, y, slope_g, slope_u, h = kept
+        ws = self._space(x.shape[0], "backward")
+        dh, dy, dx = torch.empty_like(h), torch.empty_like(y), torch.empty_like(x)
+        omc.omc_mx4_linear_backward((0.5 * dout).to(h.dtype), h, *self.mx4["w2"][:2], dh, self.grad("w2"), self.grad("b2"), ws)
+        omc.omc_gated_linear_backward(dh, slope_g, slope_u, y, self.half["wg"], self.half["wu"], dy, self.grad("wg"), self.grad("wu"), self.grad("bg"), self.grad("bu"), ws)
+        omc.omc_layer_norm_backward(dy, x, self.value("gamma"), mean, rstd, dx, self.grad("gamma"), self.grad("beta"), ws)
+        return dx + dout
+
+
+GATES = {"sigmoid": omc.OMC_GATE_SIGMOID, "swish": omc.OMC_GATE_SWISH, "gelu": omc.OMC_GATE_GELU}
+
+
 def main() -> None:
     import argparse
     p = argparse.ArgumentParser(description="Train a feed-forward module on 4-bit products, then answer single frames.")
+    p.add_argument("--gate", choices=sorted(GATES), help="a gated module: trained on bf16 and 4-bit products, answers in 8 bits")
     for name, default in (("width", 512), ("inner", 2048), ("frames", 1024), ("steps", 20)):
         p.add_argument("--" + name, type=int, default=default)
     p.add_argument("--lr", type=float, default=2e-3)
@@ -159,7 +270,7 @@ def main() -> None:
     g = torch.Generator(device="cuda").manual_seed(1)
     x = torch.randn(a.frames, a.width, device="cuda", generator=g)
     target = x + 0.3 * torch.tanh(x.roll(1, 1))
-    module = FeedForward(a.width, a.inner)
+    module = GatedFeedForward(a.width, a.inner, GATES[a.gate]) if a.gate else FeedForward(a.width, a.inner)
     for t in range(1, a.steps + 1):
         out = module.forward(x, keep=True)
         diff = out - target
@@ -167,8 +278,13 @@ def main() -> None:
         module.step(omc.opt(omc.OMC_ADAM, a.lr, t=t))
         print(f"step {t}: mean square error {diff.square().mean().item():.6f}", flush=True)
     few = min(4, a.frames)
-    single = torch.cat([module.forward(x[i:i + 1]) for i in range(few)])
-    print(f"{few} frames one by one, largest difference from the batch: {(single - module.forward(x)[:few]).abs().max().item():.3g}")
+    answer = module.forward
+    if a.gate:
+        module.prepare_answers()
+        answer = module.answer
+        print(f"answers in 8 bits, largest difference from the training pass: {(answer(x) - module.forward(x)).abs().max().item():.3g}")
+    single = torch.cat([answer(x[i:i + 1]) for i in range(few)])
+    print(f"{few} frames one by one, largest difference from the batch: {(single - answer(x)[:few]).abs().max().item():.3g}")
 
 
 if __name__ == "__main__":
