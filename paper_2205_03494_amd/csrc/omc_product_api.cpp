@@ -138,17 +138,18 @@ struct GatedBackwardLayout {
     uint16_t *dgu, *x, *wg, *wu;
     float *sums;
     void *parts;
-    uint64_t bytes;
+    uint64_t sum_bytes, bytes;                 // of the columns' sums alone (they come first, whatever K is), of all
 };
 static GatedBackwardLayout gated_backward_layout(uint8_t *ws, uint32_t M, uint32_t N, uint32_t K) {
     GatedBackwardLayout l{};
     Parts p{ws};
     const uint64_t m = to_64(M), n = to_64(N), k = to_64(K);
+    l.sums = reinterpret_cast<float *>(p.take(8ull * sum_rows(M, N) * N));
+    l.sum_bytes = p.used;
     l.dgu = reinterpret_cast<uint16_t *>(p.take(4 * m * n));
     l.x = reinterpret_cast<uint16_t *>(p.take(2 * m * k));
     l.wg = reinterpret_cast<uint16_t *>(p.take(2 * n * k));
     l.wu = reinterpret_cast<uint16_t *>(p.take(2 * n * k));
-    l.sums = reinterpret_cast<float *>(p.take(8ull * sum_rows(M, N) * N));
     const bool whole = backward_pair(M, N, K) >= 0;
     const uint64_t dx = whole ? 0 : product_workspace(kBF16AcrossB, M, K, to_64(N) / 64 * 2), dw = whole ? 0 : product_workspace(kBF16AcrossBoth, 2 * to_64(N), K, to_64(M) / 64);
     l.parts = p.take(dx > dw ? dx : dw);
@@ -257,7 +258,7 @@ omc_status omc_gated_linear_backward(const void *dH, omc_type dh_type, uint64_t 
         (dWg && !element_aligned(X, x_type)) || (dX && (!element_aligned(Wg, w_type) || !element_aligned(Wu, w_type) || !element_aligned(dX, dx_type))))
         return OMC_ERR_ALIGN;
     const GatedBackwardLayout l = gated_backward_layout(static_cast<uint8_t *>(ws), M, N, K);
-    if (const omc_status s = check_workspace(ws, ws_bytes, l.bytes)) return s;
+    if (const omc_status s = check_workspace(ws, ws_bytes, dX || dWg ? l.bytes : l.sum_bytes)) return s;
     const bool sums = dbg || dbu;
     const uint32_t rows = to_64(M), half = to_64(N), k = to_64(K);
     PackArgs packs[kMostPacks];
