@@ -510,7 +510,7 @@ omc_status omc_mx4_linear_backward(const void *dY, uint64_t lddy, const void *X,
 
 /* ---- products on 8-bit integers ------------------------------------------------------------------
  * I8: a row of values shares a scale.  With a the largest magnitude of the row,
- *     s = a / 127 in fp32,   code_i = the whole number nearest to x_i / s, ties to even (saturating at 127 where s is subnormal),   value_i = s * code_i.
+ *     s = a * (1 / 127), both rounded to fp32,   code_i = the whole number nearest to x_i / s, ties to even (saturating at 127 where s is subnormal),   value_i = s * code_i.
  * A row of zeros has s = 0 and codes 0; a row with a value that is not finite has s = NaN and codes 0, and its values are NaN.
  *
  * A matrix of `rows` rows of `cols` values is held in two buffers.

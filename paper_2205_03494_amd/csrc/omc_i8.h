@@ -1,6 +1,7 @@
 // Device side of I8: a row of values shares a scale and holds a whole number each.
 //
-//   a = max |x_i|,  s = a / 127 rounded to fp32,  code_i = the whole number nearest to x_i / s, ties to even.
+//   a = max |x_i|,  s = a * (1 / 127), both rounded to fp32,  code_i = the whole number nearest to x_i / s, ties to even.
+// (A product and not a quotient: a last place of s more or less is none of any value's, since codes go by the s that is kept.)
 // The quotient is never formed exactly: r = rint(x * (1 / s)) is off by at most one, and d = x - r s, which fp32 holds exactly (r = 0: x itself; r = 1: both are within a factor of two; otherwise x > s, and d is a
 // multiple of s' last place below s / 2 and a little), says whether the neighbour is nearer.  That is asked where x * (1 / s) comes within 2^-12 of halfway between two whole numbers (it is off by 2^-15 at most).  Scales below 2^-100 are handled times 2^100, which is exact.
 #pragma once
@@ -13,7 +14,7 @@ struct Rounding {
     bool nan;
     __device__ __forceinline__ void of(float top, bool is_nan) {
         nan = is_nan;
-        scale = is_nan ? __builtin_nanf("") : top / 127.0f;
+        scale = is_nan ? __builtin_nanf("") : top * (1.0f / 127.0f);
         up = scale < 0x1p-100f ? 0x1p100f : 1.0f;
         s = is_nan || scale == 0.0f ? 1.0f : scale * up;
         inverse = is_nan || scale == 0.0f ? 0.0f : 1.0f / s;         // 0: all codes are 0

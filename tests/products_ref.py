@@ -22,7 +22,8 @@ def i8(x, by_columns=False):
     x = (x.t() if by_columns else x).double()
     top = x.abs().amax(1)
     fine = torch.isfinite(top)
-    scales = (torch.where(fine, top, 0.0) / 127.0).float()
+    scales = torch.where(fine, top, 0.0).float()
+    scales = scales * (torch.ones_like(scales) / torch.full_like(scales, 127.0))
     t = torch.where(fine[:, None], x, 0.0) / torch.where(scales > 0, scales, 1.0).double()[:, None]
     t = torch.where(scales[:, None] > 0, t, 0.0)
     low = torch.floor(t)
