@@ -62,7 +62,8 @@ struct SlopeGrid {
     uint32_t across, groups;
     Packs packs;
 };
-template <typename T, int EACH>
+// (SHORT: rows of fewer than eight values.)
+template <typename T, int EACH, bool SHORT>
 __global__ __launch_bounds__(256) void slopes_kernel(SlopeGrid sg) {
     __shared__ float sums[4][2][512];
     if (blockIdx.x >= sg.groups) {
@@ -84,10 +85,17 @@ __global__ __launch_bounds__(256) void slopes_kernel(SlopeGrid sg) {
             slope[k][0].clear();
             slope[k][1].clear();
             if (row < sa.M && col < sa.N) {
-                dh[k].load(static_cast<const typename T::type *>(sa.dh) + row * sa.lddh, col, sa.N);
-                slope[k][0].load(sa.slope_g + row * sa.ld_slope, col, sa.N);
-                slope[k][1].load(sa.slope_u + row * sa.ld_slope, col, sa.N);
+                dh[k].template fetch<SHORT>(static_cast<const typename T::type *>(sa.dh) + row * sa.lddh, col, sa.N);
+                slope[k][0].template fetch<SHORT>(sa.slope_g + row * sa.ld_slope, col, sa.N);
+                slope[k][1].template fetch<SHORT>(sa.slope_u + row * sa.ld_slope, col, sa.N);
             }
+        }
+        const uint32_t missing = Eight<T>::missing(col, sa.N);   // of a row's last piece; nothing waits between the loads
+#pragma unroll
+        for (uint32_t k = 0; k < kTogether; ++k) {
+            dh[k].settle(missing);
+            slope[k][0].settle(missing);
+            slope[k][1].settle(missing);
         }
 #pragma unroll
         for (uint32_t k = 0; k < kTogether; ++k) {
@@ -127,8 +135,9 @@ uint32_t slope_rows(uint32_t M, uint32_t N) { return static_cast<uint64_t>((M + 
 
 template <typename T>
 static void launch_typed(const SlopeGrid &sg, uint32_t rows, uint32_t groups, hipStream_t st) {
-    if (rows == 64) slopes_kernel<T, 16><<<dim3(groups), dim3(256), 0, st>>>(sg);
-    else slopes_kernel<T, 4><<<dim3(groups), dim3(256), 0, st>>>(sg);
+    if (sg.s.N < 8) rows == 64 ? slopes_kernel<T, 16, true><<<dim3(groups), dim3(256), 0, st>>>(sg) : slopes_kernel<T, 4, true><<<dim3(groups), dim3(256), 0, st>>>(sg);
+    else if (rows == 64) slopes_kernel<T, 16, false><<<dim3(groups), dim3(256), 0, st>>>(sg);
+    else slopes_kernel<T, 4, false><<<dim3(groups), dim3(256), 0, st>>>(sg);
 }
 int launch_slopes(const SlopeArgs &sa, const PackArgs *packs, uint32_t count, void *stream) {
     hipStream_t st = static_cast<hipStream_t>(stream);

@@ -5,7 +5,7 @@
 namespace omc {
 
 // LANES lanes (64, or the workgroup's 256) take a row, R pieces of eight values each; PIECES in registers.  REREAD: the row is longer, and is read twice.
-template <typename T, int LANES, int R, bool REREAD>
+template <typename T, int LANES, int R, bool REREAD, bool SHORT = false>
 __global__ __launch_bounds__(256) void i8_rows_kernel(I8Args ia) {
     __shared__ uint32_t tops[4];
     const uint32_t row = LANES == 64 ? blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x, lane = LANES == 64 ? threadIdx.x & 63u : threadIdx.x;
@@ -13,14 +13,22 @@ __global__ __launch_bounds__(256) void i8_rows_kernel(I8Args ia) {
     const typename T::type *x = static_cast<const typename T::type *>(ia.x) + row * ia.ldx;
     const uint32_t pitch = static_cast<uint32_t>(i8_pitch(ia.cols)), run = 8 * LANES * R;
     Eight<T> v[R];
-    uint32_t top = 0;
-    for (uint32_t from = 0; from < (REREAD ? ia.cols : 1u); from += run) {
+    auto load_run = [&](uint32_t from) {       // nothing waits between the loads
 #pragma unroll
         for (uint32_t k = 0; k < R; ++k) {
             const uint32_t col = from + 8 * (lane + LANES * k);
             v[k].clear();
-            if (col < ia.cols) v[k].load(x, col, ia.cols);
+            if (col < ia.cols) v[k].template fetch<SHORT>(x, col, ia.cols);
         }
+#pragma unroll
+        for (uint32_t k = 0; k < R; ++k) {
+            const uint32_t col = from + 8 * (lane + LANES * k);
+            if (col < ia.cols) v[k].settle(Eight<T>::missing(col, ia.cols));
+        }
+    };
+    uint32_t top = 0;
+    for (uint32_t from = 0; from < (REREAD ? ia.cols : 1u); from += run) {
+        load_run(from);
 #pragma unroll
         for (uint32_t k = 0; k < R; ++k) top = max(top, v[k].top());
     }
@@ -36,14 +44,7 @@ __global__ __launch_bounds__(256) void i8_rows_kernel(I8Args ia) {
     if (lane == 0) ia.scales[row] = to.scale;
     uint8_t *codes = ia.codes + row * static_cast<uint64_t>(pitch);
     for (uint32_t from = 0; from < (REREAD ? pitch : 1u); from += run) {
-        if constexpr (REREAD) {
-#pragma unroll
-            for (uint32_t k = 0; k < R; ++k) {
-                const uint32_t col = from + 8 * (lane + LANES * k);
-                v[k].clear();
-                if (col < ia.cols) v[k].load(x, col, ia.cols);
-            }
-        }
+        if constexpr (REREAD) load_run(from);
 #pragma unroll
         for (uint32_t k = 0; k < R; ++k) {
             const uint32_t col = from + 8 * (lane + LANES * k);
@@ -146,7 +147,8 @@ __global__ __launch_bounds__(1024) void i8_columns_kernel(I8Args ia) {
 template <typename T>
 static int launch_rows(const I8Args &ia, hipStream_t st) {
     const dim3 by_wave((ia.rows + 3) / 4), by_group(ia.rows), block(256);
-    if (ia.cols <= 512) i8_rows_kernel<T, 64, 1, false><<<by_wave, block, 0, st>>>(ia);
+    if (ia.cols < 8) i8_rows_kernel<T, 64, 1, false, true><<<by_wave, block, 0, st>>>(ia);
+    else if (ia.cols <= 512) i8_rows_kernel<T, 64, 1, false><<<by_wave, block, 0, st>>>(ia);
     else if (ia.cols <= 1024) i8_rows_kernel<T, 64, 2, false><<<by_wave, block, 0, st>>>(ia);
     else if (ia.cols <= 2048) i8_rows_kernel<T, 256, 1, false><<<by_group, block, 0, st>>>(ia);
     else if (ia.cols <= 4096) i8_rows_kernel<T, 256, 2, false><<<by_group, block, 0, st>>>(ia);
