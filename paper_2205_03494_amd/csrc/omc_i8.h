@@ -11,13 +11,13 @@ namespace omc {
 
 struct Rounding {
     float scale, up, s, inverse;
-    bool nan;
-    __device__ __forceinline__ void of(float top, bool is_nan) {
-        nan = is_nan;
-        scale = is_nan ? __builtin_nanf("") : top * (1.0f / 127.0f);
+    __device__ __forceinline__ void of(float top, bool is_nan) { with(is_nan ? __builtin_nanf("") : top * (1.0f / 127.0f)); }
+    __device__ __forceinline__ void with(float its_scale) {
+        scale = its_scale;
         up = scale < 0x1p-100f ? 0x1p100f : 1.0f;
-        s = is_nan || scale == 0.0f ? 1.0f : scale * up;
-        inverse = is_nan || scale == 0.0f ? 0.0f : 1.0f / s;         // 0: all codes are 0
+        const bool some = scale > 0.0f;                              // (a NaN is not)
+        s = some ? scale * up : 1.0f;
+        inverse = some ? 1.0f / s : 0.0f;                            // 0: all codes are 0
     }
     __device__ __forceinline__ float code(float x) const {
         if (inverse == 0.0f) return 0.0f;
@@ -28,17 +28,21 @@ struct Rounding {
         if (twice > s || (twice == s && odd)) r += copysignf(1.0f, d);
         return fminf(fmaxf(r, -127.0f), 127.0f);                     // (a scale below 2^-126 is coarser than its largest value's 127th part)
     }
-    // Of eight values, where lanes seldom need code(): adding 1.5 * 2^23 rounds to a whole number, ties to even, and leaves it in the low bits.
-    __device__ __forceinline__ void eight(const float (&x)[8], float (&r)[8]) const {
+    // The same where x / s is not about halfway between two whole numbers, which `far` says (the largest distance so far): adding 1.5 * 2^23 rounds, ties to even.
+    __device__ __forceinline__ float near(float x, float &far) const {
         constexpr float kWhole = 12582912.0f;
+        const float f = x * inverse, r = (f + kWhole) - kWhole;
+        far = fmaxf(far, fabsf(f - r));
+        return r;
+    }
+    static constexpr float kFar = 0.499755859375f;                   // 1/2 - 2^-12
+    __device__ __forceinline__ bool special() const { return up != 1.0f || inverse == 0.0f; }
+    // Of eight values, where lanes seldom need code().
+    __device__ __forceinline__ void eight(const float (&x)[8], float (&r)[8]) const {
         float far = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float f = x[i] * inverse;
-            r[i] = (f + kWhole) - kWhole;
-            far = fmaxf(far, fabsf(f - r[i]));
-        }
-        if (far > 0.499755859375f || up != 1.0f || inverse == 0.0f) {
+        for (int i = 0; i < 8; ++i) r[i] = near(x[i], far);
+        if (far > kFar || special()) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) r[i] = code(x[i]);
         }

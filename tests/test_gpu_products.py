@@ -59,7 +59,7 @@ def special(rows, cols, seed, dtype):
     return x
 
 
-SHAPES = [(1, 1), (1, 7), (3, 128), (2, 129), (5, 1000), (67, 64), (129, 333), (513, 96), (9, 2048), (3, 5000), (2, 8200), (1030, 40)]
+SHAPES = [(1, 1), (1, 7), (3, 128), (2, 129), (5, 1000), (67, 64), (129, 333), (513, 96), (9, 2048), (3, 5000), (2, 8200), (1030, 40), (2100, 20), (5000, 3), (300, 2100)]
 
 
 @pytest.mark.parametrize("by_columns", [False, True])
