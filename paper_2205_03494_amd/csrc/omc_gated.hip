@@ -56,7 +56,7 @@ int product_pair_tile(uint32_t M, uint32_t N, uint32_t stages, uint32_t M2, uint
     double least = choose_tile(kBF16AcrossB, M, N, stages, false).cost + choose_tile(kBF16AcrossBoth, M2, N2, stages2, false).cost;
     for (int i = 0; i < 4; ++i) {
         const uint64_t a = tiles_of(kBF16AcrossB, i, M, N), b = tiles_of(kBF16AcrossBoth, i, M2, N2);
-        if (a + b > 0x7ffffff0u) continue;
+        if (a + b > 1u << 22) continue;        // (a workgroup for every tile, and a launch's work-items within 32 bits)
         const double c = cost(kCosts[kPair][i], kResident[i], a + b, static_cast<double>(a * stages + b * stages2) / static_cast<double>(a + b), stages > stages2 ? stages : stages2);
         if (c < least) {
             least = c;

@@ -19,30 +19,40 @@ __device__ __forceinline__ u32x4 eight_bf16(const Eight<T> &v) {
     }
     return w;
 }
-// A lane takes eight values.
+// A lane takes eight values; workgroups more than one, where a launch has too few.
 template <typename T>
-__device__ __forceinline__ void pack_pieces(const PackArgs &p, uint32_t group) {
-    const uint32_t pieces = p.pitch / 8, row0 = static_cast<uint32_t>(group * 256ull / pieces), rest = static_cast<uint32_t>(group * 256ull - static_cast<uint64_t>(row0) * pieces) + threadIdx.x;
-    const uint32_t down = rest / pieces, row = row0 + down, col = 8 * (rest - down * pieces);
-    if (row >= p.to_rows) return;
-    Eight<T> v;
-    v.clear();
-    if (row < p.rows && col < p.cols) v.load(static_cast<const typename T::type *>(p.x) + row * p.ldx, col, p.cols);
-    *reinterpret_cast<u32x4 *>(p.to + row * static_cast<uint64_t>(p.pitch) + col) = eight_bf16(v);
+__device__ __forceinline__ void pack_pieces(const PackArgs &p, uint32_t group, uint32_t groups) {
+    const uint32_t pieces = p.pitch / 8;
+    const uint64_t step = groups * 256ull;
+    uint64_t at = group * 256ull;
+    for (;;) {
+        const uint32_t row0 = static_cast<uint32_t>(at / pieces), rest = static_cast<uint32_t>(at - static_cast<uint64_t>(row0) * pieces) + threadIdx.x;
+        if (row0 >= p.to_rows) return;
+        const uint32_t down = rest / pieces, row = row0 + down, col = 8 * (rest - down * pieces);
+        if (row < p.to_rows) {
+            Eight<T> v;
+            v.clear();
+            if (row < p.rows && col < p.cols) v.load(static_cast<const typename T::type *>(p.x) + row * p.ldx, col, p.cols);
+            *reinterpret_cast<u32x4 *>(p.to + row * static_cast<uint64_t>(p.pitch) + col) = eight_bf16(v);
+        }
+        at += step;
+    }
 }
 __device__ __forceinline__ void pack(const Packs &packs, uint32_t group) {
     const uint32_t second = packs.groups[0], third = second + packs.groups[1], i = group < second ? 0u : group < third ? 1u : 2u;
     const PackArgs &p = packs.p[i];            // (by number: the arguments stay where they are)
     group -= i == 0 ? 0u : i == 1 ? second : third;
-    p.bf16 ? pack_pieces<BF16>(p, group) : pack_pieces<F32>(p, group);
+    p.bf16 ? pack_pieces<BF16>(p, group, packs.groups[i]) : pack_pieces<F32>(p, group, packs.groups[i]);
 }
+constexpr uint64_t kMostGroups = 1u << 21;     // of a copy; a launch's work-items within 32 bits
 static Packs packs_of(const PackArgs *packs, uint32_t count, uint32_t &groups) {
     Packs all{};
     groups = 0;
     for (uint32_t i = 0; i < count; ++i) {
         all.p[i] = packs[i];
         const uint64_t n = static_cast<uint64_t>(packs[i].to_rows) * (packs[i].pitch / 8);
-        all.groups[i] = static_cast<uint32_t>((n + 255) / 256);
+        const uint64_t wanted = (n + 255) / 256;
+        all.groups[i] = static_cast<uint32_t>(wanted < kMostGroups ? wanted : kMostGroups);
         groups += all.groups[i];
     }
     return all;

@@ -11,59 +11,61 @@ namespace omc {
 template <typename T, int LANES, int R, bool REREAD, bool SHORT = false>
 __global__ __launch_bounds__(256) void i8_rows_kernel(I8Args ia) {
     __shared__ uint32_t tops[4];
-    const uint32_t row = LANES == 64 ? blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x, lane = LANES == 64 ? threadIdx.x & 63u : threadIdx.x;
-    if (row >= ia.rows) return;                // (LANES == 256: the whole workgroup)
-    const typename T::type *x = static_cast<const typename T::type *>(ia.x) + row * ia.ldx;
-    const uint32_t pitch = static_cast<uint32_t>(i8_pitch(ia.cols)), run = 8 * LANES * R;
-    Eight<T> v[R];
-    auto load_run = [&](uint32_t from) {       // nothing waits between the loads
+    const uint32_t lane = LANES == 64 ? threadIdx.x & 63u : threadIdx.x, stride = LANES == 64 ? 4 * gridDim.x : gridDim.x;
+    for (uint32_t row = LANES == 64 ? blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x; row < ia.rows; row += stride) {   // (LANES == 256: the whole workgroup)
+        const typename T::type *x = static_cast<const typename T::type *>(ia.x) + row * ia.ldx;
+        const uint32_t pitch = static_cast<uint32_t>(i8_pitch(ia.cols)), run = 8 * LANES * R;
+        Eight<T> v[R];
+        auto load_run = [&](uint32_t from) {       // nothing waits between the loads
 #pragma unroll
-        for (uint32_t k = 0; k < R; ++k) {
-            const uint32_t col = from + 8 * (lane + LANES * k);
-            v[k].clear();
-            if (col < ia.cols) v[k].template fetch<SHORT>(x, col, ia.cols);
+            for (uint32_t k = 0; k < R; ++k) {
+                const uint32_t col = from + 8 * (lane + LANES * k);
+                v[k].clear();
+                if (col < ia.cols) v[k].template fetch<SHORT>(x, col, ia.cols);
+            }
+#pragma unroll
+            for (uint32_t k = 0; k < R; ++k) {
+                const uint32_t col = from + 8 * (lane + LANES * k);
+                if (col < ia.cols) v[k].settle(Eight<T>::missing(col, ia.cols));
+            }
+        };
+        uint32_t top = 0;
+        for (uint32_t from = 0; from < (REREAD ? ia.cols : 1u); from += run) {
+            load_run(from);
+#pragma unroll
+            for (uint32_t k = 0; k < R; ++k) top = max(top, v[k].top());
         }
 #pragma unroll
-        for (uint32_t k = 0; k < R; ++k) {
-            const uint32_t col = from + 8 * (lane + LANES * k);
-            if (col < ia.cols) v[k].settle(Eight<T>::missing(col, ia.cols));
+        for (int by = 1; by < 64; by *= 2) top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), by)));
+        if constexpr (LANES == 256) {
+            if ((threadIdx.x & 63u) == 0) tops[threadIdx.x >> 6] = top;
+            __syncthreads();
+            top = max(max(tops[0], tops[1]), max(tops[2], tops[3]));
         }
-    };
-    uint32_t top = 0;
-    for (uint32_t from = 0; from < (REREAD ? ia.cols : 1u); from += run) {
-        load_run(from);
+        Rounding to;
+        to.of(from_top<T>(top), top > T::kFinite);
+        if (lane == 0) ia.scales[row] = to.scale;
+        uint8_t *codes = ia.codes + row * static_cast<uint64_t>(pitch);
+        for (uint32_t from = 0; from < (REREAD ? pitch : 1u); from += run) {
+            if constexpr (REREAD) load_run(from);
 #pragma unroll
-        for (uint32_t k = 0; k < R; ++k) top = max(top, v[k].top());
-    }
+            for (uint32_t k = 0; k < R; ++k) {
+                const uint32_t col = from + 8 * (lane + LANES * k);
+                if (col >= pitch) continue;
+                float x8[8], r[8];
 #pragma unroll
-    for (int by = 1; by < 64; by *= 2) top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), by)));
-    if constexpr (LANES == 256) {
-        if ((threadIdx.x & 63u) == 0) tops[threadIdx.x >> 6] = top;
-        __syncthreads();
-        top = max(max(tops[0], tops[1]), max(tops[2], tops[3]));
-    }
-    Rounding to;
-    to.of(from_top<T>(top), top > T::kFinite);
-    if (lane == 0) ia.scales[row] = to.scale;
-    uint8_t *codes = ia.codes + row * static_cast<uint64_t>(pitch);
-    for (uint32_t from = 0; from < (REREAD ? pitch : 1u); from += run) {
-        if constexpr (REREAD) load_run(from);
+                for (int i = 0; i < 8; ++i) x8[i] = v[k].value(i);
+                to.eight(x8, r);
+                const uint64_t w = four_bytes(r) | static_cast<uint64_t>(four_bytes(r + 4)) << 32;
+                *reinterpret_cast<uint64_t *>(codes + col) = w;
+                if (ia.values && col < ia.cols) {
 #pragma unroll
-        for (uint32_t k = 0; k < R; ++k) {
-            const uint32_t col = from + 8 * (lane + LANES * k);
-            if (col >= pitch) continue;
-            float x8[8], r[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x8[i] = v[k].value(i);
-            to.eight(x8, r);
-            const uint64_t w = four_bytes(r) | static_cast<uint64_t>(four_bytes(r + 4)) << 32;
-            *reinterpret_cast<uint64_t *>(codes + col) = w;
-            if (ia.values && col < ia.cols) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) r[i] = to.value(r[i]);
-                store_run<T, 8>(static_cast<typename T::type *>(ia.values) + row * ia.ldv + col, r, ia.cols - col);
+                    for (int i = 0; i < 8; ++i) r[i] = to.value(r[i]);
+                    store_run<T, 8>(static_cast<typename T::type *>(ia.values) + row * ia.ldv + col, r, ia.cols - col);
+                }
             }
         }
+        if constexpr (LANES == 256) __syncthreads();   // tops again
     }
 }
 
@@ -162,7 +164,7 @@ constexpr uint32_t kMaximaRows = 128;
 template <typename T>
 __global__ __launch_bounds__(256) void i8_maxima_kernel(I8Args ia, uint32_t *parts) {
     __shared__ uint32_t tops[4][512];
-    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, col0 = blockIdx.x * 512, col = col0 + 8 * lane, row0 = blockIdx.y * kMaximaRows;
+    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, across = (ia.cols + 511) / 512, down = blockIdx.x / across, col0 = (blockIdx.x - down * across) * 512, col = col0 + 8 * lane, row0 = down * kMaximaRows;
     uint32_t top[8] = {};
     if (col < ia.cols) {
         const typename T::type *x = static_cast<const typename T::type *>(ia.x);
@@ -183,7 +185,7 @@ __global__ __launch_bounds__(256) void i8_maxima_kernel(I8Args ia, uint32_t *par
     for (int i = 0; i < 8; ++i) tops[wave][8 * lane + i] = top[i];
     __syncthreads();
     for (uint32_t c = threadIdx.x; c < 512; c += 256)
-        if (col0 + c < ia.cols) parts[static_cast<uint64_t>(blockIdx.y) * ia.cols + col0 + c] = max(max(tops[0][c], tops[1][c]), max(tops[2][c], tops[3][c]));
+        if (col0 + c < ia.cols) parts[static_cast<uint64_t>(down) * ia.cols + col0 + c] = max(max(tops[0][c], tops[1][c]), max(tops[2][c], tops[3][c]));
 }
 // the scales;
 __global__ __launch_bounds__(64) void i8_scales_kernel(const uint32_t *parts, uint32_t count, uint32_t cols, float *scales) {
@@ -207,55 +209,60 @@ __global__ __launch_bounds__(256) void i8_turn_kernel(I8Args ia) {
     constexpr uint32_t kPitch = 132;           // (eight columns apart, lanes write to different banks)
     __shared__ uint32_t turned[64 * kPitch / 4];
     uint8_t *bytes = reinterpret_cast<uint8_t *>(turned);
-    const uint32_t across = threadIdx.x & 7u, line = threadIdx.x >> 3, col0 = blockIdx.x * 64, col = col0 + 8 * across, row0 = blockIdx.y * 128;
-    if (col < ia.cols) {
-        const typename T::type *x = static_cast<const typename T::type *>(ia.x);
-        const uint32_t missing = Eight<T>::missing(col, ia.cols);
-        Eight<T> v[4];
+    const uint32_t across = threadIdx.x & 7u, line = threadIdx.x >> 3, tiles_across = (ia.cols + 63) / 64, tiles = tiles_across * ((ia.rows + 127) / 128);
+    for (uint32_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+        const uint32_t down = tile / tiles_across, col0 = (tile - down * tiles_across) * 64, col = col0 + 8 * across, row0 = down * 128;
+        if (col < ia.cols) {
+            const typename T::type *x = static_cast<const typename T::type *>(ia.x);
+            const uint32_t missing = Eight<T>::missing(col, ia.cols);
+            Eight<T> v[4];
 #pragma unroll
-        for (uint32_t k = 0; k < 4; ++k) v[k].template fetch<false>(x + min(row0 + 32 * k + line, ia.rows - 1) * ia.ldx, col, ia.cols);
-        Rounding to[8];
+            for (uint32_t k = 0; k < 4; ++k) v[k].template fetch<false>(x + min(row0 + 32 * k + line, ia.rows - 1) * ia.ldx, col, ia.cols);
+            Rounding to[8];
 #pragma unroll
-        for (uint32_t i = 0; i < 8; ++i) to[i].with(ia.scales[min(col + i, ia.cols - 1)]);
-        bool special = false;
+            for (uint32_t i = 0; i < 8; ++i) to[i].with(ia.scales[min(col + i, ia.cols - 1)]);
+            bool special = false;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) special |= to[i].special();
+            for (int i = 0; i < 8; ++i) special |= to[i].special();
 #pragma unroll
-        for (uint32_t k = 0; k < 4; ++k) {
-            const uint32_t row = row0 + 32 * k + line;
-            v[k].settle(missing);
-            float r[8], far = 0.0f;
+            for (uint32_t k = 0; k < 4; ++k) {
+                const uint32_t row = row0 + 32 * k + line;
+                v[k].settle(missing);
+                float r[8], far = 0.0f;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) r[i] = to[i].near(v[k].value(i), far);
-            if (far > Rounding::kFar || special) {
+                for (int i = 0; i < 8; ++i) r[i] = to[i].near(v[k].value(i), far);
+                if (far > Rounding::kFar || special) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) r[i] = to[i].code(v[k].value(i));
-            }
+                    for (int i = 0; i < 8; ++i) r[i] = to[i].code(v[k].value(i));
+                }
 #pragma unroll
-            for (int i = 0; i < 8; ++i) bytes[(8 * across + i) * kPitch + 32 * k + line] = row < ia.rows ? static_cast<uint8_t>(static_cast<int>(r[i])) : 0;
-            if (ia.values && row < ia.rows) {
+                for (int i = 0; i < 8; ++i) bytes[(8 * across + i) * kPitch + 32 * k + line] = row < ia.rows ? static_cast<uint8_t>(static_cast<int>(r[i])) : 0;
+                if (ia.values && row < ia.rows) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) r[i] = to[i].value(r[i]);
-                store_run<T, 8>(static_cast<typename T::type *>(ia.values) + row * ia.ldv + col, r, ia.cols - col);
+                    for (int i = 0; i < 8; ++i) r[i] = to[i].value(r[i]);
+                    store_run<T, 8>(static_cast<typename T::type *>(ia.values) + row * ia.ldv + col, r, ia.cols - col);
+                }
             }
         }
-    }
-    __syncthreads();
-    const uint64_t pitch = i8_pitch(ia.rows);
+        __syncthreads();
+        const uint64_t pitch = i8_pitch(ia.rows);
 #pragma unroll
-    for (uint32_t t = threadIdx.x; t < 512; t += 256) {
-        const uint32_t c = t / 8, at = 16 * (t % 8);
-        if (col0 + c >= ia.cols) continue;
-        u32x4 w;
+        for (uint32_t t = threadIdx.x; t < 512; t += 256) {
+            const uint32_t c = t / 8, at = 16 * (t % 8);
+            if (col0 + c >= ia.cols) continue;
+            u32x4 w;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = turned[(c * kPitch + at) / 4 + i];
-        *reinterpret_cast<u32x4 *>(ia.codes + (col0 + c) * pitch + row0 + at) = w;
+            for (int i = 0; i < 4; ++i) w[i] = turned[(c * kPitch + at) / 4 + i];
+            *reinterpret_cast<u32x4 *>(ia.codes + (col0 + c) * pitch + row0 + at) = w;
+        }
+        __syncthreads();
     }
 }
 
+constexpr uint32_t kMostGroups = 1u << 22;    // a launch's work-items within 32 bits; what is more is taken in turn
 template <typename T>
 static int launch_rows(const I8Args &ia, hipStream_t st) {
-    const dim3 by_wave((ia.rows + 3) / 4), by_group(ia.rows), block(256);
+    const dim3 by_wave((ia.rows + 3) / 4), by_group(ia.rows < kMostGroups ? ia.rows : kMostGroups), block(256);
     if (ia.cols < 8) i8_rows_kernel<T, 64, 1, false, true><<<by_wave, block, 0, st>>>(ia);
     else if (ia.cols <= 512) i8_rows_kernel<T, 64, 1, false><<<by_wave, block, 0, st>>>(ia);
     else if (ia.cols <= 1024) i8_rows_kernel<T, 64, 2, false><<<by_wave, block, 0, st>>>(ia);
@@ -280,9 +287,11 @@ static int launch_columns(const I8Args &ia, hipStream_t st) {
     }
     const uint32_t count = (ia.rows + kMaximaRows - 1) / kMaximaRows;
     uint32_t *parts = reinterpret_cast<uint32_t *>(ia.codes);    // (4 bytes for every kMaximaRows rows)
-    i8_maxima_kernel<T><<<dim3((ia.cols + 511) / 512, count), dim3(256), 0, st>>>(ia, parts);
+    i8_maxima_kernel<T><<<dim3((ia.cols + 511) / 512 * count), dim3(256), 0, st>>>(ia, parts);
     i8_scales_kernel<<<dim3((ia.cols + 63) / 64), dim3(64), 0, st>>>(parts, count, ia.cols, ia.scales);
-    i8_turn_kernel<T><<<dim3((ia.cols + 63) / 64, (ia.rows + 127) / 128), dim3(256), 0, st>>>(ia);
+    const uint32_t tiles = (ia.cols + 63) / 64 * count;
+    static_assert(kMaximaRows == 128, "a row of tiles");
+    i8_turn_kernel<T><<<dim3(tiles < kMostGroups ? tiles : kMostGroups), dim3(256), 0, st>>>(ia);
     return static_cast<int>(hipGetLastError());
 }
 int launch_i8_columns(const I8Args &ia, bool bf16, void *stream) {
