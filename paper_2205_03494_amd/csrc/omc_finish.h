@@ -9,8 +9,8 @@ namespace omc {
 //   sigmoid  s = 1 / (1 + exp(-g)),          s (1 - s)
 //   swish    g s,                            s (1 + g (1 - s))
 //   gelu     g P, P = erfc(-g / sqrt 2) / 2, P + g exp(-g^2 / 2) / sqrt(2 pi)
-// With the hardware's exp2 and reciprocal, an error of 2^-23 each: a tile's results are all finished at the same time, when the matrix cores have nothing to do (8192 x 4096 x 1024 in 8 bits, swish: 155 us with the
-// library's expf and divisions and every column's scale and bias fetched for every value, 96 so and with these in LDS).  The exponent's rounding counts |x| 2^-24 of exp(x), which is worth 0.3 * 2^-24 of s and 0.4 * 2^-24 of P at most.
+// With the hardware's exp2 and reciprocal, an error of 2^-23 each: while a wave finishes results it multiplies nothing (8192 x 4096 x 1024 in 8 bits, swish: 155 us with the library's expf and divisions and every column's scale
+// and bias fetched for every value, 102 so and with these in LDS, 84 with a kind's arithmetic in a branch of its own).  The exponent's rounding counts |x| 2^-24 of exp(x), which is worth 0.3 * 2^-24 of s and 0.4 * 2^-24 of P at most.
 // P's tail, exp(-g^2 / 2) q(t) with t = 1 / (1 + 0.295 |g|) and q of degree 8, was fitted here to erfc by least squares, reweighted until the errors were even: within 7e-7 of itself and 1.6e-7 in all, in fp32.
 struct Gate {
     float value, part, rest;

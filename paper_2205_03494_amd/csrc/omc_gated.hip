@@ -5,22 +5,23 @@ namespace omc {
 
 // By an estimate of the time in us: `base` is a launch; `alone` a stage of workgroups that nothing else slows down, `resident` of them on a compute unit; `busy` what a stage costs per workgroup of a unit where all units have some
 // (of the last workgroups' unevenness over the units `uneven` counts); `store` the end of 256 tiles.  A row for every kind of product, the last one for both backward products in one launch, which takes no less than its longest
-// contraction.  Fitted to 2100 sizes of 33 .. 16384 x 64 .. 8192 x 64 .. 8192 in bf16, 60 % of them with whole cache lines: 4 - 16 % (standard deviation).  On these the chosen way takes 0.5 - 1.4 % longer than the best one (both
-// backward products together or apart: 2.6 %), at worst 13 - 50 %, of a few us.
-// 8192 x 4096 x 1024, gated: 256 x 256 150 us, 256 x 128 152, 128 x 128 157, 64 x 64 238; in 8 bits, plain: 42, 46, 43, 60; 8192 x 1024 x 4096: 48, 34, 35, 38.
-// 128 x 128 has two stages and two workgroups on a unit; with four stages, eight waves and the unit for itself 8192 x 4096 x 1024, gated, took 168 us.
+// contraction.  Fitted to 1500 sizes of 33 .. 16384 x 64 .. 8192 x 64 .. 8192 in bf16, 60 % of them with whole cache lines: 4 - 18 % (standard deviation).  On these the chosen way takes 0.8 - 1.7 % longer than the best one (both
+// backward products together or apart: 3 %), at worst 20 - 40 %.
+// In 256 x 256, 256 x 128, 128 x 128, 64 x 64: 8192 x 4096 x 1024 gated with slopes 147 us, 173, 170, 303; plain in 8 bits 41, 46, 48, 76; 8192 x 1024 x 4096 in 8 bits 49, 37, 37, 56.
+// 128 x 128 has two stages and two workgroups on a unit; with four stages, eight waves and the unit for itself 8192 x 4096 x 1024, gated, took 7 % longer.  64 x 64 is bound by its fragments' reads: a ring of eight stages, or
+// whole stages of fragments read ahead, do not help it.
 // A cut costs a second launch and the parts' way through memory.
 struct TileCost {
     double base, alone, busy, uneven, store;
 };
 static constexpr int kPair = 5;
 static constexpr TileCost kCosts[6][4] = {
-    {{2.031, 1.341, 0.3, 0.5, 10.24}, {2.936, 0.497, 1.121, 0.441, 3.521}, {4.058, 0.246, 0.593, 0.637, 1.522}, {3.617, 0.239, 0.188, 1.105, 0.686}},
-    {{2.781, 1.406, 0.1, 0.5, 8.55}, {4.195, 0.495, 0.856, 0.675, 3.131}, {4.303, 0.508, 0.429, 1.007, 1.445}, {3.653, 0.261, 0.181, 1.204, 0.68}},
-    {{0.0, 1.286, 0.3, 0.5, 14.292}, {3.132, 0.454, 0.855, 0.691, 6.042}, {2.881, 0.562, 0.428, 1.104, 3.168}, {3.507, 0.272, 0.183, 1.279, 1.214}},
-    {{2.467, 1.219, 0.1, 0.5, 8.363}, {3.369, 0.405, 0.793, 0.774, 2.976}, {2.535, 0.572, 0.393, 1.177, 1.887}, {3.34, 0.264, 0.188, 1.099, 0.497}},
-    {{8.689, 1.217, 1.015, 0.5, 17.326}, {7.594, 0.075, 0.749, 0.883, 8.209}, {3.302, 0.619, 0.387, 1.442, 4.197}, {3.518, 0.278, 0.194, 1.256, 0.832}},
-    {{0.0, 1.145, 0.357, 0.5, 24.809}, {5.328, 0.66, 0.783, 0.986, 8.287}, {0.246, 0.623, 0.399, 1.662, 4.664}, {2.813, 0.276, 0.195, 1.667, 1.257}},
+    {{3.466, 0.337, 1.563, 0.488, 7.359}, {2.402, 0.457, 1.072, 0.428, 4.107}, {3.841, 0.328, 0.542, 0.732, 1.766}, {3.612, 0.244, 0.176, 1.296, 0.717}},
+    {{4.011, 1.148, 1.016, 0.5, 6.658}, {3.992, 0.478, 0.808, 0.675, 3.359}, {4.219, 0.512, 0.396, 1.099, 1.552}, {3.664, 0.267, 0.171, 1.308, 0.703}},
+    {{0.0, 1.13, 0.1, 0.5, 13.894}, {2.922, 0.058, 0.81, 0.679, 6.142}, {3.016, 0.578, 0.401, 1.109, 3.066}, {3.502, 0.292, 0.17, 1.385, 1.221}},
+    {{3.21, 1.116, 1.0, 0.5, 6.889}, {3.37, 0.0, 0.782, 0.783, 2.987}, {2.343, 0.591, 0.349, 1.276, 2.005}, {3.259, 0.279, 0.174, 1.207, 0.559}},
+    {{13.282, 1.166, 0.295, 0.5, 14.331}, {8.797, 0.568, 0.767, 0.878, 7.586}, {3.843, 0.633, 0.355, 1.452, 4.038}, {3.567, 0.271, 0.182, 1.415, 0.82}},
+    {{0.0, 1.042, 1.365, 0.679, 18.915}, {7.069, 0.678, 0.801, 0.908, 6.896}, {0.0, 0.637, 0.362, 1.654, 4.634}, {2.755, 0.29, 0.186, 1.903, 1.317}},
 };
 static constexpr uint32_t kResident[] = {1, 1, 2, 2};
 

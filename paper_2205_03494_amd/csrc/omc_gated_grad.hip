@@ -10,7 +10,8 @@ int launch_across_both(const TiledArgs &pa, bool whole, bool c_bf16, hipStream_t
     return c_bf16 ? launch_tiles<false, false, true, true, BF16>(pa, whole, st) : launch_tiles<false, false, true, true, F32>(pa, whole, st);
 }
 
-// Both in one launch, in tiles of one size, and the biases' gradients.  8192 x 4096 x 1024: two launches of 128 tiles of 256 x 128 each 242 us, 256 of 256 x 256 in one 210.
+// Both in one launch, in tiles of one size, and the biases' gradients.  8192 x 4096 x 1024: 256 tiles of 256 x 256 in one launch, a backward pass
+// of 270 us with the slopes before them; in two launches, whose 128 such tiles leave half of the chip idle, in tiles of 256 x 128 at best, 302.
 template <typename T>
 static int launch_pair_typed(int tile, const TiledArgs &dx, const TiledArgs &dw, const ColumnSums &sums, hipStream_t st) {
     PairGrid pg{grid_of(dx, tile, false, 1), grid_of(dw, tile, false, 1), 0, sums};

@@ -11,6 +11,8 @@
 // The order of reads and products is written down: a column of tiles at a time, A's fragments of the next step beside the first products, B's each as soon as its predecessor has been multiplied for the last time; a
 // stage's second step is multiplied behind the barrier of the next stage, under that one's first reads and the loads of the one that is asked for.  A workgroup's tiles follow each other without a gap: the loads
 // of the next tile are under way while the last stages of this one are multiplied.
+// What bounds it: large products the power limit (16384 x 8192 x 8192 in 8 bits 805 - 830 us, 2.65 - 2.73 POP/s, the library's 978; gated 8192 x 4096 x 4096 in bf16 412 us, 1.33 PFLOP/s); a gated one with a short contraction the
+// way of its results, 200 MB with slopes, which the products hide in part: 8192 x 4096 x 1024 145 us, 40 of which its results take by themselves at 5 TB/s, and its products 95.
 #pragma once
 #include "omc_column_sums.h"
 #include "omc_finish.h"
@@ -304,8 +306,8 @@ __device__ __forceinline__ void tiles_body(const TileGrid &tg, const uint32_t bl
                 else return Columns{zero, zero, line(0, j), line(1, j)};
             };
             constexpr uint32_t kTogether = TH % 2 == 0 ? 2 : 1;
-            // Large results in bf16 go past the caches: gated 8192 x 4096 x 1024 with slopes 168 -> 150 us, in 8 bits 102 -> 96 us; plain 8192 x 4096 x 1024 in 8 bits 42 us, 44 so.
-            const bool streams = static_cast<uint64_t>(g.M) * g.N >= (GATED ? 16u << 20 : 64u << 20) && (f.ldc | f.ld_slope) % 64 == 0 &&
+            // A gated product's large results in bf16 go past the caches: 8192 x 4096 x 1024 with slopes 156 -> 145 us, without 116 -> 113.  Plain ones do not: 8192 x 4096 x 1024 in 8 bits 37 us, 45 so.
+            const bool streams = GATED && static_cast<uint64_t>(g.M) * g.N >= 16u << 20 && (f.ldc | f.ld_slope) % 64 == 0 &&
                                  ((reinterpret_cast<uintptr_t>(f.c) | reinterpret_cast<uintptr_t>(f.slope_g) | reinterpret_cast<uintptr_t>(f.slope_u)) & 15u) == 0;
             auto rows = [&](auto kind, auto keep, auto whole) {
                 constexpr bool KEEP = decltype(keep)::value, WHOLE = decltype(whole)::value;

@@ -31,13 +31,13 @@ def tile_of(kind, M, N, K):
     return c % 16, c // 16
 
 
-I8_CASES = [(0, 1, 1561, 8968, 277), (1, 4, 8629, 66, 8985), (1, 1, 925, 6174, 20), (2, 8, 2080, 66, 8051), (2, 1, 7949, 322, 20), (3, 4, 34, 34, 1904), (3, 1, 34, 35, 20),
-            (0, 1, 4096, 4096, 512), (3, 16, 33, 33, 64000)]
-I8_GATED_CASES = [(0, 1, 918, 7833, 514), (1, 4, 8772, 36, 6440), (1, 1, 1175, 4991, 131), (2, 8, 65, 1093, 8709), (2, 1, 211, 6472, 20), (3, 4, 36, 34, 1751), (3, 1, 34, 35, 20)]
-GATED_CASES = [(0, 4, 257, 3624, 8349), (0, 1, 772, 8117, 20), (1, 4, 8984, 35, 4426), (1, 1, 408, 8189, 21), (2, 8, 2079, 34, 4616), (2, 1, 66, 8840, 21), (3, 4, 35, 34, 902), (3, 1, 34, 35, 20)]
-DX_CASES = [(0, 8, 6251, 8849, 135), (0, 1, 1848, 134, 7447), (1, 16, 2254, 6353, 65), (1, 1, 4376, 33, 2697), (2, 16, 1100, 3909, 65), (2, 1, 8980, 38, 193), (3, 8, 34, 942, 20), (3, 1, 2013, 34, 21)]
-DW_CASES = [(0, 1, 495, 6374, 2200), (1, 4, 8950, 4157, 73), (1, 1, 2250, 8209, 199), (2, 16, 7967, 1063, 70), (2, 1, 67, 2211, 1374), (3, 16, 2013, 34, 21), (3, 1, 34, 942, 20)]
-PAIRS = [(0, 1299, 585, 4947), (1, 2366, 891, 981), (2, 69, 35, 8534), (3, 34, 35, 20)]
+I8_CASES = [(0, 1, 1818, 7944, 21), (1, 1, 3668, 1538, 20), (1, 4, 8629, 66, 8985), (2, 1, 8996, 265, 22), (2, 8, 2204, 71, 6736), (3, 1, 35, 34, 21), (3, 8, 35, 34, 1996), (0, 1, 4096, 4096, 512),
+            (3, 16, 33, 33, 64000)]
+I8_GATED_CASES = [(0, 1, 4072, 1936, 20), (1, 1, 900, 6386, 141), (1, 4, 8553, 34, 5566), (2, 1, 268, 4834, 20), (2, 8, 65, 1093, 8709), (3, 1, 35, 34, 21), (3, 4, 36, 34, 1751)]
+GATED_CASES = [(0, 1, 6411, 1043, 20), (0, 4, 268, 3404, 6889), (1, 1, 443, 8122, 21), (1, 4, 8328, 34, 4964), (2, 1, 66, 8840, 21), (2, 8, 2054, 33, 4930), (3, 1, 35, 34, 21), (3, 4, 33, 34, 772)]
+DX_CASES = [(0, 1, 1815, 34, 7988), (0, 8, 130, 6597, 5609), (1, 1, 4376, 33, 2697), (1, 4, 8294, 7085, 21), (2, 1, 8980, 38, 193), (2, 16, 66, 4420, 1105), (3, 1, 1841, 34, 20), (3, 8, 34, 942, 20)]
+DW_CASES = [(0, 1, 67, 8295, 4548), (1, 1, 3857, 8319, 200), (1, 2, 8119, 8508, 70), (2, 1, 132, 8430, 359), (2, 16, 7727, 1027, 66), (3, 1, 34, 942, 20), (3, 8, 1841, 34, 20)]
+PAIRS = [(0, 903, 348, 7508), (1, 3006, 1755, 586), (2, 66, 34, 7328), (3, 35, 34, 21)]
 
 
 @pytest.mark.parametrize("c_type", [F32, BF16])
