@@ -11,8 +11,8 @@
 // The order of reads and products is written down: a column of tiles at a time, A's fragments of the next step beside the first products, B's each as soon as its predecessor has been multiplied for the last time; a
 // stage's second step is multiplied behind the barrier of the next stage, under that one's first reads and the loads of the one that is asked for.  A workgroup's tiles follow each other without a gap: the loads
 // of the next tile are under way while the last stages of this one are multiplied.
-// What bounds it: large products the power limit (16384 x 8192 x 8192 in 8 bits 805 - 830 us, 2.65 - 2.73 POP/s, the library's 978; gated 8192 x 4096 x 4096 in bf16 412 us, 1.33 PFLOP/s); a gated one with a short contraction the
-// way of its results, 200 MB with slopes, which the products hide in part: 8192 x 4096 x 1024 145 us, 40 of which its results take by themselves at 5 TB/s, and its products 95.
+// What bounds it: large products the power limit (16384 x 8192 x 8192 in 8 bits 780 - 830 us, 2.65 - 2.8 POP/s, the library's 957 - 978; gated 8192 x 4096 x 4096 in bf16 412 us, 1.33 PFLOP/s); a gated one with a short contraction the
+// way of its results, 200 MB with slopes, which the products hide in part: 8192 x 4096 x 1024 124 - 145 us, 40 of which its results take by themselves at 5 TB/s, and its products 95.
 #pragma once
 #include "omc_column_sums.h"
 #include "omc_finish.h"
