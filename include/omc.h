@@ -516,7 +516,8 @@ omc_status omc_mx4_linear_backward(const void *dY, uint64_t lddy, const void *X,
  * A matrix of `rows` rows of `cols` values is held in two buffers.
  *     codes    omc_i8_code_bytes: row r begins at byte r * 128 * ceil(cols / 128), a signed byte for every value, zeros behind them
  *     scales   a float for every row
- * codes must be 16-byte aligned; other tensors here and of the gated layer need only the alignment of their elements, and rows of theirs may lie apart (ld).  Dimensions as for MX4;
+ * codes must be 16-byte aligned; other tensors here and of the gated layer need only the alignment of their elements, and rows of theirs may lie apart (ld); what a call writes, its workspace among it,
+ * overlaps neither what it reads nor the rest of what it writes.  Dimensions as for MX4;
  * K, along which two codes' products are added up in 32-bit integers, is at most 131071 (OMC_ERR_SIZE). */
 size_t omc_i8_code_bytes(uint32_t rows, uint32_t cols);   /* 0 if the sizes are out of range */
 
@@ -524,7 +525,7 @@ size_t omc_i8_code_bytes(uint32_t rows, uint32_t cols);   /* 0 if the sizes are 
  *   x              device, rows x cols values of `type`, row stride ldx
  *   by_columns     0: a scale for every row (a token, a frame); codes of rows x cols, `rows` scales.  Otherwise a scale for every column (a channel of K x N weights):
  *                  codes and scales are those of the transpose, cols x rows, `cols` scales
- *   codes, scales  device, written whole, paddings too; must not overlap x
+ *   codes, scales  device, written whole, paddings too
  *   values         device or NULL, rows x cols of `type`, row stride ldv: what codes and scales stand for, rounded once to `type` */
 omc_status omc_i8_quantize(const void *x, omc_type type, uint32_t rows, uint32_t cols, uint64_t ldx, int by_columns, void *codes, float *scales, void *values, uint64_t ldv, void *stream);
 

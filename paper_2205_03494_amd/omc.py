@@ -742,7 +742,7 @@ def omc_gated_linear_backward(dH: torch.Tensor, slope_g: torch.Tensor, slope_u: 
     """dH, slopes [M, N]; X, dX [M, K]; weights, dWg and dWu [N, K] (gradients fp32); dbg, dbu [N] fp32.  Without dX the weights, without
     dWg and dWu X may be None (K is taken from whichever is there)."""
     M, N = dH.shape
-    K = next((t.shape[1] for t in (X, dX, dWg) if t is not None), 1)
+    K = next((t.shape[1] for t in (X, dX, Wg, dWg) if t is not None), 1)
     pdh, hkind, lddh = _matrix(dH)
     sg, su, lds = _slopes(slope_g, slope_u, M, N)
     px, xkind, ldx = (None, OMC_F32, 0) if X is None else _rows_like(X, M, K)

@@ -254,6 +254,18 @@ def test_gated_linear_backward(M, N, K, dh_type, x_type, w_type, dx_type, pad):
         assert torch.equal(a, b)
 
 
+def test_biases_gradients_alone_beside_weights():
+    """K is whichever tensor tells it, the weights too where nothing else is there."""
+    M, N, K = 70, 40, 24
+    _, Wg, Wu, _, _ = layer(M, N, K, F32, F32, 0)
+    dH, sg, su = rand(M, N, 25, F32), rand(M, N, 26, BF16), rand(M, N, 27, BF16)
+    ws = space(omc.omc_gated_linear_backward_workspace_bytes(M, N, K))[1]
+    sums = [torch.empty(N, device="cuda") for _ in range(4)]
+    omc.omc_gated_linear_backward(dH, sg, su, None, Wg, Wu, None, None, None, sums[0], sums[1], ws)
+    omc.omc_gated_linear_backward(dH, sg, su, None, None, None, None, None, None, sums[2], sums[3], ws)
+    assert torch.equal(sums[0], sums[2]) and torch.equal(sums[1], sums[3])
+
+
 @pytest.mark.parametrize("gate", GATES)
 @pytest.mark.parametrize("M,N,K", [(7, 24, 40), (96, 72, 64)])
 def test_gradients_against_differences(M, N, K, gate):
