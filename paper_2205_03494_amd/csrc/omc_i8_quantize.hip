@@ -129,9 +129,11 @@ __global__ __launch_bounds__(1024) void i8_columns_kernel(I8Args ia) {
         }
         float r[4][4], far = 0.0f;
 #pragma unroll
-        for (uint32_t k = 0; k < 4; ++k)
+        for (uint32_t k = 0; k < 4; ++k) {
+            if (first + kLines * k >= ia.rows) break;
 #pragma unroll
             for (int i = 0; i < 4; ++i) r[k][i] = to[i].near(v[k][i], far);
+        }
         if (far > Rounding::kFar || special) {
 #pragma unroll
             for (uint32_t k = 0; k < 4; ++k)
@@ -140,6 +142,7 @@ __global__ __launch_bounds__(1024) void i8_columns_kernel(I8Args ia) {
         }
 #pragma unroll
         for (uint32_t k = 0; k < 4; ++k) {
+            if (first + kLines * k >= ia.rows) break;   // (kLines is whole 128s: no codes there either)
             const uint32_t row = first + kLines * k + line;
 #pragma unroll
             for (uint32_t i = 0; i < 4; ++i) {
@@ -276,7 +279,7 @@ int launch_i8_rows(const I8Args &ia, bool bf16, void *stream) {
     hipStream_t st = static_cast<hipStream_t>(stream);
     return bf16 ? launch_rows<BF16>(ia, st) : launch_rows<F32>(ia, st);
 }
-// Columns of 1024 x 1024 in fp32 8.7 us in one launch, 12.2 in three; 2048 x 1024 11.3 and 13.3; 4096 x 256 19.5 and 13.4; 1024 x 4096 23.4 and 16.5; 100 x 8192 21.8 and 13.6; 8192 x 8192 362 and 113;
+// Strips of four columns: 971 x 243 in fp32 with values 8.3 -> 9.3 us, 2048 x 2048 23.6 -> 42.  Columns of 1024 x 1024 in fp32 8.7 us in one launch, 12.2 in three; 2048 x 1024 11.3 and 13.3; 4096 x 256 19.5 and 13.4; 1024 x 4096 23.4 and 16.5; 100 x 8192 21.8 and 13.6; 8192 x 8192 362 and 113;
 // 16384 x 8192 in bf16 593 and 158, which reads the matrix twice: 4.3 TB/s.  (Fewer than eight columns go in one launch whatever their length.)
 constexpr uint32_t kStripRows = 2048, kStripCols = 2048;
 template <typename T>
