@@ -1,7 +1,8 @@
 // Device side of I8: a row of values shares a scale and holds a whole number each.
 //
 //   a = max |x_i|,  s = a * (1 / 127), both rounded to fp32,  code_i = the whole number nearest to x_i / s, ties to even.
-// (A product and not a quotient: a last place of s more or less is none of any value's, since codes go by the s that is kept.)
+// (The product and not the quotient a / 127, which is a last place away for one fp32 row in twenty and for 6 of bf16's 128 significands.  That place decides a value halfway between two codes by its row's scale, as a / 2 is in
+// bf16, so the format has to name one of them.)
 // The quotient is never formed exactly: r = rint(x * (1 / s)) is off by at most one, and d = x - r s, which fp32 holds exactly (r = 0: x itself; r = 1: both are within a factor of two; otherwise x > s, and d is a
 // multiple of s' last place below s / 2 and a little), says whether the neighbour is nearer.  That is asked where x * (1 / s) comes within 2^-12 of halfway between two whole numbers (it is off by 2^-15 at most).  Scales below 2^-100 are handled times 2^100, which is exact.
 #pragma once
