@@ -10,7 +10,7 @@ namespace omc {
 //   swish    g s,                            s (1 + g (1 - s))
 //   gelu     g P, P = erfc(-g / sqrt 2) / 2, P + g exp(-g^2 / 2) / sqrt(2 pi)
 // With the hardware's exp2 and reciprocal, an error of 2^-23 each: while a wave finishes results it multiplies nothing (8192 x 4096 x 1024 in 8 bits, swish: 155 us with the library's expf and divisions and every column's scale
-// and bias fetched for every value, 102 so and with these in LDS, 84 with a kind's arithmetic in a branch of its own).  The exponent's rounding counts |x| 2^-24 of exp(x), which is worth 0.3 * 2^-24 of s and 0.4 * 2^-24 of P at most.
+// and bias fetched for every value, 102 so and with these in LDS, 84 with a kind's arithmetic in a branch of its own; 70 - 73 now that one wave multiplies while another finishes).  The exponent's rounding counts |x| 2^-24 of exp(x), which is worth 0.3 * 2^-24 of s and 0.4 * 2^-24 of P at most.
 // P's tail, exp(-g^2 / 2) q(t) with t = 1 / (1 + 0.295 |g|) and q of degree 8, was fitted here to erfc by least squares, reweighted until the errors were even, 4.4e-7 of itself.  In fp32, measured: P is within 2.2e-7 in all; the tail
 // within 7e-7 of itself up to |g| = 3, and farther out by what the exponent's two roundings are worth, g^2 2^-24: 1.8e-6 at 5, 5e-6 at 10, 8.4e-6 at 13.  s for g < 0 likewise, by |g| 2^-24: 3.4e-7 up to 5, 9e-7 at 12, 3.9e-6 at 80.
 struct Gate {

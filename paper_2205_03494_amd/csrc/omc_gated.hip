@@ -7,7 +7,7 @@ namespace omc {
 // (of the last workgroups' unevenness over the units `uneven` counts); `store` the end of 256 tiles.  A row for every kind of product, the last one for both backward products in one launch, which takes no less than its longest
 // contraction.  Fitted to 1500 sizes of 33 .. 16384 x 64 .. 8192 x 64 .. 8192 in bf16, 60 % of them with whole cache lines: 4 - 18 % (standard deviation).  On these the chosen way takes 0.8 - 1.7 % longer than the best one (both
 // backward products together or apart: 3 %), at worst 20 - 40 %.
-// In 256 x 256, 256 x 128, 128 x 128, 64 x 64: 8192 x 4096 x 1024 gated with slopes 147 us, 173, 170, 303; plain in 8 bits 41, 46, 48, 76; 8192 x 1024 x 4096 in 8 bits 49, 37, 37, 56.
+// In 256 x 256, 256 x 128, 128 x 128, 64 x 64: 8192 x 4096 x 1024 gated with slopes 143 us, 170, 166, 300; without 110, 127, 127, 218; plain in 8 bits 40, 46, 46, 73; 8192 x 1024 x 4096 in 8 bits 48, 36, 37, 54.
 // 128 x 128 has two stages and two workgroups on a unit; with four stages, eight waves and the unit for itself 8192 x 4096 x 1024, gated, took 7 % longer.  64 x 64 is bound by its fragments' reads: a ring of eight stages, or
 // whole stages of fragments read ahead, do not help it.
 // A cut costs a second launch and the parts' way through memory.

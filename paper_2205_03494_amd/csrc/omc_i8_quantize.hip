@@ -279,8 +279,11 @@ int launch_i8_rows(const I8Args &ia, bool bf16, void *stream) {
     hipStream_t st = static_cast<hipStream_t>(stream);
     return bf16 ? launch_rows<BF16>(ia, st) : launch_rows<F32>(ia, st);
 }
-// Strips of four columns: 971 x 243 in fp32 with values 8.3 -> 9.3 us, 2048 x 2048 23.6 -> 42.  Columns of 1024 x 1024 in fp32 8.7 us in one launch, 12.2 in three; 2048 x 1024 11.3 and 13.3; 4096 x 256 19.5 and 13.4; 1024 x 4096 23.4 and 16.5; 100 x 8192 21.8 and 13.6; 8192 x 8192 362 and 113;
-// 16384 x 8192 in bf16 593 and 158, which reads the matrix twice: 4.3 TB/s.  (Fewer than eight columns go in one launch whatever their length.)
+// In a graph, fp32 / bf16, in one launch and in three.  Up to the limits, without values: 971 x 243 7.4 / 7.8 us and 15.5 / 15.4, 1024 x 1024 10.2 / 10.1 and 13.8 / 12.5, 1024 x 2048 12.1 / 12.1 and 15.5 / 14.7, 2048 x 1024 14.3 / 13.4
+// and 15.8 / 14.7, 2048 x 1536 17.0 / 15.5 and 16.9 / 16.4, 2048 x 2048 18.4 / 17.6 and 18.4 / 16.7.  With values three win in the far corner, by 3 us at most: 2048 x 1024 18.5 / 15.1 and 16.9 / 15.4, 2048 x 1536 21.4 / 17.3 and 18.7 / 17.4,
+// 2048 x 2048 23.6 / 20.2 and 20.7 / 18.0 (1024 x 2048: 14.5 / 13.9 and 16.7 / 15.7); one rule for both.  Beyond: 1024 x 4096 21.8 / 21.6 and 17.0 / 16.4, 4096 x 1024 36.5 / 32.0 and 18.2 / 17.4; 8192 x 8192 in fp32 362 and 113;
+// 16384 x 8192 in bf16 593 and 158, which reads the matrix twice: 4.3 TB/s.  Strips of four columns instead of eight: 971 x 243 in fp32 with values 8.3 -> 9.3 us, 2048 x 2048 23.6 -> 42.
+// Fewer than eight columns go in one launch whatever their length, since the others' loads are of eight: all in one workgroup, 0.23 ms for 65536 x 7 in fp32, 4.4 for 2^20 x 7, 90 for 2^24 x 7 (of eight columns, in three launches, 0.4 and 7.1).
 constexpr uint32_t kStripRows = 2048, kStripCols = 2048;
 template <typename T>
 static int launch_columns(const I8Args &ia, hipStream_t st) {
